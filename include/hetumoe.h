@@ -5,10 +5,14 @@
  * The calls follow Algorithm 1 of the paper (one training step of an MoE layer):
  *   step 1  W, id = Gate(x)                      -> moe_gate
  *   step 2  x' = Layout_Transform(x, id)         -> moe_dispatch
+ *   step 4  y' = Experts(x')                     -> moe_experts
  *   step 6  y = Reverse_Layout_Transform(y', id) -> moe_combine (gate-weighted)
  * plus the gradients of steps 2 and 6            -> moe_dispatch_bwd, moe_combine_bwd,
- * and of step 1                                  -> moe_gate_bwd.
- * Steps 3-5 (AllToAll and the expert networks) are outside this library.
+ * of step 4                                      -> moe_experts_bwd,
+ * and of step 1                                  -> moe_gate_bwd;
+ * the clipping of all gradients by their norm    -> moe_grad_norm, moe_grad_clip;
+ * and the whole layer for a few tokens           -> moe_token_layer.
+ * Steps 3 and 5 (AllToAll) are outside this library.
  *
  * Conventions shared by every call
  * --------------------------------
@@ -426,6 +430,165 @@ MOE_API moe_status moe_gate_bwd(const moe_gate_bwd_params* p, const void* x, con
                                 float* dlogits, void* dx, float* dwg, float* dbias,
                                 float* aux_loss, void* workspace, size_t workspace_bytes,
                                 hipStream_t stream);
+
+/* Activations of the expert networks. */
+typedef enum {
+  MOE_ACT_RELU = 0, /* max(a, 0) */
+  MOE_ACT_GELU = 1, /* the tanh form, 0.5 a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) */
+  MOE_ACT_SILU = 2  /* a / (1 + exp(-a)) */
+} moe_act;
+
+/* Parameters of moe_experts and moe_experts_bwd (host memory). */
+typedef struct {
+  int32_t E;        /* experts */
+  int32_t capacity; /* C: slots per expert */
+  int32_t d;        /* model width */
+  int32_t h;        /* width of the hidden rows */
+  int32_t act;      /* moe_act */
+  int32_t gated;    /* 0: hidden = act(pre), w1 has h1 = h columns;
+                       1: hidden = act(pre[:h]) * pre[h:], w1 has h1 = 2 h columns */
+  int32_t dtype;    /* moe_dtype of the rows, the weights and their gradients */
+} moe_experts_params;
+
+/*
+ * moe_experts -- step 4 of Algorithm 1: the expert networks, two linear layers
+ * each, on the rows that moe_dispatch laid out.  For the first counts[e] rows of
+ * each expert:
+ *   pre    = xe w1[e] + b1[e]
+ *   hidden = act(pre), or act(pre[:h]) * pre[h:] when gated
+ *   ye     = hidden w2[e] + b2[e]
+ * The rows behind counts[e] are not read, whatever they hold, and are zero in
+ * every output.  Sums are fp32 (each 256 terms of fp32 products on their own);
+ * pre and hidden are rounded once to dtype, hidden from the unrounded pre, and
+ * the second product reads the rounded hidden.
+ *
+ * Inputs   xe [E,C,d]; w1 [E,d,h1], w2 [E,h,d] (dtype); b1 [E,h1], b2 [E,d] fp32 or
+ *          NULL (zero); counts [E] int32, as written by moe_gate, or NULL (all C;
+ *          values outside [0, C] are taken as the nearer end).
+ * Outputs  pre [E,C,h1] or NULL (needed by moe_experts_bwd), hidden [E,C,h], ye
+ *          [E,C,d].
+ * Range    d and h up to 2^20, their rows multiples of 16 bytes; every matrix
+ *          16-byte aligned.  E * C = 0 does nothing.
+ */
+MOE_API moe_status moe_experts(const moe_experts_params* p, const void* xe, const void* w1,
+                               const float* b1, const void* w2, const float* b2,
+                               const int32_t* counts, void* pre, void* hidden, void* ye,
+                               hipStream_t stream);
+
+/* Bytes of device workspace moe_experts_bwd needs for `p` (the gradient of pre,
+ * [E,C,h1], and sums for the biases). */
+MOE_API moe_status moe_experts_bwd_workspace_size(const moe_experts_params* p, size_t* bytes);
+
+/*
+ * moe_experts_bwd -- gradient of moe_experts, from the gradient dye of ye and the
+ * pre and hidden that moe_experts wrote.  Over the first counts[e] rows c:
+ *   dhidden = dye w2[e]^T
+ *   dpre    = dhidden * act'(pre);  gated: the first h columns dhidden * pre[h:] *
+ *             act'(pre[:h]), the others dhidden * act(pre[:h])
+ *   dxe     = dpre w1[e]^T              dw1[e] = sum_c xe[c]^T dpre[c]
+ *   db1[e]  = sum_c dpre[c]             dw2[e] = sum_c hidden[c]^T dye[c]
+ *   db2[e]  = sum_c dye[c]
+ * The derivative of relu at 0 is 0.  Sums are fp32; dpre is rounded to dtype for
+ * the products that read it, db1 adds it unrounded; dxe, dw1 and dw2 are rounded
+ * once.  Sums over rows run in a fixed order (no atomics): bitwise reproducible.
+ *
+ * Inputs   as moe_experts (rows behind counts[e] are not read); pre [E,C,h1], hidden
+ *          [E,C,h].  An input that none of the outputs asked for needs may be NULL: xe
+ *          serves dw1, w1 dxe, hidden dw2, w2 and pre dxe, dw1 and db1.
+ * Outputs  each optional (NULL skips it): dxe [E,C,d] (zero behind counts[e]), dw1
+ *          [E,d,h1], dw2 [E,h,d] (dtype); db1 [E,h1], db2 [E,d] fp32.  An expert
+ *          without rows gets zero gradients.
+ * Workspace device memory of at least moe_experts_bwd_workspace_size() bytes,
+ *          16-byte aligned; contents on entry are ignored.
+ */
+MOE_API moe_status moe_experts_bwd(const moe_experts_params* p, const void* dye, const void* xe,
+                                   const void* w1, const void* w2, const int32_t* counts,
+                                   const void* pre, const void* hidden, void* dxe, void* dw1,
+                                   float* db1, void* dw2, float* db2, void* workspace,
+                                   size_t workspace_bytes, hipStream_t stream);
+
+/* Most tokens of one moe_token_layer call. */
+#define MOE_TOKEN_LAYER_MAX 256
+
+/* Parameters of moe_token_layer (host memory). */
+typedef struct {
+  moe_gate_params gate; /* as for moe_gate, with capacity 0 and logits_in 0 */
+  int32_t h;            /* as moe_experts_params */
+  int32_t act;
+  int32_t gated;
+  int32_t routed;       /* 1: ids and weights are inputs (of another gate); of `gate`, only S, d, E, k
+                           and dtype count, and wg, bias, noise, token_ids, hash_table are NULL */
+} moe_token_layer_params;
+
+/* Bytes of device workspace moe_token_layer needs for `p`. */
+MOE_API moe_status moe_token_layer_workspace_size(const moe_token_layer_params* p, size_t* bytes);
+
+/*
+ * moe_token_layer -- the whole layer for a few tokens (a decoding step), without
+ * slots: nothing is dropped.
+ *   y[s] = sum_r weights[s,r] * expert_{ids[s,r]}(x[s])
+ * with ids and weights as moe_gate gives them for the same parameters and inputs,
+ * and the expert networks of moe_experts (hidden rounded once to dtype).  Only the
+ * weights of experts that a token chose are read.  fp32 sums, rounded once.
+ *
+ * Inputs   x [S,d], S <= MOE_TOKEN_LAYER_MAX; wg, bias, token_ids, noise, hash_table
+ *          as moe_gate (x is required for HASH too); w1, b1, w2, b2 as moe_experts.
+ *          With routed, ids [S,k] and weights [S,k] are inputs; an id outside [0, E)
+ *          stands for no expert (padding) and adds nothing.
+ * Outputs  y [S,d]; ids and weights [S,k] unless routed.
+ * Range    d h1 and S k h elements within 2^31 bytes, else MOE_ERR_UNSUPPORTED.
+ * Workspace device memory of at least moe_token_layer_workspace_size() bytes,
+ *          16-byte aligned; contents on entry are ignored.
+ */
+MOE_API moe_status moe_token_layer(const moe_token_layer_params* p, const void* x, const void* wg,
+                                   const float* bias, const int32_t* token_ids, const float* noise,
+                                   const int32_t* hash_table, const void* w1, const float* b1,
+                                   const void* w2, const float* b2, int32_t* ids, float* weights,
+                                   void* y, void* workspace, size_t workspace_bytes,
+                                   hipStream_t stream);
+
+/* One gradient of moe_grad_norm and moe_grad_clip: n elements of device memory
+ * with natural alignment (the descriptors themselves are host memory). */
+typedef struct {
+  const void* src;
+  void* dst;     /* moe_grad_clip: where the clipped gradient goes; may be src */
+  int64_t n;
+  int32_t dtype; /* moe_dtype of src and dst */
+  int32_t pad;
+} moe_grad_tensor;
+
+/* Bytes of device workspace moe_grad_norm needs for these sizes (0 is possible). */
+MOE_API moe_status moe_grad_norm_workspace_size(const moe_grad_tensor* tensors, int32_t count,
+                                                size_t* bytes);
+
+/*
+ * moe_grad_norm -- the 2-norm of many gradients taken as one vector:
+ *   sumsq = sum over all tensors and elements of src^2, norm = sqrt(sumsq).
+ * Squares and sums are fp64 in a fixed order.  Ranks that hold different experts
+ * add their sumsq before moe_grad_clip.
+ *
+ * Outputs  sumsq [1] fp64 (8-byte aligned), norm [1] fp32; either may be NULL.  No
+ *          tensors give 0.  An infinity or NaN in a gradient shows in both.
+ * Workspace device memory of at least moe_grad_norm_workspace_size() bytes, 16-byte
+ *          aligned; contents on entry are ignored.
+ */
+MOE_API moe_status moe_grad_norm(const moe_grad_tensor* tensors, int32_t count, double* sumsq,
+                                 float* norm, void* workspace, size_t workspace_bytes,
+                                 hipStream_t stream);
+
+/*
+ * moe_grad_clip -- gradients scaled so that their norm is at most max_norm:
+ *   dst = src * scale, scale = min(1, max_norm / sqrt(sumsq)) in fp32,
+ * rounded once.  A norm of at most max_norm leaves the values as they are; a NaN
+ * norm makes the scale NaN.  In place (dst == src) a scale of 1 writes nothing.
+ *
+ * Inputs   sumsq [1] fp64 in device memory (moe_grad_norm's, or its sum over ranks);
+ *          max_norm finite and >= 0.
+ * Outputs  every dst; norm [1] fp32 = sqrt(sumsq), or NULL.  An output may overlap no
+ *          other tensor's output or input: a tensor listed twice is refused.
+ */
+MOE_API moe_status moe_grad_clip(const moe_grad_tensor* tensors, int32_t count, const double* sumsq,
+                                 float max_norm, float* norm, hipStream_t stream);
 
 /* Static description of a status code. */
 MOE_API const char* moe_status_string(moe_status s);

@@ -23,12 +23,16 @@ LIB_PATH = os.environ.get("HETUMOE_LIBRARY") or os.path.join(_PKG, "libhetumoe.s
 MOE_OK, MOE_ERR_INVALID_ARG, MOE_ERR_UNSUPPORTED, MOE_ERR_WORKSPACE, MOE_ERR_HIP, MOE_ERR_NOT_CONVERGED = range(6)
 MOE_F32, MOE_BF16 = 0, 1
 MOE_GATE_TOPK, MOE_GATE_KTOP1, MOE_GATE_HASH, MOE_GATE_HTOPK = 0, 1, 2, 3
+MOE_ACT_RELU, MOE_ACT_GELU, MOE_ACT_SILU = 0, 1, 2
+MOE_TOKEN_LAYER_MAX = 256
 
 EXPORTED = (
     "moe_gate_workspace_size", "moe_gate", "moe_gate_noalloc", "moe_dispatch", "moe_combine",
     "moe_dispatch_bwd", "moe_combine_bwd", "moe_gate_bwd_workspace_size", "moe_gate_bwd",
     "moe_hash_balanced_table", "moe_base_gate_workspace_size", "moe_base_gate",
-    "moe_base_gate_async", "moe_status_string", "moe_last_error", "moe_abi_version",
+    "moe_base_gate_async", "moe_experts", "moe_experts_bwd_workspace_size", "moe_experts_bwd",
+    "moe_token_layer_workspace_size", "moe_token_layer", "moe_grad_norm_workspace_size", "moe_grad_norm",
+    "moe_grad_clip", "moe_status_string", "moe_last_error", "moe_abi_version",
 )
 
 
@@ -75,6 +79,27 @@ class BaseInfo(ctypes.Structure):
     _fields_ = [("phases", ctypes.c_int32), ("rounds", ctypes.c_int32), ("eps", ctypes.c_double)]
 
 
+class ExpertsParams(ctypes.Structure):
+    _fields_ = [
+        ("E", ctypes.c_int32), ("capacity", ctypes.c_int32), ("d", ctypes.c_int32), ("h", ctypes.c_int32),
+        ("act", ctypes.c_int32), ("gated", ctypes.c_int32), ("dtype", ctypes.c_int32),
+    ]
+
+
+class TokenLayerParams(ctypes.Structure):
+    _fields_ = [
+        ("gate", GateParams), ("h", ctypes.c_int32), ("act", ctypes.c_int32), ("gated", ctypes.c_int32),
+        ("routed", ctypes.c_int32),
+    ]
+
+
+class GradTensor(ctypes.Structure):
+    _fields_ = [
+        ("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("n", ctypes.c_int64), ("dtype", ctypes.c_int32),
+        ("pad", ctypes.c_int32),
+    ]
+
+
 # moe_base_status, which moe_base_gate_async writes to device memory: 24 bytes,
 # read back as int32 [6] (phases, rounds, eps as two words, status, pad)
 BASE_STATUS_BYTES = 24
@@ -111,6 +136,20 @@ def load():
                                   vp, vp, ctypes.c_size_t, ctypes.POINTER(BaseInfo), vp]
     lib.moe_base_gate_async.argtypes = [ctypes.POINTER(BaseParams), vp, vp, f32p, f32p, i32p, i32p, f32p, i32p,
                                         i32p, vp, vp, ctypes.c_size_t, ctypes.c_int32, vp, vp]
+    sz, szp = ctypes.c_size_t, ctypes.POINTER(ctypes.c_size_t)
+    lib.moe_experts.argtypes = [ctypes.POINTER(ExpertsParams), vp, vp, f32p, vp, f32p, i32p, vp, vp, vp, vp]
+    lib.moe_experts_bwd_workspace_size.argtypes = [ctypes.POINTER(ExpertsParams), szp]
+    lib.moe_experts_bwd.argtypes = [ctypes.POINTER(ExpertsParams), vp, vp, vp, vp, i32p, vp, vp, vp, vp, f32p, vp, f32p,
+                                    vp, sz, vp]
+    lib.moe_token_layer_workspace_size.argtypes = [ctypes.POINTER(TokenLayerParams), szp]
+    lib.moe_token_layer.argtypes = [ctypes.POINTER(TokenLayerParams), vp, vp, f32p, i32p, f32p, i32p, vp, f32p, vp, f32p,
+                                    i32p, f32p, vp, vp, sz, vp]
+    lib.moe_grad_norm_workspace_size.argtypes = [ctypes.POINTER(GradTensor), ctypes.c_int32, szp]
+    lib.moe_grad_norm.argtypes = [ctypes.POINTER(GradTensor), ctypes.c_int32, vp, f32p, vp, sz, vp]
+    lib.moe_grad_clip.argtypes = [ctypes.POINTER(GradTensor), ctypes.c_int32, vp, ctypes.c_float, f32p, vp]
+    for name in ("moe_experts", "moe_experts_bwd_workspace_size", "moe_experts_bwd", "moe_token_layer_workspace_size",
+                 "moe_token_layer", "moe_grad_norm_workspace_size", "moe_grad_norm", "moe_grad_clip"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("moe_gate_workspace_size", "moe_gate", "moe_dispatch", "moe_combine",
                  "moe_dispatch_bwd", "moe_combine_bwd", "moe_gate_bwd_workspace_size", "moe_gate_bwd",
                  "moe_hash_balanced_table", "moe_base_gate_workspace_size", "moe_base_gate",
@@ -506,3 +545,221 @@ def gate_bwd(kind, logits, ids, dw, *, x=None, wg=None, normalize=0, dx=None, ac
     moe_gate_bwd(params, x if want_dwg else None, wg if want_dx else None, logits, ids, dw, out["dlogits"],
                  out["dx"], out["dwg"], out["dbias"], out["aux_loss"], ws, stream)
     return out
+
+
+# ---------------------------------------------------------------- expert networks
+
+def experts_params(E, capacity, d, h, act=MOE_ACT_RELU, gated=False, dtype=MOE_F32):
+    return ExpertsParams(E, capacity, d, h, act, int(bool(gated)), dtype)
+
+
+def _expert_sizes(p):
+    """Elements of xe / ye, of w1, of w2, of pre, of hidden, and h1."""
+    E, C, d, h = p.E, p.capacity, p.d, p.h
+    h1 = 2 * h if p.gated else h
+    return E * C * d, E * d * h1, E * h * d, E * C * h1, E * C * h, h1
+
+
+def _dt(code):
+    return torch.bfloat16 if code == MOE_BF16 else torch.float32
+
+
+def _bytes(workspace):
+    return 0 if workspace is None else workspace.numel() * workspace.element_size()
+
+
+def moe_experts(params, xe, w1, b1, w2, b2, counts, pre, hidden, ye, stream=None):
+    dt, f32 = _dt(params.dtype), torch.float32
+    rows, n1, n2, npre, nhid, h1 = _expert_sizes(params)
+    E = params.E
+    _check(load().moe_experts(
+        ctypes.byref(params), _ptr(xe, dt, "xe", rows), _ptr(w1, dt, "w1", n1), _ptr(b1, f32, "b1", E * h1),
+        _ptr(w2, dt, "w2", n2), _ptr(b2, f32, "b2", E * params.d), _ptr(counts, torch.int32, "counts", E),
+        _ptr(pre, dt, "pre", npre), _ptr(hidden, dt, "hidden", nhid), _ptr(ye, dt, "ye", rows), _stream(stream)))
+
+
+def moe_experts_bwd_workspace_size(params):
+    n = ctypes.c_size_t(0)
+    _check(load().moe_experts_bwd_workspace_size(ctypes.byref(params), ctypes.byref(n)))
+    return n.value
+
+
+def moe_experts_bwd(params, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace, stream=None):
+    dt, f32 = _dt(params.dtype), torch.float32
+    rows, n1, n2, npre, nhid, h1 = _expert_sizes(params)
+    E = params.E
+    _check(load().moe_experts_bwd(
+        ctypes.byref(params), _ptr(dye, dt, "dye", rows), _ptr(xe, dt, "xe", rows), _ptr(w1, dt, "w1", n1),
+        _ptr(w2, dt, "w2", n2), _ptr(counts, torch.int32, "counts", E), _ptr(pre, dt, "pre", npre),
+        _ptr(hidden, dt, "hidden", nhid), _ptr(dxe, dt, "dxe", rows), _ptr(dw1, dt, "dw1", n1),
+        _ptr(db1, f32, "db1", E * h1), _ptr(dw2, dt, "dw2", n2), _ptr(db2, f32, "db2", E * params.d),
+        _ptr(workspace, None, "workspace"), _bytes(workspace), _stream(stream)))
+
+
+def _weight_shapes(w1, w2, d, gated):
+    """E and h of two expert weights [E, d, h1] and [E, h, d]."""
+    E, h = int(w2.shape[0]), int(w2.shape[1])
+    if tuple(w2.shape) != (E, h, d) or tuple(w1.shape) != (E, d, 2 * h if gated else h):
+        raise ValueError(f"w1 {tuple(w1.shape)} and w2 {tuple(w2.shape)} are no weights of width {d}"
+                         f"{', gated' if gated else ''}: [E, d, {'2 h' if gated else 'h'}] and [E, h, d] expected")
+    return E, h
+
+
+def experts(xe, w1, w2, *, b1=None, b2=None, counts=None, act=MOE_ACT_RELU, gated=False, want_pre=False, stream=None):
+    """Allocate the outputs and run moe_experts; returns a dict with ye, hidden
+    and pre (None unless want_pre; experts_bwd needs it)."""
+    E, C, d = xe.shape
+    if _weight_shapes(w1, w2, d, gated)[0] != E:
+        raise ValueError(f"xe has {E} experts, the weights {w2.shape[0]}")
+    h = int(w2.shape[1])
+    new = dict(dtype=xe.dtype, device=xe.device)
+    out = {
+        "ye": torch.empty((E, C, d), **new),
+        "hidden": torch.empty((E, C, h), **new),
+        "pre": torch.empty((E, C, w1.shape[2]), **new) if want_pre else None,
+    }
+    moe_experts(experts_params(E, C, d, h, act, gated, _dtype_code(xe)), xe, w1, b1, w2, b2, counts, out["pre"],
+                out["hidden"], out["ye"], stream)
+    return out
+
+
+def experts_bwd(dye, xe, w1, w2, pre, hidden, *, counts=None, act=MOE_ACT_RELU, gated=False, want_dxe=True,
+                want_dw=True, want_db=True, stream=None):
+    """Allocating wrapper of moe_experts_bwd; returns a dict with dxe, dw1, db1,
+    dw2 and db2 (None where not wanted)."""
+    E, C, d = dye.shape
+    if _weight_shapes(w1, w2, d, gated)[0] != E:
+        raise ValueError(f"dye has {E} experts, the weights {w2.shape[0]}")
+    h = int(w2.shape[1])
+    params = experts_params(E, C, d, h, act, gated, _dtype_code(dye))
+    f32 = dict(dtype=torch.float32, device=dye.device)
+    out = {
+        "dxe": torch.empty_like(dye) if want_dxe else None,
+        "dw1": torch.empty_like(w1) if want_dw else None,
+        "db1": torch.empty((E, w1.shape[2]), **f32) if want_db else None,
+        "dw2": torch.empty_like(w2) if want_dw else None,
+        "db2": torch.empty((E, d), **f32) if want_db else None,
+    }
+    ws = torch.empty((moe_experts_bwd_workspace_size(params),), dtype=torch.uint8, device=dye.device)
+    moe_experts_bwd(params, dye, xe, w1, w2, counts, pre, hidden, out["dxe"], out["dw1"], out["db1"], out["dw2"],
+                    out["db2"], ws, stream)
+    return out
+
+
+# ---------------------------------------------------------------- the layer for few tokens
+
+def token_layer_params(S, d, E, k, h, kind=MOE_GATE_TOPK, act=MOE_ACT_RELU, gated=False, dtype=MOE_F32, normalize=0,
+                       routed=False, groups=0, hash_seed=0, temperature=0.0, hash_vocab=0):
+    return TokenLayerParams(gate_params(S, d, E, k, 0, kind, normalize, 0, dtype, hash_seed, groups, temperature,
+                                        hash_vocab), h, act, int(bool(gated)), int(bool(routed)))
+
+
+def moe_token_layer_workspace_size(params):
+    n = ctypes.c_size_t(0)
+    _check(load().moe_token_layer_workspace_size(ctypes.byref(params), ctypes.byref(n)))
+    return n.value
+
+
+def moe_token_layer(params, x, wg, bias, token_ids, noise, hash_table, w1, b1, w2, b2, ids, weights, y, workspace,
+                    stream=None):
+    g = params.gate
+    dt, f32, i32 = _dt(g.dtype), torch.float32, torch.int32
+    S, d, E, k, h = g.S, g.d, g.E, g.k, params.h
+    h1 = 2 * h if params.gated else h
+    _check(load().moe_token_layer(
+        ctypes.byref(params), _ptr(x, dt, "x", S * d), _ptr(wg, dt, "wg", d * E), _ptr(bias, f32, "bias", E),
+        _ptr(token_ids, i32, "token_ids", S), _ptr(noise, f32, "noise", S * E),
+        _ptr(hash_table, i32, "hash_table", g.hash_vocab), _ptr(w1, dt, "w1", E * d * h1), _ptr(b1, f32, "b1", E * h1),
+        _ptr(w2, dt, "w2", E * h * d), _ptr(b2, f32, "b2", E * d), _ptr(ids, i32, "ids", S * k),
+        _ptr(weights, f32, "weights", S * k), _ptr(y, dt, "y", S * d), _ptr(workspace, None, "workspace"),
+        _bytes(workspace), _stream(stream)))
+
+
+def token_layer(x, w1, w2, *, b1=None, b2=None, act=MOE_ACT_RELU, gated=False, kind=MOE_GATE_TOPK, k=None, wg=None,
+                bias=None, normalize=0, groups=0, token_ids=None, hash_seed=0, hash_table=None, noise=None,
+                temperature=0.0, ids=None, weights=None, stream=None):
+    """The whole layer on x [S, d], S <= MOE_TOKEN_LAYER_MAX: allocate the outputs
+    and run moe_token_layer.  The gate's arguments are those of `gate`; or pass
+    another gate's ids and weights [S, k].  Returns a dict with y, ids and weights."""
+    S, d = x.shape
+    E, h = _weight_shapes(w1, w2, d, gated)
+    routed = ids is not None or weights is not None
+    if routed:
+        if ids is None or weights is None or tuple(ids.shape) != tuple(weights.shape) or ids.dim() != 2 or ids.shape[0] != S:
+            raise ValueError("ids and weights go together, [S, k] each")
+        k = int(ids.shape[1])
+    else:
+        k = 1 if k is None else k
+        ids = torch.empty((S, k), dtype=torch.int32, device=x.device)
+        weights = torch.empty((S, k), dtype=torch.float32, device=x.device)
+    vocab = 0 if hash_table is None else int(hash_table.shape[0])
+    params = token_layer_params(S, d, E, k, h, kind, act, gated, _dtype_code(x), normalize, routed, groups, hash_seed,
+                                temperature, vocab)
+    y = torch.empty_like(x)
+    ws = torch.empty((moe_token_layer_workspace_size(params),), dtype=torch.uint8, device=x.device)
+    moe_token_layer(params, x, wg, bias, token_ids, noise, hash_table, w1, b1, w2, b2, ids, weights, y, ws, stream)
+    return {"y": y, "ids": ids, "weights": weights}
+
+
+# ---------------------------------------------------------------- gradient norm and clipping
+
+def grad_tensors(grads, out=None):
+    """Descriptors of gradients (and, for clipping, of their outputs; in place by
+    default).  They hold addresses: keep the tensors alive as long as them."""
+    n = len(grads)
+    if out is not None and len(out) != n:
+        raise ValueError(f"{n} gradients, {len(out)} outputs")
+    arr = (GradTensor * n)()
+    for i, g in enumerate(grads):
+        t = arr[i]
+        t.dtype = _dtype_code(g)
+        t.n = g.numel()
+        t.src = t.dst = _ptr(g, None, "gradient")
+        if out is not None:
+            t.dst = _ptr(out[i], g.dtype, "output", t.n)
+    return arr
+
+
+def moe_grad_norm_workspace_size(tensors):
+    n = ctypes.c_size_t(0)
+    _check(load().moe_grad_norm_workspace_size(tensors, len(tensors), ctypes.byref(n)))
+    return n.value
+
+
+def moe_grad_norm(tensors, sumsq, norm, workspace, stream=None):
+    _check(load().moe_grad_norm(tensors, len(tensors), _ptr(sumsq, torch.float64, "sumsq", 1),
+                                _ptr(norm, torch.float32, "norm", 1), _ptr(workspace, None, "workspace"),
+                                _bytes(workspace), _stream(stream)))
+
+
+def moe_grad_clip(tensors, sumsq, max_norm, norm=None, stream=None):
+    _check(load().moe_grad_clip(tensors, len(tensors), _ptr(sumsq, torch.float64, "sumsq", 1), float(max_norm),
+                                _ptr(norm, torch.float32, "norm", 1), _stream(stream)))
+
+
+def grad_norm(grads, stream=None):
+    """2-norm of the gradients taken as one vector: (norm float32 [1], sumsq
+    float64 [1]) on the device.  Ranks that hold different experts add their sumsq and
+    pass it to clip_grads."""
+    arr = grad_tensors(grads)
+    dev = grads[0].device if len(grads) else torch.device("cuda", torch.cuda.current_device())
+    norm = torch.empty((1,), dtype=torch.float32, device=dev)
+    sumsq = torch.empty((1,), dtype=torch.float64, device=dev)
+    ws = torch.empty((moe_grad_norm_workspace_size(arr),), dtype=torch.uint8, device=dev)
+    moe_grad_norm(arr, sumsq, norm, ws, stream)
+    return norm, sumsq
+
+
+def clip_grads(grads, max_norm, out=None, sumsq=None, stream=None):
+    """Scale the gradients to a norm of at most max_norm, in place or into `out`;
+    returns their norm before that (float32 [1], on the device).  `sumsq`: the sum of
+    squares to go by (of all ranks) instead of these gradients' own."""
+    arr = grad_tensors(grads, out)
+    dev = grads[0].device if len(grads) else torch.device("cuda", torch.cuda.current_device())
+    norm = torch.empty((1,), dtype=torch.float32, device=dev)
+    if sumsq is None:
+        sumsq = torch.empty((1,), dtype=torch.float64, device=dev)
+        ws = torch.empty((moe_grad_norm_workspace_size(arr),), dtype=torch.uint8, device=dev)
+        moe_grad_norm(arr, sumsq, None, ws, stream)
+    moe_grad_clip(arr, sumsq, max_norm, norm, stream)
+    return norm

@@ -431,55 +431,12 @@ moe_status scratch_address(const char* who, void** out) {
   return MOE_OK;
 }
 
-// moe_gate and moe_gate_noalloc: with `noalloc` the workspace arguments are
-// ignored and the gate runs in the library's scratch.
-moe_status gate_call(const char* who, bool noalloc, const moe_gate_params* p, const void* x, const void* wg,
-                     const float* bias, const int32_t* token_ids, const float* noise, const int32_t* hash_table,
-                     float* logits, int32_t* ids, int32_t* slots, float* weights, int32_t* counts, int32_t* demand,
-                     int32_t* slot_src, void* workspace, size_t workspace_bytes, hipStream_t stream) {
-  CHECK(check_gate_params(p));
-  const int64_t S = p->S, E = p->E, k = p->k, C = p->capacity;
-  const size_t elt = elt_size(p->dtype);
-  if (p->kind == MOE_GATE_HASH) {
-    CHECK(need(token_ids, S, 4, who, "token_ids"));
-    if (x || wg || bias || logits || noise) return fail(MOE_ERR_INVALID_ARG, "%s: HASH takes no x, wg, bias, logits or noise", who);
-    if (p->hash_vocab > 0) CHECK(need(hash_table, p->hash_vocab, 4, who, "hash_table"));
-    else if (hash_table) return fail(MOE_ERR_INVALID_ARG, "%s: hash_table needs hash_vocab > 0", who);
-  } else {
-    if (hash_table) return fail(MOE_ERR_INVALID_ARG, "%s: hash_table is only for HASH", who);
-    if (noise && p->temperature == 0.f) return fail(MOE_ERR_INVALID_ARG, "%s: noise needs a temperature > 0", who);
-    CHECK(need(noise, 0, 4, who, "noise"));
-    if (p->logits_in) {
-      CHECK(need(logits, S * E, 4, who, "logits"));
-      if (x || wg || bias || token_ids) return fail(MOE_ERR_INVALID_ARG, "%s: with logits_in, x, wg, bias and token_ids must be NULL", who);
-    } else {
-      CHECK(need(x, S * p->d, 16, who, "x"));
-      CHECK(need(wg, static_cast<int64_t>(p->d) * E, elt, who, "wg"));
-      CHECK(need(bias, 0, 4, who, "bias"));
-      CHECK(need(logits, 0, 4, who, "logits"));
-      if (token_ids) return fail(MOE_ERR_INVALID_ARG, "%s: token_ids is only for HASH", who);
-    }
-  }
-  CHECK(need(ids, S * k, 4, who, "ids"));
-  CHECK(need(slots, S * k, 4, who, "slots"));
-  CHECK(need(weights, S * k, 4, who, "weights"));
-  CHECK(need(counts, E, 4, who, "counts"));
-  CHECK(need(demand, 0, 4, who, "demand"));
-  CHECK(need(slot_src, E * C, 4, who, "slot_src"));
-  const size_t ws = gate_workspace_bytes(p);
-  if (noalloc) {
-    if (ws > kGateScratchBytes)
-      return fail(MOE_ERR_UNSUPPORTED, "%s: this gate needs %zu bytes of scratch; the fixed scratch holds %zu "
-                  "(use moe_gate with a workspace)", who, ws, kGateScratchBytes);
-    CHECK(scratch_address(who, &workspace));
-    workspace_bytes = kGateScratchBytes;
-  } else {
-    if (workspace_bytes < ws) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, ws);
-    if (ws > 0 && !workspace) return fail(MOE_ERR_WORKSPACE, "%s: workspace is NULL", who);
-    if (workspace && !aligned(workspace, 16)) return fail(MOE_ERR_WORKSPACE, "%s: workspace is not 16-byte aligned", who);
-  }
-
-  const int nb = static_cast<int>(hist_blocks(S));
+// Logits, selection and weights of checked arguments, and the histogram at the
+// workspace's start (at least gate_workspace_bytes()).
+moe_status gate_select(const moe_gate_params* p, const void* x, const void* wg, const float* bias,
+                       const int32_t* token_ids, const float* noise, const int32_t* hash_table, float* logits,
+                       int32_t* ids, float* weights, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const int nb = static_cast<int>(hist_blocks(p->S));
   int32_t* hist = static_cast<int32_t*>(workspace);
   hipError_t err;
 
@@ -533,11 +490,62 @@ moe_status gate_call(const char* who, bool noalloc, const moe_gate_params* p, co
     err = launch_select_rows(sel, stream);
     if (err != hipSuccess) return hip_fail(err, "moe_gate: selection kernel launch");
   }
+  return MOE_OK;
+}
 
+// moe_gate and moe_gate_noalloc: with `noalloc` the workspace arguments are
+// ignored and the gate runs in the library's scratch.
+moe_status gate_call(const char* who, bool noalloc, const moe_gate_params* p, const void* x, const void* wg,
+                     const float* bias, const int32_t* token_ids, const float* noise, const int32_t* hash_table,
+                     float* logits, int32_t* ids, int32_t* slots, float* weights, int32_t* counts, int32_t* demand,
+                     int32_t* slot_src, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  CHECK(check_gate_params(p));
+  const int64_t S = p->S, E = p->E, k = p->k, C = p->capacity;
+  const size_t elt = elt_size(p->dtype);
+  if (p->kind == MOE_GATE_HASH) {
+    CHECK(need(token_ids, S, 4, who, "token_ids"));
+    if (x || wg || bias || logits || noise) return fail(MOE_ERR_INVALID_ARG, "%s: HASH takes no x, wg, bias, logits or noise", who);
+    if (p->hash_vocab > 0) CHECK(need(hash_table, p->hash_vocab, 4, who, "hash_table"));
+    else if (hash_table) return fail(MOE_ERR_INVALID_ARG, "%s: hash_table needs hash_vocab > 0", who);
+  } else {
+    if (hash_table) return fail(MOE_ERR_INVALID_ARG, "%s: hash_table is only for HASH", who);
+    if (noise && p->temperature == 0.f) return fail(MOE_ERR_INVALID_ARG, "%s: noise needs a temperature > 0", who);
+    CHECK(need(noise, 0, 4, who, "noise"));
+    if (p->logits_in) {
+      CHECK(need(logits, S * E, 4, who, "logits"));
+      if (x || wg || bias || token_ids) return fail(MOE_ERR_INVALID_ARG, "%s: with logits_in, x, wg, bias and token_ids must be NULL", who);
+    } else {
+      CHECK(need(x, S * p->d, 16, who, "x"));
+      CHECK(need(wg, static_cast<int64_t>(p->d) * E, elt, who, "wg"));
+      CHECK(need(bias, 0, 4, who, "bias"));
+      CHECK(need(logits, 0, 4, who, "logits"));
+      if (token_ids) return fail(MOE_ERR_INVALID_ARG, "%s: token_ids is only for HASH", who);
+    }
+  }
+  CHECK(need(ids, S * k, 4, who, "ids"));
+  CHECK(need(slots, S * k, 4, who, "slots"));
+  CHECK(need(weights, S * k, 4, who, "weights"));
+  CHECK(need(counts, E, 4, who, "counts"));
+  CHECK(need(demand, 0, 4, who, "demand"));
+  CHECK(need(slot_src, E * C, 4, who, "slot_src"));
+  const size_t ws = gate_workspace_bytes(p);
+  if (noalloc) {
+    if (ws > kGateScratchBytes)
+      return fail(MOE_ERR_UNSUPPORTED, "%s: this gate needs %zu bytes of scratch; the fixed scratch holds %zu "
+                  "(use moe_gate with a workspace)", who, ws, kGateScratchBytes);
+    CHECK(scratch_address(who, &workspace));
+    workspace_bytes = kGateScratchBytes;
+  } else {
+    if (workspace_bytes < ws) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, workspace_bytes, ws);
+    if (ws > 0 && !workspace) return fail(MOE_ERR_WORKSPACE, "%s: workspace is NULL", who);
+    if (workspace && !aligned(workspace, 16)) return fail(MOE_ERR_WORKSPACE, "%s: workspace is not 16-byte aligned", who);
+  }
+
+  CHECK(gate_select(p, x, wg, bias, token_ids, noise, hash_table, logits, ids, weights, workspace, workspace_bytes, stream));
   AssignArgs aa{};
-  aa.S = p->S; aa.E = p->E; aa.k = p->k; aa.nb = nb; aa.C = p->capacity;
-  aa.ids = ids; aa.hist = hist; aa.counts = counts; aa.demand = demand; aa.slots = slots; aa.slot_src = slot_src;
-  err = launch_assign(aa, stream);
+  aa.S = p->S; aa.E = p->E; aa.k = p->k; aa.nb = static_cast<int>(hist_blocks(S)); aa.C = p->capacity;
+  aa.ids = ids; aa.hist = static_cast<int32_t*>(workspace); aa.counts = counts; aa.demand = demand; aa.slots = slots; aa.slot_src = slot_src;
+  const hipError_t err = launch_assign(aa, stream);
   if (err != hipSuccess) return hip_fail(err, "moe_gate: assign kernel launch");
   return ok();
 }
@@ -787,6 +795,373 @@ moe_status moe_base_gate_async(const moe_base_params* p, const void* x, const vo
   if (!aligned(status, 8)) return fail(MOE_ERR_INVALID_ARG, "%s: status is not 8-byte aligned", who);
   return base_gate_run(who, p, x, wg, bias, logits, ids, slots, weights, counts, slot_src, prices, workspace,
                        workspace_bytes, nullptr, launch_rounds, status, stream);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- expert networks
+namespace {
+
+constexpr int32_t kMaxWidth = 1 << 20;  // d and h: tile offsets stay below 2^31 bytes
+
+moe_status check_act(const char* who, int32_t act, int32_t gated) {
+  if (act < MOE_ACT_RELU || act > MOE_ACT_SILU) return fail(MOE_ERR_INVALID_ARG, "%s: activation %d unknown", who, act);
+  if (gated != 0 && gated != 1) return fail(MOE_ERR_INVALID_ARG, "%s: gated must be 0 or 1", who);
+  return MOE_OK;
+}
+
+// Row lengths of the expert networks.
+moe_status check_widths(const char* who, int32_t d, int32_t h, int32_t dtype) {
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: dtype %d unknown", who, dtype);
+  if (d < 1 || h < 1) return fail(MOE_ERR_INVALID_ARG, "%s: need d >= 1 and h >= 1, got %d and %d", who, d, h);
+  const int64_t elt = static_cast<int64_t>(elt_size(dtype));
+  if (d * elt % 16 != 0 || h * elt % 16 != 0)
+    return fail(MOE_ERR_UNSUPPORTED, "%s: rows of d = %d and h = %d elements are no multiples of 16 bytes", who, d, h);
+  if (d > kMaxWidth || h > kMaxWidth)
+    return fail(MOE_ERR_UNSUPPORTED, "%s: d = %d or h = %d beyond %d", who, d, h, kMaxWidth);
+  return MOE_OK;
+}
+
+moe_status check_experts(const moe_experts_params* p, const char* who) {
+  if (!p) return fail(MOE_ERR_INVALID_ARG, "%s: params is NULL", who);
+  if (p->E < 1 || p->E > 1024) return fail(MOE_ERR_INVALID_ARG, "%s: E = %d outside [1, 1024]", who, p->E);
+  if (p->capacity < 0) return fail(MOE_ERR_INVALID_ARG, "%s: capacity = %d < 0", who, p->capacity);
+  if (static_cast<int64_t>(p->E) * p->capacity > kI32Max) return fail(MOE_ERR_INVALID_ARG, "%s: E * capacity >= 2^31", who);
+  CHECK(check_act(who, p->act, p->gated));
+  CHECK(check_widths(who, p->d, p->h, p->dtype));
+  // blocks of the smallest tiles (64 x 64) of every product, in one grid dimension
+  const int64_t t = 64, h1 = static_cast<int64_t>(p->h) * (p->gated ? 2 : 1);
+  const int64_t tc = (p->capacity + t - 1) / t, td = (p->d + t - 1) / t, th = (h1 + t - 1) / t;
+  if (std::max({tc * td, tc * th, td * th}) > (int64_t(1) << 30) / p->E)
+    return fail(MOE_ERR_UNSUPPORTED, "%s: more than 2^30 tiles", who);
+  return MOE_OK;
+}
+
+ExpertArgs expert_args(const moe_experts_params* p) {
+  ExpertArgs a{};
+  a.E = p->E; a.C = p->capacity; a.d = p->d; a.h = p->h; a.act = p->act; a.gated = p->gated; a.dtype = p->dtype;
+  return a;
+}
+
+// Workspace of moe_experts_bwd, each piece 256-byte aligned: dpre [E, C, h1] and the
+// partial column sums of dpre and of dye.
+struct ExpertsBwdPlan {
+  size_t off_dpre, off_col, off_row, total;
+};
+ExpertsBwdPlan plan_experts_bwd(const moe_experts_params* p) {
+  const ExpertArgs a = expert_args(p);
+  const size_t E = static_cast<size_t>(p->E), h1 = static_cast<size_t>(p->h) * (p->gated ? 2 : 1);
+  ExpertsBwdPlan w{};
+  w.off_dpre = 0;
+  w.off_col = align256(E * static_cast<size_t>(p->capacity) * h1 * elt_size(p->dtype));
+  w.off_row = w.off_col + align256(E * static_cast<size_t>(expert_parts(a)) * h1 * 4);
+  w.total = w.off_row + align256(E * static_cast<size_t>(expert_row_parts(a)) * static_cast<size_t>(p->d) * 4);
+  return w;
+}
+
+moe_status check_workspace(const char* who, const void* workspace, size_t bytes, size_t want) {
+  if (bytes < want) return fail(MOE_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, bytes, want);
+  if (want > 0 && !workspace) return fail(MOE_ERR_WORKSPACE, "%s: workspace is NULL", who);
+  if (workspace && !aligned(workspace, 16)) return fail(MOE_ERR_WORKSPACE, "%s: workspace is not 16-byte aligned", who);
+  return MOE_OK;
+}
+
+// ---------------------------------------------------------------- the layer for few tokens
+moe_status check_token_layer(const moe_token_layer_params* p, const char* who) {
+  if (!p) return fail(MOE_ERR_INVALID_ARG, "%s: params is NULL", who);
+  const moe_gate_params& g = p->gate;
+  if (p->routed != 0 && p->routed != 1) return fail(MOE_ERR_INVALID_ARG, "%s: routed must be 0 or 1", who);
+  if (g.capacity != 0) return fail(MOE_ERR_INVALID_ARG, "%s: the layer has no slots; capacity must be 0", who);
+  if (g.logits_in != 0) return fail(MOE_ERR_INVALID_ARG, "%s: takes no logits; pass a gate's ids and weights with routed", who);
+  if (p->routed) {
+    if (g.S < 0 || g.E < 1 || g.E > 1024 || g.k < 1 || g.k > 8)
+      return fail(MOE_ERR_INVALID_ARG, "%s: need S >= 0, 1 <= E <= 1024, 1 <= k <= 8 (got S=%d E=%d k=%d)", who, g.S, g.E, g.k);
+  } else {
+    CHECK(check_gate_params(&g));
+  }
+  CHECK(check_act(who, p->act, p->gated));
+  CHECK(check_widths(who, g.d, p->h, g.dtype));
+  if (g.S > MOE_TOKEN_LAYER_MAX)
+    return fail(MOE_ERR_UNSUPPORTED, "%s: %d tokens, at most %d are served", who, g.S, MOE_TOKEN_LAYER_MAX);
+  // 32-bit offsets into one expert's matrices and into the rows
+  const int64_t most = kI32Max - 65536, elt = static_cast<int64_t>(elt_size(g.dtype));
+  const int64_t h1 = static_cast<int64_t>(p->h) * (p->gated ? 2 : 1);
+  if (g.d * h1 * elt > most || static_cast<int64_t>(g.S) * g.k * p->h * elt > most)
+    return fail(MOE_ERR_UNSUPPORTED, "%s: an expert's matrix or the hidden rows exceed 2^31 bytes", who);
+  return MOE_OK;
+}
+
+struct TokenLayerPlan {
+  LayerArgs a;
+  size_t gate, off_hidden, off_part, total;
+};
+TokenLayerPlan plan_token_layer(const moe_token_layer_params* p) {
+  const moe_gate_params& g = p->gate;
+  TokenLayerPlan w{};
+  LayerArgs& a = w.a;
+  a.S = g.S; a.d = g.d; a.E = g.E; a.k = g.k; a.h = p->h; a.act = p->act; a.gated = p->gated; a.dtype = g.dtype;
+  a.by_choice = static_cast<int64_t>(g.S) * g.k <= g.E ? 1 : 0;
+  a.z2 = layer_splits(a);
+  const size_t choices = static_cast<size_t>(g.S) * static_cast<size_t>(g.k);
+  w.gate = p->routed ? 0 : std::max(gate_workspace_bytes(&g), gate_split_bytes(&g));
+  w.off_hidden = align256(w.gate);
+  w.off_part = w.off_hidden + align256(choices * static_cast<size_t>(p->h) * elt_size(g.dtype));
+  w.total = w.off_part + align256(static_cast<size_t>(a.z2) * choices * static_cast<size_t>(g.d) * 4);
+  return w;
+}
+
+// ---------------------------------------------------------------- gradient norm
+static_assert(kLayerMaxTokens == MOE_TOKEN_LAYER_MAX, "tokens of the layer");
+
+int64_t grad_chunks(int64_t n) { return (n + kGradChunk - 1) / kGradChunk; }
+
+moe_status check_grads(const moe_grad_tensor* t, int32_t count, bool scale, const char* who) {
+  if (count < 0) return fail(MOE_ERR_INVALID_ARG, "%s: count = %d < 0", who, count);
+  if (count > 0 && !t) return fail(MOE_ERR_INVALID_ARG, "%s: tensors is NULL", who);
+  int64_t chunks = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    if (t[i].dtype != MOE_F32 && t[i].dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: dtype %d unknown", who, i, t[i].dtype);
+    if (t[i].n < 0) return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d: n < 0", who, i);
+    const size_t elt = elt_size(t[i].dtype);
+    CHECK(need(t[i].src, t[i].n, elt, who, "src"));
+    if (scale) CHECK(need(t[i].dst, t[i].n, elt, who, "dst"));
+    if (t[i].n > (int64_t(1) << 44)) return fail(MOE_ERR_UNSUPPORTED, "%s: tensor %d: more than 2^44 elements", who, i);
+    chunks += grad_chunks(t[i].n);
+    if (chunks > kI32Max) return fail(MOE_ERR_UNSUPPORTED, "%s: more than 2^31 chunks of %d elements", who, kGradChunk);
+  }
+  return MOE_OK;
+}
+
+// What the tensors write may overlap neither each other's output nor another
+// one's input.
+moe_status check_grad_overlap(const moe_grad_tensor* t, int32_t count, const char* who) {
+  struct Range {
+    uintptr_t lo, hi;
+    int32_t i;
+    bool out;
+  };
+  std::vector<Range> r;
+  try {
+    r.reserve(2 * static_cast<size_t>(count));
+    for (int32_t i = 0; i < count; ++i) {
+      if (t[i].n == 0) continue;
+      const size_t bytes = static_cast<size_t>(t[i].n) * elt_size(t[i].dtype);
+      const uintptr_t s = reinterpret_cast<uintptr_t>(t[i].src), d = reinterpret_cast<uintptr_t>(t[i].dst);
+      r.push_back({d, d + bytes, i, true});
+      if (s != d) r.push_back({s, s + bytes, i, false});
+    }
+    std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.lo < b.lo; });
+  } catch (...) {
+    return fail(MOE_ERR_UNSUPPORTED, "%s: out of host memory", who);
+  }
+  // furthest end so far of the outputs and of the inputs that start no later
+  uintptr_t end_out = 0, end_in = 0;
+  for (const Range& x : r) {
+    if (x.lo < end_out || (x.out && x.lo < end_in))
+      return fail(MOE_ERR_INVALID_ARG, "%s: tensor %d overlaps an output (pass each tensor once)", who, x.i);
+    (x.out ? end_out : end_in) = std::max(x.out ? end_out : end_in, x.hi);
+  }
+  return MOE_OK;
+}
+
+// Calls fn(list) for the tensors in lists of at most kGradListMax.
+template <class Fn>
+hipError_t by_grad_list(const moe_grad_tensor* t, int32_t count, Fn fn) {
+  GradList l{};
+  for (int32_t i = 0; i <= count; ++i) {
+    if (l.n > 0 && (i == count || l.n == kGradListMax)) {
+      const hipError_t err = fn(l);
+      if (err != hipSuccess) return err;
+      l.n = l.chunks = 0;
+    }
+    if (i == count || t[i].n == 0) continue;
+    GradTensor& g = l.t[l.n++];
+    g.src = t[i].src; g.dst = t[i].dst; g.n = t[i].n; g.first = l.chunks;
+    g.dtype = static_cast<int8_t>(t[i].dtype);
+    g.vec_src = aligned(t[i].src, 16);
+    g.vec_both = g.vec_src && aligned(t[i].dst, 16);
+    l.chunks += static_cast<int>(grad_chunks(t[i].n));
+  }
+  return hipSuccess;
+}
+
+// Partial sums: one per block of each list.
+size_t grad_parts(const moe_grad_tensor* t, int32_t count) {
+  size_t n = 0;
+  (void)by_grad_list(t, count, [&](const GradList& l) {
+    n += static_cast<size_t>(grad_blocks(l.chunks));
+    return hipSuccess;
+  });
+  return n;
+}
+
+}  // namespace
+
+extern "C" {
+
+moe_status moe_experts(const moe_experts_params* p, const void* xe, const void* w1, const float* b1, const void* w2,
+                       const float* b2, const int32_t* counts, void* pre, void* hidden, void* ye, hipStream_t stream) {
+  static const char* who = "moe_experts";
+  CHECK(check_experts(p, who));
+  const int64_t rows = static_cast<int64_t>(p->E) * p->capacity;
+  if (rows > 0) {
+    CHECK(need(w1, 1, 16, who, "w1"));
+    CHECK(need(w2, 1, 16, who, "w2"));
+  }
+  CHECK(need(xe, rows, 16, who, "xe"));
+  CHECK(need(hidden, rows, 16, who, "hidden"));
+  CHECK(need(ye, rows, 16, who, "ye"));
+  CHECK(need(pre, 0, 16, who, "pre"));
+  CHECK(need(b1, 0, 4, who, "b1"));
+  CHECK(need(b2, 0, 4, who, "b2"));
+  CHECK(need(counts, 0, 4, who, "counts"));
+  if (rows == 0) return ok();
+  ExpertArgs a = expert_args(p);
+  a.counts = counts; a.xe = xe; a.w1 = w1; a.w2 = w2; a.b1 = b1; a.b2 = b2; a.pre = pre; a.hidden = hidden; a.ye = ye;
+  const hipError_t err = launch_experts(a, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_experts: kernel launch");
+  return ok();
+}
+
+moe_status moe_experts_bwd_workspace_size(const moe_experts_params* p, size_t* bytes) {
+  static const char* who = "moe_experts_bwd_workspace_size";
+  if (!bytes) return fail(MOE_ERR_INVALID_ARG, "bytes is NULL");
+  CHECK(check_experts(p, who));
+  *bytes = plan_experts_bwd(p).total;
+  return ok();
+}
+
+moe_status moe_experts_bwd(const moe_experts_params* p, const void* dye, const void* xe, const void* w1, const void* w2,
+                           const int32_t* counts, const void* pre, const void* hidden, void* dxe, void* dw1,
+                           float* db1, void* dw2, float* db2, void* workspace, size_t workspace_bytes,
+                           hipStream_t stream) {
+  static const char* who = "moe_experts_bwd";
+  CHECK(check_experts(p, who));
+  const int64_t rows = static_cast<int64_t>(p->E) * p->capacity;
+  const bool back = dxe || dw1 || db1;  // through the activation
+  CHECK(need(dye, rows, 16, who, "dye"));
+  CHECK(need(xe, dw1 ? rows : 0, 16, who, "xe"));
+  CHECK(need(w1, dxe ? rows : 0, 16, who, "w1"));
+  CHECK(need(w2, back ? rows : 0, 16, who, "w2"));
+  CHECK(need(pre, back ? rows : 0, 16, who, "pre"));
+  CHECK(need(hidden, dw2 ? rows : 0, 16, who, "hidden"));
+  CHECK(need(counts, 0, 4, who, "counts"));
+  CHECK(need(dxe, 0, 16, who, "dxe"));
+  CHECK(need(dw1, 0, 16, who, "dw1"));
+  CHECK(need(dw2, 0, 16, who, "dw2"));
+  CHECK(need(db1, 0, 4, who, "db1"));
+  CHECK(need(db2, 0, 4, who, "db2"));
+  const ExpertsBwdPlan w = plan_experts_bwd(p);
+  CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
+  char* ws = static_cast<char*>(workspace);
+  ExpertArgs a = expert_args(p);
+  a.counts = counts; a.dye = dye; a.xe = xe; a.w1 = w1; a.w2 = w2;
+  a.pre = const_cast<void*>(pre); a.hidden = const_cast<void*>(hidden);
+  a.dpre = ws + w.off_dpre;
+  a.colsum = reinterpret_cast<float*>(ws + w.off_col);
+  a.rowsum = reinterpret_cast<float*>(ws + w.off_row);
+  a.dxe = dxe; a.dw1 = dw1; a.db1 = db1; a.dw2 = dw2; a.db2 = db2;
+  const hipError_t err = launch_experts_bwd(a, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_experts_bwd: kernel launch");
+  return ok();
+}
+
+moe_status moe_token_layer_workspace_size(const moe_token_layer_params* p, size_t* bytes) {
+  static const char* who = "moe_token_layer_workspace_size";
+  if (!bytes) return fail(MOE_ERR_INVALID_ARG, "bytes is NULL");
+  CHECK(check_token_layer(p, who));
+  *bytes = plan_token_layer(p).total;
+  return ok();
+}
+
+moe_status moe_token_layer(const moe_token_layer_params* p, const void* x, const void* wg, const float* bias,
+                           const int32_t* token_ids, const float* noise, const int32_t* hash_table, const void* w1,
+                           const float* b1, const void* w2, const float* b2, int32_t* ids, float* weights, void* y,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  static const char* who = "moe_token_layer";
+  CHECK(check_token_layer(p, who));
+  const moe_gate_params& g = p->gate;
+  const int64_t S = g.S, E = g.E;
+  CHECK(need(x, S, 16, who, "x"));
+  CHECK(need(w1, S, 16, who, "w1"));
+  CHECK(need(w2, S, 16, who, "w2"));
+  CHECK(need(b1, 0, 4, who, "b1"));
+  CHECK(need(b2, 0, 4, who, "b2"));
+  CHECK(need(ids, S, 4, who, "ids"));
+  CHECK(need(weights, S, 4, who, "weights"));
+  CHECK(need(y, S, 16, who, "y"));
+  const bool hash = !p->routed && g.kind == MOE_GATE_HASH, learned = !p->routed && !hash;
+  if (learned) CHECK(need(wg, static_cast<int64_t>(g.d) * E, elt_size(g.dtype), who, "wg"));
+  else if (wg || bias || noise) return fail(MOE_ERR_INVALID_ARG, "%s: wg, bias and noise are for a learned gate", who);
+  CHECK(need(bias, 0, 4, who, "bias"));
+  if (noise && g.temperature == 0.f) return fail(MOE_ERR_INVALID_ARG, "%s: noise needs a temperature > 0", who);
+  CHECK(need(noise, 0, 4, who, "noise"));
+  if (hash) {
+    CHECK(need(token_ids, S, 4, who, "token_ids"));
+    if (g.hash_vocab > 0) CHECK(need(hash_table, g.hash_vocab, 4, who, "hash_table"));
+    else if (hash_table) return fail(MOE_ERR_INVALID_ARG, "%s: hash_table needs hash_vocab > 0", who);
+  } else if (token_ids || hash_table) {
+    return fail(MOE_ERR_INVALID_ARG, "%s: token_ids and hash_table are only for HASH", who);
+  }
+  TokenLayerPlan w = plan_token_layer(p);
+  CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
+  if (S == 0) return ok();
+  char* ws = static_cast<char*>(workspace);
+  if (!p->routed)
+    CHECK(gate_select(&g, hash ? nullptr : x, wg, bias, token_ids, noise, hash_table, nullptr, ids, weights, ws, w.gate, stream));
+  LayerArgs& a = w.a;
+  a.x = x; a.w1 = w1; a.w2 = w2; a.b1 = b1; a.b2 = b2; a.ids = ids; a.weights = weights; a.y = y;
+  a.hidden = ws + w.off_hidden;
+  a.part = reinterpret_cast<float*>(ws + w.off_part);
+  const hipError_t err = launch_layer(a, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_token_layer: kernel launch");
+  return ok();
+}
+
+moe_status moe_grad_norm_workspace_size(const moe_grad_tensor* tensors, int32_t count, size_t* bytes) {
+  if (!bytes) return fail(MOE_ERR_INVALID_ARG, "bytes is NULL");
+  CHECK(check_grads(tensors, count, false, "moe_grad_norm_workspace_size"));
+  *bytes = grad_parts(tensors, count) * sizeof(double);
+  return ok();
+}
+
+moe_status moe_grad_norm(const moe_grad_tensor* tensors, int32_t count, double* sumsq, float* norm, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+  static const char* who = "moe_grad_norm";
+  CHECK(check_grads(tensors, count, false, who));
+  CHECK(need(sumsq, 0, 8, who, "sumsq"));
+  CHECK(need(norm, 0, 4, who, "norm"));
+  const size_t n = grad_parts(tensors, count);
+  CHECK(check_workspace(who, workspace, workspace_bytes, n * sizeof(double)));
+  double* part = static_cast<double*>(workspace);
+  size_t at = 0;
+  hipError_t err = by_grad_list(tensors, count, [&](const GradList& l) {
+    const hipError_t e = launch_grad_squares(l, part + at, stream);
+    at += static_cast<size_t>(grad_blocks(l.chunks));
+    return e;
+  });
+  if (err == hipSuccess) err = launch_grad_finish(part, static_cast<int>(n), sumsq, norm, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_grad_norm: kernel launch");
+  return ok();
+}
+
+moe_status moe_grad_clip(const moe_grad_tensor* tensors, int32_t count, const double* sumsq, float max_norm,
+                         float* norm, hipStream_t stream) {
+  static const char* who = "moe_grad_clip";
+  CHECK(check_grads(tensors, count, true, who));
+  if (!std::isfinite(max_norm) || max_norm < 0.f) return fail(MOE_ERR_INVALID_ARG, "%s: max_norm must be finite and >= 0", who);
+  CHECK(need(sumsq, 1, 8, who, "sumsq"));
+  CHECK(need(norm, 0, 4, who, "norm"));
+  CHECK(check_grad_overlap(tensors, count, who));
+  bool first = true;
+  hipError_t err = by_grad_list(tensors, count, [&](const GradList& l) {
+    const hipError_t e = launch_grad_scale(l, sumsq, max_norm, first ? norm : nullptr, stream);
+    first = false;
+    return e;
+  });
+  if (err == hipSuccess && first && norm) err = launch_grad_scale(GradList{}, sumsq, max_norm, norm, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_grad_clip: kernel launch");
+  return ok();
 }
 
 }  // extern "C"

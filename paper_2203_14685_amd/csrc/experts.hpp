@@ -1,0 +1,210 @@
+// Expert networks (step 4 of Algorithm 1): argument blocks, activations and the
+// pieces that the tiled products of both element types share.
+//
+//   pre = xe w1 + b1,  hidden = act(pre)  or, gated, act(pre[:, :h]) * pre[:, h:],
+//   ye = hidden w2 + b2
+// and its gradients are six batched products D[m, n] = sum_k A(m, k) B(n, k), one
+// matrix pair per expert, whose operands lie in memory in one of two ways:
+//   kRows   row m holds its K elements next to each other (xe, hidden, dye, dpre as
+//           left operands; both weights in the products with a transposed weight)
+//   kCols   row k holds the elements of all m (both weights in the forward products;
+//           both operands of the weight gradients, where K is the expert's rows)
+#pragma once
+
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace hetumoe {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+typedef __attribute__((address_space(3))) void lds_void;
+
+constexpr int kRows = 0, kCols = 1;
+constexpr int kExpertOob = 0x7ffffff0;  // offset past every buffer resource: loads return zeros
+
+// What becomes of the product.
+constexpr int kEpiStore = 0;    // + bias, rounded once
+constexpr int kEpiAct = 1;      // + bias: pre (optional); hidden
+constexpr int kEpiActGrad = 2;  // dhidden: times the activation's gradient -> dpre; column sums of it
+
+// gfx950's LDS transpose read (ds_read_b64_tr_b16): within each group of 16
+// lanes, lane i receives element i % 4 of the four-element pieces addressed by
+// lanes i / 4 + 4 j, j = 0..3.
+__device__ __forceinline__ uint2 expert_tr16(const bf16_t* p) {
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
+}
+
+// Loads straight into LDS: lane l's 16 bytes at `off` go to dst + 16 l; offsets
+// past the resource bring zeros.
+__device__ __forceinline__ void expert_dma(__amdgpu_buffer_rsrc_t r, void* dst, int off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void*)(dst), 16, off, 0, 0, 0);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t expert_rsrc(const void* p, int bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+
+// Every load of this wave has arrived in LDS and every LDS read has returned;
+// after the barrier that holds for the whole block.
+__device__ __forceinline__ void expert_stage_barrier() {
+  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// ---------------------------------------------------------------- operands
+// K elements per stage: 128 bytes of a row that runs along K.
+template <class T> constexpr int kExpertBk = 128 / static_cast<int>(sizeof(T));
+// Elements of a 16-byte piece.
+template <class T> constexpr int kExpertPe = 16 / static_cast<int>(sizeof(T));
+
+// Which 16-byte piece of its row lies at place `c` of LDS row `row`.
+//   kRows: 8 pieces per 128-byte row; two rows fill the 64 banks.  A fragment read takes
+//          rows r .. r + 15 (left operand) or, of the right one, 8 i + 4 t + 0..3, i = 0..3
+//          (bf16) or 4 i + t, i = 0..15 (fp32).
+//   kCols: bf16: a transpose read takes k rows 8 g + 4 h + 0..3, of each 32 contiguous bytes
+//          (left) or four 8-byte halves of neighbouring pieces (right); fp32 reads run along
+//          a row and need no other order.
+template <class T, int KIND, bool RIGHT, int W>
+__device__ __forceinline__ int expert_swz(int row) {
+  if constexpr (KIND == kRows) {
+    if constexpr (!RIGHT) return (row >> 1) & 7;
+    else if constexpr (sizeof(T) == 2) return ((row >> 1) & 1) | ((row >> 2) & 6);
+    else return (row >> 2) & 7;
+  } else if constexpr (sizeof(T) == 4) {
+    return 0;
+  } else if constexpr (W >= 128) {
+    if constexpr (RIGHT) return (row & 3) << 2;
+    else return ((row & 3) << 1) | (row & 8);
+  } else {
+    if constexpr (RIGHT) return ((row >> 1) & 1) << 2;
+    else return (((row >> 1) & 1) << 1) | ((row & 8) >> 1);
+  }
+}
+
+// One operand's loads: W rows (kRows) or columns (kCols) of the tile.
+template <class T, int KIND, bool RIGHT, int W, int WAVES>
+struct ExpertOperand {
+  static constexpr int kBk = kExpertBk<T>, kPe = kExpertPe<T>, kElt = static_cast<int>(sizeof(T));
+  static constexpr int kBytes = W * 128;
+  static constexpr int N = kBytes / 1024 / WAVES;  // loads per wave and stage
+  static_assert(N * WAVES * 1024 == kBytes, "whole loads");
+  const char* base;   // (first row or column, k = 0)
+  int64_t step;       // bytes per stage
+  int64_t limit;      // bytes behind base that may be read, less what the stages took
+  int cap;            // most that a stage's resource needs
+  int off[N];
+  int kc;             // kRows: the lane's K element in a stage
+
+  // map(piece) gives the column of the tile's piece, or -1 behind the matrix.
+  template <class Map>
+  __device__ __forceinline__ void init(const T* p, int ld, int first, int valid, int K, int wave, Map map) {
+    const int lane = lane_id();
+    if constexpr (KIND == kRows) {
+      base = reinterpret_cast<const char*>(p + static_cast<int64_t>(first) * ld);
+      step = 128;
+      limit = static_cast<int64_t>(valid) * ld * kElt;
+      cap = 0x7fffff00;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = (i * WAVES + wave) * 8 + lane / 8;
+        const int piece = (lane % 8) ^ expert_swz<T, KIND, RIGHT, W>(row);
+        if (i == 0) kc = piece * kPe;  // the same for every i: rows differ by multiples of 32
+        off[i] = row < valid ? row * ld * kElt + piece * 16 : kExpertOob;
+      }
+    } else {
+      constexpr int P = W / kPe;   // pieces per row
+      constexpr int R = 64 / P;  // rows per load
+      base = reinterpret_cast<const char*>(p);
+      step = static_cast<int64_t>(kBk) * ld * kElt;
+      limit = static_cast<int64_t>(K) * ld * kElt;
+      cap = kBk * ld * kElt;
+      kc = 0;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = (i * WAVES + wave) * R + lane / P;
+        const int col = map((lane % P) ^ expert_swz<T, KIND, RIGHT, W>(row));
+        off[i] = col >= 0 ? (row * ld + col) * kElt : kExpertOob;
+      }
+    }
+  }
+  // The stage `base` points at; `left` K elements remain.
+  __device__ __forceinline__ void load(T* lds, int wave, int left) {
+    const __amdgpu_buffer_rsrc_t r = expert_rsrc(base, static_cast<int>(min(limit, static_cast<int64_t>(cap))));
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      int o = off[i];
+      if constexpr (KIND == kRows) o = kc < left ? o : kExpertOob;
+      expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, o);
+    }
+    base += step;
+    limit -= step;
+  }
+};
+
+// ---------------------------------------------------------------- activations
+// sigmoid by the hardware exponential and reciprocal: both within about one
+// unit of the last place of fp32 for the arguments that matter.
+__device__ __forceinline__ float expert_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
+
+constexpr float kGeluA = 0.7978845608028654f;  // sqrt(2 / pi)
+constexpr float kGeluB = 0.044715f;
+
+// 0.5 (1 + tanh u) = sigmoid(2 u)
+template <int ACT>
+__device__ __forceinline__ float expert_act(float a) {
+  if constexpr (ACT == 0) return a < 0.f ? 0.f : a;  // a NaN stays one
+  else if constexpr (ACT == 2) return a * expert_sigmoid(a);
+  else return a * expert_sigmoid(2.f * kGeluA * (a + kGeluB * a * a * a));
+}
+
+// The activation and its derivative.
+template <int ACT>
+__device__ __forceinline__ void expert_act_grad(float a, float& f, float& df) {
+  if constexpr (ACT == 0) {
+    f = a < 0.f ? 0.f : a;
+    df = a > 0.f ? 1.f : 0.f;
+  } else if constexpr (ACT == 2) {
+    const float p = expert_sigmoid(a);
+    f = a * p;
+    df = p + f * (1.f - p);
+  } else {
+    const float p = expert_sigmoid(2.f * kGeluA * (a + kGeluB * a * a * a));
+    f = a * p;
+    df = p + f * (1.f - p) * (2.f * kGeluA) * (1.f + 3.f * kGeluB * a * a);
+  }
+}
+
+// fn(ExpertInt<ACT>()) for a run-time activation.
+template <int V> struct ExpertInt { static constexpr int v = V; };
+template <class Fn>
+__device__ __forceinline__ void expert_by_act(int act, Fn fn) {
+  if (act == 0) fn(ExpertInt<0>());
+  else if (act == 2) fn(ExpertInt<2>());
+  else fn(ExpertInt<1>());
+}
+
+// Rows in use of expert e.
+__device__ __forceinline__ int expert_count(const int32_t* counts, int e, int C) {
+  return counts ? max(0, min(counts[e], C)) : C;
+}
+
+// Block -> (expert, m tile, n tile).  Blocks go round the 8 XCDs in turn; each XCD
+// takes one contiguous piece of the tiles, an expert's tiles together, so that
+// its own L2 serves an expert's rows and weights to the tiles that share them.
+__device__ __forceinline__ bool expert_tile(int tiles, int tm, int tn, int& e, int& bm, int& bn) {
+  const int per = (tiles + 7) / 8;
+  const int t = static_cast<int>(blockIdx.x % 8) * per + static_cast<int>(blockIdx.x / 8);
+  if (static_cast<int>(blockIdx.x / 8) >= per || t >= tiles) return false;
+  e = t / (tm * tn);
+  const int r = t - e * tm * tn;
+  bn = r / tm;
+  bm = r - bn * tm;
+  return true;
+}
+
+}  // namespace hetumoe

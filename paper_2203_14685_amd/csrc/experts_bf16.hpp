@@ -1,0 +1,250 @@
+// Batched bf16 products of the expert networks on v_mfma_f32_16x16x32_bf16.
+//
+// A block forms BM x BN of one expert's product, WM x WN waves, 64 columns each.
+// Per stage of 64 K elements both operands go straight from memory to LDS as
+// they lie there (16 bytes per lane, no registers), two stages in turn: the next
+// one is on its way while this one is multiplied, one barrier per stage.  Operands
+// whose rows run along K are read as 16-byte fragments, the others through LDS
+// transpose reads.  16-byte pieces are placed by an exclusive-or with bits of
+// their row, so that the 16 lanes of a fragment read touch different banks; since
+// a load to LDS fills it in lane order, the lane fetches the piece that belongs
+// where it writes.
+//
+// The product is formed transposed (columns n are the rows of the matrix unit),
+// and the 16 x 16 tiles come in pairs whose rows interleave by fours: a lane then
+// holds 8 neighbouring columns of one row, one 16-byte store.
+//
+// Rows past the expert's count and pieces past K are zeros from outside the buffer
+// resource; nothing behind the count is read.
+#pragma once
+
+#include "experts.hpp"
+
+namespace hetumoe {
+
+constexpr int kEBK = kExpertBk<bf16_t>;
+
+// Fragment of K step ks (32 elements): lane (g, m) gets K 8 g .. 8 g + 7 of
+// left: row (or column) x0 + m;  right: x0 + 8 (m / 4) + 4 t + m % 4, tile t of a pair.
+template <int KIND, bool RIGHT, int W>
+__device__ __forceinline__ u32x4 expert_frag(const bf16_t* lds, int x0, int t, int ks, int g, int m) {
+  if constexpr (KIND == kRows) {
+    const int row = x0 + (RIGHT ? 8 * (m / 4) + 4 * t + m % 4 : m);
+    const int piece = (4 * ks + g) ^ expert_swz<bf16_t, KIND, RIGHT, W>(row);
+    return *reinterpret_cast<const u32x4*>(lds + row * kEBK + piece * 8);
+  } else {
+    uint2 half[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int row = 32 * ks + 8 * g + 4 * h + m / 4;
+      const int col = x0 + (RIGHT ? 8 * (m % 4) + 4 * t : 4 * (m % 4));
+      half[h] = expert_tr16(lds + row * W + (((col / 8) ^ expert_swz<bf16_t, KIND, RIGHT, W>(row)) * 8) + col % 8);
+    }
+    return u32x4{half[0].x, half[0].y, half[1].x, half[1].y};
+  }
+}
+
+template <int BM, int BN, int WM, int WN, int KA, int KB, int EPI, bool GATED>
+__global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGemmArgs a) {
+  constexpr int WAVES = WM * WN;
+  constexpr int MT = BM / WM / 16, NT = BN / WN / 16, NP = NT / 2;
+  static_assert(NT == 4, "64 columns per wave");
+  // columns of the output per block and wave: with GATED in the forward product half of
+  // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
+  constexpr bool kSplit = EPI == kEpiAct && GATED;
+  constexpr int BNO = kSplit ? BN / 2 : BN;
+  __shared__ __align__(1024) bf16_t A0[BM * kEBK], B0[BN * kEBK], A1[BM * kEBK], B1[BN * kEBK];
+
+  int e, bm, bn;
+  if (!expert_tile(a.tiles, a.tm, a.tn, e, bm, bn)) return;
+  const int lane = lane_id(), g = lane / 16, m = lane % 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wm = wave / WN, wn = wave % WN;
+  const int cnt = expert_count(a.counts, e, a.C);
+  const int K = a.k_is_rows ? cnt : a.K;
+  const int rows = a.k_is_rows ? a.M : cnt;  // rows of the output that are sums
+  const int m0 = bm * BM, n0 = bn * BNO;
+  const int mvalid = max(0, min(BM, rows - m0));
+
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  if (mvalid > 0 && K > 0) {
+    ExpertOperand<bf16_t, KA, false, BM, WAVES> oa;
+    ExpertOperand<bf16_t, KB, true, BN, WAVES> ob;
+    oa.init(reinterpret_cast<const bf16_t*>(a.A) + e * a.sA, a.lda, m0, mvalid, K, wave,
+            [&](int piece) { return m0 + piece * 8 < a.M ? m0 + piece * 8 : -1; });
+    ob.init(reinterpret_cast<const bf16_t*>(a.B) + e * a.sB, a.ldb, n0, min(BN, a.N - n0), K, wave, [&](int piece) {
+      if constexpr (kSplit) {
+        // pieces 0..3 of each wave's 8 are the gate's
+        const int c = n0 + (piece / 8) * 32 + (piece % 4) * 8;
+        return c < a.N ? c + (piece % 8 < 4 ? 0 : a.N) : -1;
+      } else {
+        return n0 + piece * 8 < a.N ? n0 + piece * 8 : -1;
+      }
+    });
+    auto multiply = [&](const bf16_t* As, const bf16_t* Bs) {
+#pragma unroll
+      for (int ks = 0; ks < kEBK / 32; ++ks) {
+        u32x4 fb[NT], fa[MT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) fb[j] = expert_frag<KB, true, BN>(Bs, wn * 64 + 32 * (j / 2), j % 2, ks, g, m);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fa[i] = expert_frag<KA, false, BM>(As, (wm * MT + i) * 16, 0, ks, g, m);
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[j]),
+                                                                __builtin_bit_cast(bf16x8, fa[i]), acc[i][j], 0, 0, 0);
+      }
+    };
+    oa.load(A0, wave, K);
+    ob.load(B0, wave, K);
+    int left = K;
+    for (; left > kEBK; left -= 2 * kEBK) {
+      expert_stage_barrier();
+      oa.load(A1, wave, left - kEBK);
+      ob.load(B1, wave, left - kEBK);
+      multiply(A0, B0);
+      expert_stage_barrier();
+      if (left > 2 * kEBK) {
+        oa.load(A0, wave, left - 2 * kEBK);
+        ob.load(B0, wave, left - 2 * kEBK);
+      }
+      multiply(A1, B1);
+    }
+    if (left > 0) {
+      expert_stage_barrier();
+      multiply(A0, B0);
+    }
+  }
+
+  // lane (g, m): row m of tile i, columns 32 p + 8 g .. + 7 of pair p
+  const int row0 = m0 + wm * MT * 16 + m;
+  const int col0 = n0 + (kSplit ? wn * 32 : wn * 64) + 8 * g;
+  auto value = [&](int i, int p, int q) { return acc[i][2 * p + q / 4][q % 4]; };
+  if constexpr (EPI == kEpiStore) {
+    float bias[NP][8];
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        bias[p][q] = a.bias && col0 + 32 * p < a.N ? a.bias[static_cast<int64_t>(e) * a.N + col0 + 32 * p + q] : 0.f;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+      const int row = row0 + 16 * i;
+      if (row >= a.M) continue;
+      uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + e * a.sO + static_cast<int64_t>(row) * a.ldo;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        if (col0 + 32 * p >= a.N) continue;
+        float v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = row < rows ? value(i, p, q) + bias[p][q] : 0.f;
+        *reinterpret_cast<u32x4*>(out + col0 + 32 * p) = Chunk<bf16_t>::pack(v);
+      }
+    }
+  } else if constexpr (EPI == kEpiAct) {
+    const int N1 = GATED ? 2 * a.N : a.N;
+    constexpr int NPO = kSplit ? 1 : NP;
+    float bias[NP][8];
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int c = kSplit ? col0 : col0 + 32 * p;
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        bias[p][q] = a.bias && c < a.N ? a.bias[static_cast<int64_t>(e) * N1 + c + q + (kSplit && p ? a.N : 0)] : 0.f;
+    }
+    expert_by_act(a.act, [&](auto which) {
+      constexpr int ACT = decltype(which)::v;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int row = row0 + 16 * i;
+        if (row >= a.M) continue;
+        uint16_t* hid = reinterpret_cast<uint16_t*>(a.out) + e * a.sO + static_cast<int64_t>(row) * a.ldo;
+        uint16_t* pre = reinterpret_cast<uint16_t*>(a.pre) + (static_cast<int64_t>(e) * a.C + row) * N1;
+#pragma unroll
+        for (int p = 0; p < NPO; ++p) {
+          const int c = col0 + 32 * p;
+          if (c >= a.N) continue;
+          float v[8], u[8], f[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            v[q] = row < rows ? value(i, p, q) + bias[p][q] : 0.f;
+            f[q] = expert_act<ACT>(v[q]);
+            if constexpr (kSplit) {
+              u[q] = row < rows ? value(i, 1, q) + bias[1][q] : 0.f;
+              f[q] *= u[q];
+            }
+          }
+          if (a.pre) {
+            *reinterpret_cast<u32x4*>(pre + c) = Chunk<bf16_t>::pack(v);
+            if constexpr (kSplit) *reinterpret_cast<u32x4*>(pre + a.N + c) = Chunk<bf16_t>::pack(u);
+          }
+          *reinterpret_cast<u32x4*>(hid + c) = Chunk<bf16_t>::pack(f);
+        }
+      }
+    });
+  } else {
+    // dpre, and its sums over the wave's rows before the rounding: [E, tm * WM, N1]
+    const int N1 = GATED ? 2 * a.N : a.N;
+    float* part = a.colsum ? a.colsum + (static_cast<int64_t>(e) * a.tm * WM + bm * WM + wm) * N1 : nullptr;
+    expert_by_act(a.act, [&](auto which) {
+      constexpr int ACT = decltype(which)::v;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int c = col0 + 32 * p;
+        float s0[8], s1[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) s0[q] = s1[q] = 0.f;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int row = row0 + 16 * i;
+          if (row >= a.M || c >= a.N) continue;
+          const int64_t at = (static_cast<int64_t>(e) * a.C + row) * N1 + c;
+          uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + at;
+          float v[8], u[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) v[q] = u[q] = 0.f;
+          if (row < rows) {
+            const uint16_t* src = reinterpret_cast<const uint16_t*>(a.pre) + at;
+            Chunk<bf16_t>::unpack(*reinterpret_cast<const u32x4*>(src), v);
+            if constexpr (GATED) Chunk<bf16_t>::unpack(*reinterpret_cast<const u32x4*>(src + a.N), u);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              float f, df;
+              expert_act_grad<ACT>(v[q], f, df);
+              const float dh = value(i, p, q);
+              v[q] = GATED ? dh * u[q] * df : dh * df;
+              u[q] = dh * f;
+              s0[q] += v[q];
+              if constexpr (GATED) s1[q] += u[q];
+            }
+          }
+          *reinterpret_cast<u32x4*>(out) = Chunk<bf16_t>::pack(v);
+          if constexpr (GATED) *reinterpret_cast<u32x4*>(out + a.N) = Chunk<bf16_t>::pack(u);
+        }
+        if (part) {
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            s0[q] = group_reduce<16>(s0[q], OpAdd());
+            if constexpr (GATED) s1[q] = group_reduce<16>(s1[q], OpAdd());
+          }
+          if (m == 0 && c < a.N) {
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              part[c + q] = s0[q];
+              if constexpr (GATED) part[a.N + c + q] = s1[q];
+            }
+          }
+        }
+      }
+    });
+  }
+}
+
+}  // namespace hetumoe

@@ -1,0 +1,256 @@
+// Batched fp32 products of the expert networks on v_mfma_f32_16x16x4_f32: the
+// scheme of experts_bf16.hpp with 32 K elements per stage.
+//
+// The order of K inside a product is free, so lane group g of a step of 16 takes
+// K 4 g .. 4 g + 3, one 16-byte read where rows run along K, and its i-th product
+// K 4 g + i; an operand whose rows run the other way is read four columns at a
+// time, tile j taking column 4 m + j, so a lane ends with 4 neighbouring columns.
+// Each 256 K are summed on their own and then added to the running sum.
+#pragma once
+
+#include "experts.hpp"
+
+namespace hetumoe {
+
+constexpr int kFBK = kExpertBk<float>;
+constexpr int kFSum = 8;  // stages summed on their own
+
+// Left operand, step ks of 16: lane (g, m) gets K 4 g + 0..3 of row (column) x0 + m.
+template <int KIND, int W>
+__device__ __forceinline__ f32x4 expert_left_f32(const float* lds, int x0, int ks, int g, int m) {
+  if constexpr (KIND == kRows) {
+    const int row = x0 + m;
+    const int piece = (4 * ks + g) ^ expert_swz<float, KIND, false, W>(row);
+    return *reinterpret_cast<const f32x4*>(lds + row * kFBK + piece * 4);
+  } else {
+    const float* p = lds + (16 * ks + 4 * g) * W + x0 + m;
+    return f32x4{p[0], p[W], p[2 * W], p[3 * W]};
+  }
+}
+
+// Right operand: fb[j][i] is K 4 g + i of row (column) x0 + 4 m + j.
+template <int KIND, int W>
+__device__ __forceinline__ void expert_right_f32(const float* lds, int x0, int ks, int g, int m, f32x4 (&fb)[4]) {
+  if constexpr (KIND == kRows) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int row = x0 + 4 * m + j;
+      const int piece = (4 * ks + g) ^ expert_swz<float, KIND, true, W>(row);
+      fb[j] = *reinterpret_cast<const f32x4*>(lds + row * kFBK + piece * 4);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(lds + (16 * ks + 4 * g + i) * W + x0 + 4 * m);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) fb[j][i] = v[j];
+    }
+  }
+}
+
+template <int BM, int BN, int WM, int WN, int KA, int KB, int EPI, bool GATED>
+__global__ __launch_bounds__(WM* WN * 64) void experts_gemm_f32_kernel(ExpertGemmArgs a) {
+  constexpr int WAVES = WM * WN;
+  constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
+  static_assert(NT == 4, "64 columns per wave");
+  constexpr bool kSplit = EPI == kEpiAct && GATED;  // 32 columns of the gate and 32 of the other factor per wave
+  constexpr int BNO = kSplit ? BN / 2 : BN;
+  __shared__ __align__(1024) float A0[BM * kFBK], B0[BN * kFBK], A1[BM * kFBK], B1[BN * kFBK];
+
+  int e, bm, bn;
+  if (!expert_tile(a.tiles, a.tm, a.tn, e, bm, bn)) return;
+  const int lane = lane_id(), g = lane / 16, m = lane % 16;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int wm = wave / WN, wn = wave % WN;
+  const int cnt = expert_count(a.counts, e, a.C);
+  const int K = a.k_is_rows ? cnt : a.K;
+  const int rows = a.k_is_rows ? a.M : cnt;
+  const int m0 = bm * BM, n0 = bn * BNO;
+  const int mvalid = max(0, min(BM, rows - m0));
+
+  f32x4 acc[MT][NT], sum[MT][NT];
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = sum[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  if (mvalid > 0 && K > 0) {
+    ExpertOperand<float, KA, false, BM, WAVES> oa;
+    ExpertOperand<float, KB, true, BN, WAVES> ob;
+    oa.init(reinterpret_cast<const float*>(a.A) + e * a.sA, a.lda, m0, mvalid, K, wave,
+            [&](int piece) { return m0 + piece * 4 < a.M ? m0 + piece * 4 : -1; });
+    ob.init(reinterpret_cast<const float*>(a.B) + e * a.sB, a.ldb, n0, min(BN, a.N - n0), K, wave, [&](int piece) {
+      if constexpr (kSplit) {
+        // lane group g of a wave ends with pieces 4 g .. 4 g + 3 of its 16: two of
+        // the gate, the same two of the other factor
+        const int pp = piece % 16;
+        const int c = n0 + (piece / 16) * 32 + ((pp / 4) * 2 + (pp & 1)) * 4;
+        return c < a.N ? c + (pp & 2 ? a.N : 0) : -1;
+      } else {
+        return n0 + piece * 4 < a.N ? n0 + piece * 4 : -1;
+      }
+    });
+    auto multiply = [&](const float* As, const float* Bs) {
+#pragma unroll
+      for (int ks = 0; ks < kFBK / 16; ++ks) {
+        f32x4 fb[NT], fa[MT];
+        expert_right_f32<KB, BN>(Bs, wn * 64, ks, g, m, fb);
+#pragma unroll
+        for (int i = 0; i < MT; ++i) fa[i] = expert_left_f32<KA, BM>(As, (wm * MT + i) * 16, ks, g, m);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[j][q], fa[i][q], acc[i][j], 0, 0, 0);
+      }
+    };
+    auto flush = [&]() {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) {
+          sum[i][j] += acc[i][j];
+          acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+    };
+    oa.load(A0, wave, K);
+    ob.load(B0, wave, K);
+    int stage = 0;
+    int left = K;
+    for (; left > kFBK; left -= 2 * kFBK) {
+      expert_stage_barrier();
+      oa.load(A1, wave, left - kFBK);
+      ob.load(B1, wave, left - kFBK);
+      multiply(A0, B0);
+      expert_stage_barrier();
+      if (left > 2 * kFBK) {
+        oa.load(A0, wave, left - 2 * kFBK);
+        ob.load(B0, wave, left - 2 * kFBK);
+      }
+      multiply(A1, B1);
+      stage += 2;
+      if (stage % kFSum == 0) flush();
+    }
+    if (left > 0) {
+      expert_stage_barrier();
+      multiply(A0, B0);
+    }
+    flush();
+  }
+
+  // lane (g, m): row m of tile i, columns 16 g + 4 r + 0..3, r = 0..3
+  const int row0 = m0 + wm * MT * 16 + m;
+  const int col0 = n0 + (kSplit ? wn * 32 + 8 * g : wn * 64 + 16 * g);
+  auto value = [&](int i, int r, int q) { return sum[i][q][r]; };
+  auto put = [](float* p, const float (&v)[4]) { *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]}; };
+  if constexpr (EPI == kEpiStore) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int c = col0 + 4 * r;
+      if (c >= a.N) continue;
+      float bias[4];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) bias[q] = a.bias ? a.bias[static_cast<int64_t>(e) * a.N + c + q] : 0.f;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) {
+        const int row = row0 + 16 * i;
+        if (row >= a.M) continue;
+        float v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = row < rows ? value(i, r, q) + bias[q] : 0.f;
+        put(reinterpret_cast<float*>(a.out) + e * a.sO + static_cast<int64_t>(row) * a.ldo + c, v);
+      }
+    }
+  } else if constexpr (EPI == kEpiAct) {
+    const int N1 = GATED ? 2 * a.N : a.N;
+    constexpr int R = kSplit ? 2 : 4;
+    expert_by_act(a.act, [&](auto which) {
+      constexpr int ACT = decltype(which)::v;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int c = col0 + 4 * r;
+        if (c >= a.N) continue;
+        float b0[4], b1[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          b0[q] = a.bias ? a.bias[static_cast<int64_t>(e) * N1 + c + q] : 0.f;
+          b1[q] = kSplit && a.bias ? a.bias[static_cast<int64_t>(e) * N1 + a.N + c + q] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int row = row0 + 16 * i;
+          if (row >= a.M) continue;
+          float v[4], u[4], f[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            v[q] = row < rows ? value(i, r, q) + b0[q] : 0.f;
+            f[q] = expert_act<ACT>(v[q]);
+            if constexpr (kSplit) {
+              u[q] = row < rows ? value(i, r + 2, q) + b1[q] : 0.f;
+              f[q] *= u[q];
+            }
+          }
+          if (a.pre) {
+            float* pre = reinterpret_cast<float*>(a.pre) + (static_cast<int64_t>(e) * a.C + row) * N1 + c;
+            put(pre, v);
+            if constexpr (kSplit) put(pre + a.N, u);
+          }
+          put(reinterpret_cast<float*>(a.out) + e * a.sO + static_cast<int64_t>(row) * a.ldo + c, f);
+        }
+      }
+    });
+  } else {
+    const int N1 = GATED ? 2 * a.N : a.N;
+    float* part = a.colsum ? a.colsum + (static_cast<int64_t>(e) * a.tm * WM + bm * WM + wm) * N1 : nullptr;
+    expert_by_act(a.act, [&](auto which) {
+      constexpr int ACT = decltype(which)::v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int c = col0 + 4 * r;
+        float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const int row = row0 + 16 * i;
+          if (row >= a.M || c >= a.N) continue;
+          const int64_t at = (static_cast<int64_t>(e) * a.C + row) * N1 + c;
+          float v[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f};
+          if (row < rows) {
+            const float* src = reinterpret_cast<const float*>(a.pre) + at;
+            Chunk<float>::unpack(*reinterpret_cast<const u32x4*>(src), v);
+            if constexpr (GATED) Chunk<float>::unpack(*reinterpret_cast<const u32x4*>(src + a.N), u);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float f, df;
+              expert_act_grad<ACT>(v[q], f, df);
+              const float dh = value(i, r, q);
+              v[q] = GATED ? dh * u[q] * df : dh * df;
+              u[q] = dh * f;
+              s0[q] += v[q];
+              if constexpr (GATED) s1[q] += u[q];
+            }
+          }
+          put(reinterpret_cast<float*>(a.out) + at, v);
+          if constexpr (GATED) put(reinterpret_cast<float*>(a.out) + at + a.N, u);
+        }
+        if (part) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            s0[q] = group_reduce<16>(s0[q], OpAdd());
+            if constexpr (GATED) s1[q] = group_reduce<16>(s1[q], OpAdd());
+          }
+          if (m == 0 && c < a.N) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              part[c + q] = s0[q];
+              if constexpr (GATED) part[a.N + c + q] = s1[q];
+            }
+          }
+        }
+      }
+    });
+  }
+}
+
+}  // namespace hetumoe

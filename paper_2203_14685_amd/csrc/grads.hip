@@ -1,0 +1,159 @@
+// The global norm of many gradients and their clipping.
+//
+// Bound by memory: one read for the norm, one read and one write to scale.  The
+// tensors are cut into chunks of kChunk elements; each block takes every gridDim-th
+// chunk, adds the squares in 64 bits (a square of fp32 may not fit fp32, and the sum of
+// 10^9 terms needs more than 24 bits) and leaves one sum, which one block adds in
+// order: the result depends on the sizes alone and repeats bit for bit.
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace hetumoe {
+
+namespace {
+
+constexpr int kGradUnroll = 8;  // 16-byte pieces in flight per thread
+
+// Tensor of chunk `c`: the last one whose first chunk is not behind it.
+__device__ __forceinline__ int tensor_of(const GradList& l, int c) {
+  int lo = 0, hi = l.n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (l.t[mid].first <= c) lo = mid;
+    else hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ double square(float v) { return static_cast<double>(v) * static_cast<double>(v); }
+
+template <class T>
+__device__ __forceinline__ double chunk_squares(const T* p, int64_t n, bool vec) {
+  constexpr int PE = Chunk<T>::kElems;
+  double s = 0.0;
+  int64_t done = 0;
+  if (vec) {
+    const int64_t pieces = n / PE;
+    const u32x4* q = reinterpret_cast<const u32x4*>(p);
+    for (int64_t i = threadIdx.x; i < pieces; i += kBlock * kGradUnroll) {
+      u32x4 v[kGradUnroll];
+#pragma unroll
+      for (int u = 0; u < kGradUnroll; ++u)
+        if (i + u * kBlock < pieces) v[u] = q[i + u * kBlock];
+#pragma unroll
+      for (int u = 0; u < kGradUnroll; ++u) {
+        if (i + u * kBlock >= pieces) continue;
+        float f[PE];
+        Chunk<T>::unpack(v[u], f);
+#pragma unroll
+        for (int e = 0; e < PE; ++e) s += square(f[e]);
+      }
+    }
+    done = pieces * PE;
+  }
+  for (int64_t i = done + threadIdx.x; i < n; i += kBlock) s += square(load_elem(p, i));
+  return s;
+}
+
+__device__ __forceinline__ double block_sum(double s) {
+  __shared__ double lds[kWavesPerBlock];
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) s += xor_partner(s, m);
+  if (lane_id() == 0) lds[threadIdx.x / kWave] = s;
+  __syncthreads();
+  double t = 0.0;
+#pragma unroll
+  for (int w = 0; w < kWavesPerBlock; ++w) t += lds[w];
+  return t;
+}
+
+__global__ __launch_bounds__(kBlock) void grad_squares_kernel(GradList l, double* part) {
+  double s = 0.0;
+  for (int c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+    const GradTensor& t = l.t[tensor_of(l, c)];
+    const int64_t at = static_cast<int64_t>(c - t.first) * kGradChunk;
+    const int64_t n = min(static_cast<int64_t>(kGradChunk), t.n - at);
+    s += t.dtype == 1 ? chunk_squares(static_cast<const bf16_t*>(t.src) + at, n, t.vec_src)
+                      : chunk_squares(static_cast<const float*>(t.src) + at, n, t.vec_src);
+  }
+  s = block_sum(s);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+__global__ __launch_bounds__(kBlock) void grad_finish_kernel(const double* part, int n, double* sumsq, float* norm) {
+  double s = 0.0;
+  for (int i = threadIdx.x; i < n; i += kBlock) s += part[i];
+  s = block_sum(s);
+  if (threadIdx.x == 0) {
+    if (sumsq) *sumsq = s;
+    if (norm) *norm = static_cast<float>(sqrt(s));
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, bool vec, float scale) {
+  constexpr int PE = Chunk<T>::kElems;
+  int64_t done = 0;
+  if (vec) {
+    const int64_t pieces = n / PE;
+    const u32x4* q = reinterpret_cast<const u32x4*>(src);
+    u32x4* o = reinterpret_cast<u32x4*>(dst);
+    for (int64_t i = threadIdx.x; i < pieces; i += kBlock * kGradUnroll) {
+      u32x4 v[kGradUnroll];
+#pragma unroll
+      for (int u = 0; u < kGradUnroll; ++u)
+        if (i + u * kBlock < pieces) v[u] = q[i + u * kBlock];
+#pragma unroll
+      for (int u = 0; u < kGradUnroll; ++u) {
+        if (i + u * kBlock >= pieces) continue;
+        float f[PE];
+        Chunk<T>::unpack(v[u], f);
+#pragma unroll
+        for (int e = 0; e < PE; ++e) f[e] *= scale;
+        o[i + u * kBlock] = Chunk<T>::pack(f);
+      }
+    }
+    done = pieces * PE;
+  }
+  for (int64_t i = done + threadIdx.x; i < n; i += kBlock) {
+    const float v = load_elem(src, i) * scale;
+    if constexpr (sizeof(T) == 2) dst[i].bits = static_cast<uint16_t>(f32_to_bf16_bits(v));
+    else dst[i] = v;
+  }
+}
+
+__global__ __launch_bounds__(kBlock) void grad_scale_kernel(GradList l, const double* sumsq, float max_norm, float* norm) {
+  const double nm = sqrt(*sumsq);
+  // a NaN norm makes the scale NaN
+  const float scale = nm <= max_norm ? 1.f : static_cast<float>(max_norm / nm);
+  if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(nm);
+  for (int c = blockIdx.x; c < l.chunks; c += gridDim.x) {
+    const GradTensor& t = l.t[tensor_of(l, c)];
+    if (scale == 1.f && t.src == t.dst) continue;
+    const int64_t at = static_cast<int64_t>(c - t.first) * kGradChunk;
+    const int64_t n = min(static_cast<int64_t>(kGradChunk), t.n - at);
+    if (t.dtype == 1)
+      chunk_scale(static_cast<const bf16_t*>(t.src) + at, static_cast<bf16_t*>(t.dst) + at, n, t.vec_both, scale);
+    else
+      chunk_scale(static_cast<const float*>(t.src) + at, static_cast<float*>(t.dst) + at, n, t.vec_both, scale);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_grad_squares(const GradList& l, double* part, hipStream_t st) {
+  grad_squares_kernel<<<grad_blocks(l.chunks), kBlock, 0, st>>>(l, part);
+  return hipGetLastError();
+}
+
+hipError_t launch_grad_finish(const double* part, int n, double* sumsq, float* norm, hipStream_t st) {
+  grad_finish_kernel<<<1, kBlock, 0, st>>>(part, n, sumsq, norm);
+  return hipGetLastError();
+}
+
+hipError_t launch_grad_scale(const GradList& l, const double* sumsq, float max_norm, float* norm, hipStream_t st) {
+  grad_scale_kernel<<<l.chunks > 0 ? grad_blocks(l.chunks) : 1, kBlock, 0, st>>>(l, sumsq, max_norm, norm);
+  return hipGetLastError();
+}
+
+}  // namespace hetumoe

@@ -233,4 +233,79 @@ hipError_t run_base_auction(const BaseArgs& a, hipStream_t st, BaseStats* stats)
 // auction did not finish (its current one, else s mod E).
 hipError_t run_base_auction_async(const BaseArgs& a, int launch_rounds, BaseDevStatus* status, hipStream_t st);
 
+// Expert networks (step 4 of Algorithm 1): one batched product (experts.hpp).
+struct ExpertGemmArgs {
+  int C;                    // slots per expert
+  int M, N, K;              // of the product; N: columns of out (gated forward: of hidden)
+  int k_is_rows;            // K is the expert's rows in use (weight gradients), else M is cut at them
+  int tm, tn, tiles;        // blocks along M and N, all blocks
+  const int32_t* counts;    // [E] or null (all C)
+  const void *A, *B;
+  int64_t sA, sB, sO;       // elements from one expert's matrix to the next
+  int lda, ldb, ldo;
+  const float* bias;        // [E, N] ([E, 2 N] gated forward) or null
+  void* out;
+  void* pre;                // kEpiAct: output or null; kEpiActGrad: input
+  float* colsum;            // kEpiActGrad: [E, parts, N1] or null
+  int act;
+};
+
+struct ExpertArgs {
+  int E, C, d, h, act, gated, dtype;
+  const int32_t* counts;
+  const void *xe, *w1, *w2;
+  const float *b1, *b2;
+  void *pre, *hidden, *ye;
+  // backward
+  const void* dye;
+  void *dpre, *dxe, *dw1, *dw2;
+  float *db1, *db2;
+  float* colsum;            // workspace [E, expert_parts, h1]
+  float* rowsum;            // workspace [E, expert_row_parts, d]
+};
+hipError_t launch_experts(const ExpertArgs& a, hipStream_t st);
+hipError_t launch_experts_bwd(const ExpertArgs& a, hipStream_t st);
+// Row ranges per expert whose sums of dpre, and of dye, go to the workspace.
+int expert_parts(const ExpertArgs& a);
+int expert_row_parts(const ExpertArgs& a);
+
+// The layer for a few tokens (layer.hip), behind its gate.
+constexpr int kLayerMaxTokens = 256;
+constexpr int kLayerMaxChoices = kLayerMaxTokens * 8;
+struct LayerArgs {
+  int S, d, E, k, h, act, gated, dtype;
+  int by_choice;            // blocks per choice (S * k <= E), else per expert
+  int z2;                   // parts of the second product's K
+  const void *x, *w1, *w2;
+  const float *b1, *b2;
+  const int32_t* ids;       // [S, k]; outside [0, E): no expert
+  const float* weights;     // [S, k]
+  void* hidden;             // workspace [S * k, h]
+  float* part;              // workspace [z2, S * k, d]
+  void* y;                  // [S, d]
+};
+int layer_splits(const LayerArgs& a);
+hipError_t launch_layer(const LayerArgs& a, hipStream_t st);
+
+// Gradients by chunks (grads.hip).  A list holds as many tensors as fit a launch's
+// arguments; longer ones take several launches.
+constexpr int kGradChunk = 16384;
+constexpr int kGradListMax = 64;
+constexpr int kGradMaxBlocks = 2048;
+struct GradTensor {
+  const void* src;
+  void* dst;
+  int64_t n;
+  int first;                // its first chunk within the list
+  int8_t dtype, vec_src, vec_both, pad;  // vec: 16-byte aligned
+};
+struct GradList {
+  GradTensor t[kGradListMax];
+  int n, chunks;
+};
+inline int grad_blocks(int chunks) { return chunks < kGradMaxBlocks ? chunks : kGradMaxBlocks; }
+hipError_t launch_grad_squares(const GradList& l, double* part, hipStream_t st);
+hipError_t launch_grad_finish(const double* part, int n, double* sumsq, float* norm, hipStream_t st);
+hipError_t launch_grad_scale(const GradList& l, const double* sumsq, float max_norm, float* norm, hipStream_t st);
+
 }  // namespace hetumoe
