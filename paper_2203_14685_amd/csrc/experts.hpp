@@ -47,10 +47,11 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t expert_rsrc(const void* p, int
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
 }
 
-// Every load of this wave has arrived in LDS and every LDS read has returned;
-// after the barrier that holds for the whole block.
+// At most VM of this wave's loads to LDS are still on their way and every LDS read has
+// returned; after the barrier that holds for the whole block.
+template <int VM = 0>
 __device__ __forceinline__ void expert_stage_barrier() {
-  __builtin_amdgcn_s_waitcnt(0x0070);  // vmcnt(0) lgkmcnt(0)
+  __builtin_amdgcn_s_waitcnt(0x0070 | (VM & 15) | ((VM >> 4) << 14));  // vmcnt(VM) lgkmcnt(0)
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
@@ -62,28 +63,25 @@ template <class T> constexpr int kExpertBk = 128 / static_cast<int>(sizeof(T));
 // Elements of a 16-byte piece.
 template <class T> constexpr int kExpertPe = 16 / static_cast<int>(sizeof(T));
 
-// Which 16-byte piece of its row lies at place `c` of LDS row `row`.
+// Which 16-byte piece of its row lies at place `c` of LDS row `row`: piece c ^ swz.
 //   kRows: 8 pieces per 128-byte row; two rows fill the 64 banks.  A fragment read takes
-//          rows r .. r + 15 (left operand) or, of the right one, 8 i + 4 t + 0..3, i = 0..3
-//          (bf16) or 4 i + t, i = 0..15 (fp32).
-//   kCols: bf16: a transpose read takes k rows 8 g + 4 h + 0..3, of each 32 contiguous bytes
-//          (left) or four 8-byte halves of neighbouring pieces (right); fp32 reads run along
-//          a row and need no other order.
+//          rows r .. r + 15 or, of the right operand in fp32, 4 i + t, i = 0..15.
+//   kCols: bf16: a transpose read takes k rows 8 g + 4 h + 0..3, g = 0..3, of each 32
+//          contiguous bytes; fp32 reads run along a row and need no other order.
 template <class T, int KIND, bool RIGHT, int W>
 __device__ __forceinline__ int expert_swz(int row) {
-  if constexpr (KIND == kRows) {
-    if constexpr (!RIGHT) return (row >> 1) & 7;
-    else if constexpr (sizeof(T) == 2) return ((row >> 1) & 1) | ((row >> 2) & 6);
-    else return (row >> 2) & 7;
-  } else if constexpr (sizeof(T) == 4) {
-    return 0;
-  } else if constexpr (W >= 128) {
-    if constexpr (RIGHT) return (row & 3) << 2;
-    else return ((row & 3) << 1) | (row & 8);
-  } else {
-    if constexpr (RIGHT) return ((row >> 1) & 1) << 2;
-    else return (((row >> 1) & 1) << 1) | ((row & 8) >> 1);
-  }
+  if constexpr (KIND == kRows) return (RIGHT && sizeof(T) == 4 ? row >> 2 : row >> 1) & 7;
+  else if constexpr (sizeof(T) == 4) return 0;
+  else if constexpr (W >= 128) return ((row & 3) << 1) | (row & 8);
+  else return (((row >> 1) & 1) << 1) | ((row & 8) >> 1);
+}
+
+// Keeps what is computed from v inside the loop: a sum or exclusive-or per use instead
+// of a register held for each.
+template <class V>
+__device__ __forceinline__ V expert_opaque(V v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // One operand's loads: W rows (kRows) or columns (kCols) of the tile.
@@ -93,54 +91,58 @@ struct ExpertOperand {
   static constexpr int kBytes = W * 128;
   static constexpr int N = kBytes / 1024 / WAVES;  // loads per wave and stage
   static_assert(N * WAVES * 1024 == kBytes, "whole loads");
+  static constexpr int P = KIND == kRows ? 8 : W / kPe;  // pieces per LDS row
+  static constexpr int R = 64 / P;                       // rows per load
+  // a lane's rows are R * WAVES apart: where that changes the order of the pieces, two offsets in turn
+  static constexpr int kAlt = KIND == kCols && kElt == 2 && R * WAVES % 16 != 0 ? 2 : 1;
+  static_assert(KIND == kCols || R * WAVES % 32 == 0, "one order of the pieces per lane");
   const char* base;   // (first row or column, k = 0)
   int64_t step;       // bytes per stage
   int64_t limit;      // bytes behind base that may be read, less what the stages took
   int cap;            // most that a stage's resource needs
-  int off[N];
+  unsigned off[kAlt], stride;
   int kc;             // kRows: the lane's K element in a stage
 
   // map(piece) gives the column of the tile's piece, or -1 behind the matrix.
   template <class Map>
   __device__ __forceinline__ void init(const T* p, int ld, int first, int valid, int K, int wave, Map map) {
     const int lane = lane_id();
+    const int row0 = wave * R + lane / P;
+    stride = static_cast<unsigned>(R * WAVES) * static_cast<unsigned>(ld) * kElt;
+    kc = 0;
     if constexpr (KIND == kRows) {
       base = reinterpret_cast<const char*>(p + static_cast<int64_t>(first) * ld);
       step = 128;
       limit = static_cast<int64_t>(valid) * ld * kElt;
       cap = 0x7fffff00;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int row = (i * WAVES + wave) * 8 + lane / 8;
-        const int piece = (lane % 8) ^ expert_swz<T, KIND, RIGHT, W>(row);
-        if (i == 0) kc = piece * kPe;  // the same for every i: rows differ by multiples of 32
-        off[i] = row < valid ? row * ld * kElt + piece * 16 : kExpertOob;
-      }
+      const int piece = (lane % 8) ^ expert_swz<T, KIND, RIGHT, W>(row0);
+      kc = piece * kPe;
+      off[0] = static_cast<unsigned>(row0 * ld * kElt + piece * 16);
     } else {
-      constexpr int P = W / kPe;   // pieces per row
-      constexpr int R = 64 / P;  // rows per load
       base = reinterpret_cast<const char*>(p);
       step = static_cast<int64_t>(kBk) * ld * kElt;
       limit = static_cast<int64_t>(K) * ld * kElt;
       cap = kBk * ld * kElt;
-      kc = 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const int row = (i * WAVES + wave) * R + lane / P;
-        const int col = map((lane % P) ^ expert_swz<T, KIND, RIGHT, W>(row));
-        off[i] = col >= 0 ? (row * ld + col) * kElt : kExpertOob;
+      for (int i = 0; i < kAlt; ++i) {
+        const int col = map((lane % P) ^ expert_swz<T, KIND, RIGHT, W>(row0 + i * R * WAVES));
+        off[i] = col >= 0 ? static_cast<unsigned>((row0 * ld + col) * kElt) : static_cast<unsigned>(kExpertOob);
       }
     }
   }
-  // The stage `base` points at; `left` K elements remain.
+  // The stage `base` points at; `left` K elements remain.  An offset past the resource
+  // stays past it (below 2^32) with the rows' strides added.
   __device__ __forceinline__ void load(T* lds, int wave, int left) {
     const __amdgpu_buffer_rsrc_t r = expert_rsrc(base, static_cast<int>(min(limit, static_cast<int64_t>(cap))));
+    unsigned o[kAlt];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      int o = off[i];
-      if constexpr (KIND == kRows) o = kc < left ? o : kExpertOob;
-      expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, o);
+    for (int i = 0; i < kAlt; ++i) {
+      o[i] = expert_opaque(off[i]);
+      if constexpr (KIND == kRows) o[i] = kc < left ? o[i] : static_cast<unsigned>(kExpertOob);
     }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, static_cast<int>(o[i % kAlt] + i * stride));
     base += step;
     limit -= step;
   }

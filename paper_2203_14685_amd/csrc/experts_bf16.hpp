@@ -2,17 +2,21 @@
 //
 // A block forms BM x BN of one expert's product, WM x WN waves, 64 columns each.
 // Per stage of 64 K elements both operands go straight from memory to LDS as
-// they lie there (16 bytes per lane, no registers), two stages in turn: the next
-// one is on its way while this one is multiplied, one barrier per stage.  Operands
+// they lie there (16 bytes per lane, no registers), two stages in turn.  Operands
 // whose rows run along K are read as 16-byte fragments, the others through LDS
 // transpose reads.  16-byte pieces are placed by an exclusive-or with bits of
 // their row, so that the 16 lanes of a fragment read touch different banks; since
 // a load to LDS fills it in lane order, the lane fetches the piece that belongs
 // where it writes.
 //
-// The product is formed transposed (columns n are the rows of the matrix unit),
-// and the 16 x 16 tiles come in pairs whose rows interleave by fours: a lane then
-// holds 8 neighbouring columns of one row, one 16-byte store.
+// While one half of a stage (32 K) is multiplied the fragments of the next half are
+// read, so the reads' latency and the one barrier per stage lie behind products; the
+// stage after next is requested as soon as every wave has read the last half of
+// the stage in its place.
+//
+// The product is formed transposed (columns n are the rows of the matrix unit), so a lane
+// holds 4 neighbouring columns of one row; a swap with the neighbouring 16 lanes over a
+// pair of tiles makes that 8, one 16-byte store.
 //
 // Rows past the expert's count and pieces past K are zeros from outside the buffer
 // resource; nothing behind the count is read.
@@ -24,25 +28,33 @@ namespace hetumoe {
 
 constexpr int kEBK = kExpertBk<bf16_t>;
 
-// Fragment of K step ks (32 elements): lane (g, m) gets K 8 g .. 8 g + 7 of
-// left: row (or column) x0 + m;  right: x0 + 8 (m / 4) + 4 t + m % 4, tile t of a pair.
-template <int KIND, bool RIGHT, int W>
-__device__ __forceinline__ u32x4 expert_frag(const bf16_t* lds, int x0, int t, int ks, int g, int m) {
-  if constexpr (KIND == kRows) {
-    const int row = x0 + (RIGHT ? 8 * (m / 4) + 4 * t + m % 4 : m);
-    const int piece = (4 * ks + g) ^ expert_swz<bf16_t, KIND, RIGHT, W>(row);
-    return *reinterpret_cast<const u32x4*>(lds + row * kEBK + piece * 8);
-  } else {
-    uint2 half[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int row = 32 * ks + 8 * g + 4 * h + m / 4;
-      const int col = x0 + (RIGHT ? 8 * (m % 4) + 4 * t : 4 * (m % 4));
-      half[h] = expert_tr16(lds + row * W + (((col / 8) ^ expert_swz<bf16_t, KIND, RIGHT, W>(row)) * 8) + col % 8);
+// Fragments: of K step ks (32 elements) lane (g, m) gets K 8 g .. 8 g + 7 of row (or
+// column) x0 + 16 i + m, i = 0 .. MT - 1, x0 a multiple of 16 MT.
+template <int KIND, bool RIGHT, int W, int MT>
+struct ExpertFrag {
+  unsigned at;  // byte of (i = 0, ks = 0)
+  __device__ __forceinline__ void init(int x0, int g, int m) {
+    if constexpr (KIND == kRows) {
+      at = (x0 + m) * 128 + ((g ^ expert_swz<bf16_t, KIND, RIGHT, W>(m)) * 16);
+    } else {
+      const int row = 8 * g + m / 4;
+      at = row * W * 2 + (((x0 / 8 + m % 4 / 2) ^ expert_swz<bf16_t, KIND, RIGHT, W>(row)) * 16) + m % 2 * 8;
     }
-    return u32x4{half[0].x, half[0].y, half[1].x, half[1].y};
   }
-}
+  // kRows: tiles are 16 rows apart, the steps' pieces differ in bit 2 of their place.
+  // kCols: a tile is 32 bytes, bits that are free of carries; rows 4 and 32 on keep their order.
+  __device__ __forceinline__ u32x4 read(const bf16_t* lds, unsigned from, int ks, int i) const {
+    const char* p = reinterpret_cast<const char*>(lds);
+    if constexpr (KIND == kRows) {
+      return *reinterpret_cast<const u32x4*>(p + (from ^ (ks * 64)) + i * 2048);
+    } else {
+      const char* q = p + (from ^ (i * 32)) + ks * 64 * W;
+      const uint2 lo = expert_tr16(reinterpret_cast<const bf16_t*>(q));
+      const uint2 hi = expert_tr16(reinterpret_cast<const bf16_t*>(q + 8 * W));
+      return u32x4{lo.x, lo.y, hi.x, hi.y};
+    }
+  }
+};
 
 template <int BM, int BN, int WM, int WN, int KA, int KB, int EPI, bool GATED>
 __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGemmArgs a) {
@@ -86,46 +98,76 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         return n0 + piece * 8 < a.N ? n0 + piece * 8 : -1;
       }
     });
-    auto multiply = [&](const bf16_t* As, const bf16_t* Bs) {
+    ExpertFrag<KA, false, BM, MT> ra;
+    ExpertFrag<KB, true, BN, NT> rb;
+    ra.init(wm * MT * 16, g, m);
+    rb.init(wn * NT * 16, g, m);
+    constexpr int kLoads = ExpertOperand<bf16_t, KA, false, BM, WAVES>::N + ExpertOperand<bf16_t, KB, true, BN, WAVES>::N;
+    u32x4 fa[MT], fb[NT], fn[NT];
+    // Products of the half stage in fa and fb; each left fragment makes room for the one of
+    // the next half, step ks of (As, Bs), as soon as it is used.
+    auto half = [&](u32x4 (&cur)[NT], u32x4 (&next)[NT], const bf16_t* As, const bf16_t* Bs, int ks) {
+      const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
 #pragma unroll
-      for (int ks = 0; ks < kEBK / 32; ++ks) {
-        u32x4 fb[NT], fa[MT];
+      for (int j = 0; j < NT; ++j) next[j] = rb.read(Bs, at_b, ks, j);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) fb[j] = expert_frag<KB, true, BN>(Bs, wn * 64 + 32 * (j / 2), j % 2, ks, g, m);
+      for (int i = 0; i < MT; ++i) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) fa[i] = expert_frag<KA, false, BM>(As, (wm * MT + i) * 16, 0, ks, g, m);
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int j = 0; j < NT; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, fb[j]),
-                                                                __builtin_bit_cast(bf16x8, fa[i]), acc[i][j], 0, 0, 0);
+        for (int j = 0; j < NT; ++j)
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, cur[j]),
+                                                              __builtin_bit_cast(bf16x8, fa[i]), acc[i][j], 0, 0, 0);
+        fa[i] = ra.read(As, at_a, ks, i);
       }
+    };
+    // One stage in (As, Bs), its first half in fa and fb; `left` K elements from its
+    // start.  Leaves the first half of the next stage, (An, Bn), there (after the last
+    // stage: what that buffer holds, unused).
+    auto stage = [&](bf16_t* As, bf16_t* Bs, bf16_t* An, bf16_t* Bn, int left) {
+      half(fb, fn, As, Bs, 1);
+      expert_stage_barrier();
+      if (left > 2 * kEBK) {
+        oa.load(As, wave, left - 2 * kEBK);
+        ob.load(Bs, wave, left - 2 * kEBK);
+      }
+      half(fn, fb, An, Bn, 0);
     };
     oa.load(A0, wave, K);
     ob.load(B0, wave, K);
+    if (K > kEBK) {
+      oa.load(A1, wave, K - kEBK);
+      ob.load(B1, wave, K - kEBK);
+      expert_stage_barrier<kLoads>();
+    } else {
+      expert_stage_barrier();
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) fb[j] = rb.read(B0, rb.at, 0, j);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) fa[i] = ra.read(A0, ra.at, 0, i);
     int left = K;
     for (; left > kEBK; left -= 2 * kEBK) {
-      expert_stage_barrier();
-      oa.load(A1, wave, left - kEBK);
-      ob.load(B1, wave, left - kEBK);
-      multiply(A0, B0);
-      expert_stage_barrier();
-      if (left > 2 * kEBK) {
-        oa.load(A0, wave, left - 2 * kEBK);
-        ob.load(B0, wave, left - 2 * kEBK);
-      }
-      multiply(A1, B1);
+      stage(A0, B0, A1, B1, left);
+      stage(A1, B1, A0, B0, left - kEBK);
     }
-    if (left > 0) {
-      expert_stage_barrier();
-      multiply(A0, B0);
-    }
+    if (left > 0) stage(A0, B0, A1, B1, left);
   }
 
-  // lane (g, m): row m of tile i, columns 32 p + 8 g .. + 7 of pair p
+  // lane (g, m): row m of tile i, columns 4 g .. 4 g + 3 of each tile.  Odd groups of 16
+  // lanes swap their first tile of a pair for the second one of the group before:
+  // 8 neighbouring columns each, from 16 (g % 2) + 8 (g / 2).
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(acc[i][2 * p][q]),
+                                                        __float_as_uint(acc[i][2 * p + 1][q]), false, false);
+        acc[i][2 * p][q] = __uint_as_float(r[0]);
+        acc[i][2 * p + 1][q] = __uint_as_float(r[1]);
+      }
   const int row0 = m0 + wm * MT * 16 + m;
-  const int col0 = n0 + (kSplit ? wn * 32 : wn * 64) + 8 * g;
+  const int col0 = n0 + (kSplit ? wn * 32 : wn * 64) + 16 * (g % 2) + 8 * (g / 2);
   auto value = [&](int i, int p, int q) { return acc[i][2 * p + q / 4][q % 4]; };
   if constexpr (EPI == kEpiStore) {
     float bias[NP][8];
