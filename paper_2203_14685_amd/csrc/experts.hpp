@@ -195,18 +195,76 @@ __device__ __forceinline__ int expert_count(const int32_t* counts, int e, int C)
   return counts ? max(0, min(counts[e], C)) : C;
 }
 
-// Block -> (expert, m tile, n tile).  Blocks go round the 8 XCDs in turn; each XCD
-// takes one contiguous piece of the tiles, an expert's tiles together, so that
-// its own L2 serves an expert's rows and weights to the tiles that share them.
-__device__ __forceinline__ bool expert_tile(int tiles, int tm, int tn, int& e, int& bm, int& bn) {
-  const int per = (tiles + 7) / 8;
-  const int t = static_cast<int>(blockIdx.x % 8) * per + static_cast<int>(blockIdx.x / 8);
-  if (static_cast<int>(blockIdx.x / 8) >= per || t >= tiles) return false;
-  e = t / (tm * tn);
-  const int r = t - e * tm * tn;
-  bn = r / tm;
-  bm = r - bn * tm;
-  return true;
+// Block -> (expert, m tile, n tile).  Blocks go round the 8 XCDs in turn.  Groups of
+// neighbouring tiles (an expert's m tiles first: they share its weights, and a few n
+// tiles its rows) go to one XCD, whose L2 then serves them, the groups round the XCDs
+// in order, so that experts of any load spread evenly (64 experts of uneven load, one
+// contiguous piece of the tiles per XCD: CUs busy 62 % of the time).  Tiles without rows in
+// use, which are only cleared, come behind all others.
+constexpr int kTileGroup = 32;
+inline int expert_group(int tiles) { return tiles >= 8 * kTileGroup ? kTileGroup : tiles >= 8 ? (tiles + 7) / 8 : 1; }
+// Blocks that the mapping below may need: every tile, and one round of groups.
+inline unsigned expert_blocks(int tiles) { return static_cast<unsigned>((tiles + 7) / 8 * 8 + 8 * expert_group(tiles) + 8); }
+
+// Slot j of XCD x -> index below `n`, or -1; `used` slots per XCD serve the n.
+__device__ __forceinline__ int expert_slot(int n, int x, int j, int& used) {
+  const int g = n >= 8 * kTileGroup ? kTileGroup : n >= 8 ? (n + 7) / 8 : 1;
+  const int groups = (n + g - 1) / g;
+  used = (groups + 7) / 8 * g;
+  const int q = j / g;
+  const int v = (q * 8 + x) * g + (j - q * g);
+  return j < used && v < n ? v : -1;
+}
+
+template <int BM>
+__device__ __forceinline__ bool expert_tile(const ExpertGemmArgs& a, int& e, int& bm, int& bn) {
+  const int x = blockIdx.x % 8, j = blockIdx.x / 8;
+  const int E = a.E;
+  int used;
+  if (a.k_is_rows || !a.counts) {
+    const int t = expert_slot(a.tiles, x, j, used);
+    if (t < 0) return false;
+    e = t / (a.tm * a.tn);
+    const int r = t - e * a.tm * a.tn;
+    bn = r / a.tm;
+    bm = r - bn * a.tm;
+    return true;
+  }
+  // m tiles with rows in use, summed over the experts; each wave does this for itself
+  const int lane = lane_id();
+  auto tiles_of = [&](int i) { return i < E ? (expert_count(a.counts, i, a.C) + BM - 1) / BM : 0; };
+  int total = 0;
+  for (int e0 = 0; e0 < E; e0 += kWave) total += tiles_of(e0 + lane);
+  total = __builtin_amdgcn_readfirstlane(group_reduce<kWave>(total, OpAdd()));
+  const int nv = total * a.tn;
+  int want = expert_slot(nv, x, j, used);
+  const bool empty = want < 0;
+  if (empty) {
+    want = (j - used) * 8 + x;
+    if (j < used || want >= a.tiles - nv) return false;
+  }
+  int before = 0;
+  for (int e0 = 0; e0 < E; e0 += kWave) {
+    const int mine = e0 + lane < E ? (empty ? a.tm - tiles_of(e0 + lane) : tiles_of(e0 + lane)) : 0;
+    int sum = mine;
+#pragma unroll
+    for (int s = 1; s < kWave; s <<= 1) {
+      const int up = __shfl_up(sum, s);
+      sum += lane >= s ? up : 0;
+    }
+    const uint64_t past = __ballot((before + sum) * a.tn > want);
+    if (past) {
+      const int l = __builtin_ctzll(past);
+      const int mt = __builtin_amdgcn_readlane(mine, l);
+      const int r = want - (before + __builtin_amdgcn_readlane(sum, l) - mt) * a.tn;
+      e = e0 + l;
+      bn = r / mt;
+      bm = r - bn * mt + (empty ? a.tm - mt : 0);
+      return true;
+    }
+    before += __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  return false;
 }
 
 }  // namespace hetumoe

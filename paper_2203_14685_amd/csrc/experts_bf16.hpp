@@ -68,7 +68,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   __shared__ __align__(1024) bf16_t A0[BM * kEBK], B0[BN * kEBK], A1[BM * kEBK], B1[BN * kEBK];
 
   int e, bm, bn;
-  if (!expert_tile(a.tiles, a.tm, a.tn, e, bm, bn)) return;
+  if (!expert_tile<BM>(a, e, bm, bn)) return;
   const int lane = lane_id(), g = lane / 16, m = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave / WN, wn = wave % WN;

@@ -8,6 +8,7 @@ namespace hetumoe {
 // What every product of the pass shares; tm, tn and tiles are left to the tile choice.
 inline ExpertGemmArgs expert_base_args(const ExpertArgs& x) {
   ExpertGemmArgs a{};
+  a.E = x.E;
   a.C = x.C;
   a.counts = x.counts;
   a.act = x.act;
@@ -19,9 +20,6 @@ inline void expert_set_tiles(ExpertGemmArgs& a, int E, int BM, int BNO) {
   a.tn = (a.N + BNO - 1) / BNO;
   a.tiles = E * a.tm * a.tn;
 }
-
-// Grid: a multiple of 8 (one contiguous piece of the tiles per XCD).
-inline dim3 expert_grid(const ExpertGemmArgs& a) { return dim3(static_cast<unsigned>((a.tiles + 7) / 8 * 8)); }
 
 // a.N: columns of hidden
 hipError_t expert_act_bf16(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st);

@@ -23,7 +23,7 @@ template <class TL, int KA, int KB, int EPI, bool GATED>
 static hipError_t launch_tile_f32(const ExpertArgs& x, ExpertGemmArgs a, hipStream_t st) {
   expert_set_tiles(a, x.E, TL::bm, EPI == kEpiAct && GATED ? TL::bn / 2 : TL::bn);
   experts_gemm_f32_kernel<TL::bm, TL::bn, TL::wm, TL::wn, KA, KB, EPI, GATED>
-      <<<expert_grid(a), dim3(TL::wm * TL::wn * kWave), 0, st>>>(a);
+      <<<dim3(expert_blocks(a.tiles)), dim3(TL::wm * TL::wn * kWave), 0, st>>>(a);
   return hipGetLastError();
 }
 

@@ -235,7 +235,7 @@ hipError_t run_base_auction_async(const BaseArgs& a, int launch_rounds, BaseDevS
 
 // Expert networks (step 4 of Algorithm 1): one batched product (experts.hpp).
 struct ExpertGemmArgs {
-  int C;                    // slots per expert
+  int E, C;                 // experts, slots of each
   int M, N, K;              // of the product; N: columns of out (gated forward: of hidden)
   int k_is_rows;            // K is the expert's rows in use (weight gradients), else M is cut at them
   int tm, tn, tiles;        // blocks along M and N, all blocks
