@@ -58,19 +58,23 @@ __device__ __forceinline__ void expert_stage_barrier() {
 }
 
 // ---------------------------------------------------------------- operands
-// K elements per stage: 128 bytes of a row that runs along K.
-template <class T> constexpr int kExpertBk = 128 / static_cast<int>(sizeof(T));
+// Bytes of a row that runs along K in one stage, and its K elements.
+template <class T> constexpr int kExpertRow = sizeof(T) == 2 ? 64 : 128;
+template <class T> constexpr int kExpertBk = kExpertRow<T> / static_cast<int>(sizeof(T));
 // Elements of a 16-byte piece.
 template <class T> constexpr int kExpertPe = 16 / static_cast<int>(sizeof(T));
 
 // Which 16-byte piece of its row lies at place `c` of LDS row `row`: piece c ^ swz.
-//   kRows: 8 pieces per 128-byte row; two rows fill the 64 banks.  A fragment read takes
-//          rows r .. r + 15 or, of the right operand in fp32, 4 i + t, i = 0..15.
+//   kRows: bf16: 4 pieces per 64-byte row, four rows fill the 64 banks; fp32: 8 pieces per 128
+//          bytes.  A fragment read takes rows r .. r + 15 or, of the right operand in
+//          fp32, 4 i + t, i = 0..15; sixteen lanes at a time, of which half are rows 0-3 and
+//          12-15 (or 4-11) of one g and half the other rows of the next g.
 //   kCols: bf16: a transpose read takes k rows 8 g + 4 h + 0..3, g = 0..3, of each 32
 //          contiguous bytes; fp32 reads run along a row and need no other order.
 template <class T, int KIND, bool RIGHT, int W>
 __device__ __forceinline__ int expert_swz(int row) {
-  if constexpr (KIND == kRows) return (RIGHT && sizeof(T) == 4 ? row >> 2 : row >> 1) & 7;
+  if constexpr (KIND == kRows && sizeof(T) == 2) return ((row >> 2) ^ (row >> 1)) & 3;
+  else if constexpr (KIND == kRows) return (RIGHT ? row >> 2 : row >> 1) & 7;
   else if constexpr (sizeof(T) == 4) return 0;
   else if constexpr (W >= 128) return ((row & 3) << 1) | (row & 8);
   else return (((row >> 1) & 1) << 1) | ((row & 8) >> 1);
@@ -88,41 +92,35 @@ __device__ __forceinline__ V expert_opaque(V v) {
 template <class T, int KIND, bool RIGHT, int W, int WAVES>
 struct ExpertOperand {
   static constexpr int kBk = kExpertBk<T>, kPe = kExpertPe<T>, kElt = static_cast<int>(sizeof(T));
-  static constexpr int kBytes = W * 128;
+  static constexpr int kBytes = W * kExpertRow<T>;
   static constexpr int N = kBytes / 1024 / WAVES;  // loads per wave and stage
   static_assert(N * WAVES * 1024 == kBytes, "whole loads");
-  static constexpr int P = KIND == kRows ? 8 : W / kPe;  // pieces per LDS row
+  static constexpr int P = KIND == kRows ? kExpertRow<T> / 16 : W / kPe;  // pieces per LDS row
   static constexpr int R = 64 / P;                       // rows per load
   // a lane's rows are R * WAVES apart: where that changes the order of the pieces, two offsets in turn
   static constexpr int kAlt = KIND == kCols && kElt == 2 && R * WAVES % 16 != 0 ? 2 : 1;
   static_assert(KIND == kCols || R * WAVES % 32 == 0, "one order of the pieces per lane");
-  const char* base;   // (first row or column, k = 0)
-  int64_t step;       // bytes per stage
-  int64_t limit;      // bytes behind base that may be read, less what the stages took
-  int cap;            // most that a stage's resource needs
-  unsigned off[kAlt], stride;
+  const char* base;   // (first row or column, k = 0), moved on by the stages
+  int rows;           // kRows: bytes behind base that may be read
+  int pitch;          // bytes per row of the matrix
+  unsigned off[kAlt];
   int kc;             // kRows: the lane's K element in a stage
 
   // map(piece) gives the column of the tile's piece, or -1 behind the matrix.
   template <class Map>
-  __device__ __forceinline__ void init(const T* p, int ld, int first, int valid, int K, int wave, Map map) {
-    const int lane = lane_id();
+  __device__ __forceinline__ void init(const T* p, int ld, int first, int valid, int wave, Map map) {
+    const int lane = expert_opaque(lane_id());
     const int row0 = wave * R + lane / P;
-    stride = static_cast<unsigned>(R * WAVES) * static_cast<unsigned>(ld) * kElt;
-    kc = 0;
+    pitch = ld * kElt;
+    kc = rows = 0;
     if constexpr (KIND == kRows) {
       base = reinterpret_cast<const char*>(p + static_cast<int64_t>(first) * ld);
-      step = 128;
-      limit = static_cast<int64_t>(valid) * ld * kElt;
-      cap = 0x7fffff00;
-      const int piece = (lane % 8) ^ expert_swz<T, KIND, RIGHT, W>(row0);
+      rows = max(0, valid) * pitch;
+      const int piece = (lane % P) ^ expert_swz<T, KIND, RIGHT, W>(row0);
       kc = piece * kPe;
       off[0] = static_cast<unsigned>(row0 * ld * kElt + piece * 16);
     } else {
       base = reinterpret_cast<const char*>(p);
-      step = static_cast<int64_t>(kBk) * ld * kElt;
-      limit = static_cast<int64_t>(K) * ld * kElt;
-      cap = kBk * ld * kElt;
 #pragma unroll
       for (int i = 0; i < kAlt; ++i) {
         const int col = map((lane % P) ^ expert_swz<T, KIND, RIGHT, W>(row0 + i * R * WAVES));
@@ -130,10 +128,12 @@ struct ExpertOperand {
       }
     }
   }
-  // The stage `base` points at; `left` K elements remain.  An offset past the resource
+  // The stage `base` points at; `left` K elements remain (none: zeros).  An offset past the resource
   // stays past it (below 2^32) with the rows' strides added.
   __device__ __forceinline__ void load(T* lds, int wave, int left) {
-    const __amdgpu_buffer_rsrc_t r = expert_rsrc(base, static_cast<int>(min(limit, static_cast<int64_t>(cap))));
+    const __amdgpu_buffer_rsrc_t r = expert_rsrc(
+        base, __builtin_amdgcn_readfirstlane(KIND == kRows ? max(rows, 0) : max(0, min(left, kBk)) * pitch));
+    const unsigned stride = static_cast<unsigned>(R * WAVES) * static_cast<unsigned>(pitch);
     unsigned o[kAlt];
 #pragma unroll
     for (int i = 0; i < kAlt; ++i) {
@@ -143,8 +143,8 @@ struct ExpertOperand {
 #pragma unroll
     for (int i = 0; i < N; ++i)
       expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, static_cast<int>(o[i % kAlt] + i * stride));
-    base += step;
-    limit -= step;
+    base += KIND == kRows ? kExpertRow<T> : kBk * pitch;
+    if constexpr (KIND == kRows) rows -= kExpertRow<T>;
   }
 };
 
@@ -195,76 +195,100 @@ __device__ __forceinline__ int expert_count(const int32_t* counts, int e, int C)
   return counts ? max(0, min(counts[e], C)) : C;
 }
 
-// Block -> (expert, m tile, n tile).  Blocks go round the 8 XCDs in turn.  Groups of
-// neighbouring tiles (an expert's m tiles first: they share its weights, and a few n
-// tiles its rows) go to one XCD, whose L2 then serves them, the groups round the XCDs
-// in order, so that experts of any load spread evenly (64 experts of uneven load, one
-// contiguous piece of the tiles per XCD: CUs busy 62 % of the time).  Tiles without rows in
-// use, which are only cleared, come behind all others.
+// ---------------------------------------------------------------- tiles
+// A block takes one tile after another, those of its XCD (blocks go round the 8 XCDs in
+// turn).  Groups of neighbouring tiles (an expert's m tiles first: they share its
+// weights, and a few n tiles its rows) go to one XCD, whose L2 then serves them, the
+// groups round the XCDs in order, so that experts of any load spread evenly (64 experts of
+// uneven load, one contiguous piece of the tiles per XCD: CUs busy 62 % of the time).
+// Tiles without rows in use, which are only cleared, come behind all others.
 constexpr int kTileGroup = 32;
-inline int expert_group(int tiles) { return tiles >= 8 * kTileGroup ? kTileGroup : tiles >= 8 ? (tiles + 7) / 8 : 1; }
-// Blocks that the mapping below may need: every tile, and one round of groups.
-inline unsigned expert_blocks(int tiles) { return static_cast<unsigned>((tiles + 7) / 8 * 8 + 8 * expert_group(tiles) + 8); }
+constexpr int kMaxExperts = 1024;
 
-// Slot j of XCD x -> index below `n`, or -1; `used` slots per XCD serve the n.
-__device__ __forceinline__ int expert_slot(int n, int x, int j, int& used) {
-  const int g = n >= 8 * kTileGroup ? kTileGroup : n >= 8 ? (n + 7) / 8 : 1;
-  const int groups = (n + g - 1) / g;
-  used = (groups + 7) / 8 * g;
-  const int q = j / g;
-  const int v = (q * 8 + x) * g + (j - q * g);
-  return j < used && v < n ? v : -1;
-}
+struct ExpertTile {
+  int e, bm, bn;
+};
 
 template <int BM>
-__device__ __forceinline__ bool expert_tile(const ExpertGemmArgs& a, int& e, int& bm, int& bn) {
-  const int x = blockIdx.x % 8, j = blockIdx.x / 8;
-  const int E = a.E;
-  int used;
-  if (a.k_is_rows || !a.counts) {
-    const int t = expert_slot(a.tiles, x, j, used);
-    if (t < 0) return false;
-    e = t / (a.tm * a.tn);
-    const int r = t - e * a.tm * a.tn;
-    bn = r / a.tm;
-    bm = r - bn * a.tm;
-    return true;
-  }
-  // m tiles with rows in use, summed over the experts; each wave does this for itself
-  const int lane = lane_id();
-  auto tiles_of = [&](int i) { return i < E ? (expert_count(a.counts, i, a.C) + BM - 1) / BM : 0; };
-  int total = 0;
-  for (int e0 = 0; e0 < E; e0 += kWave) total += tiles_of(e0 + lane);
-  total = __builtin_amdgcn_readfirstlane(group_reduce<kWave>(total, OpAdd()));
-  const int nv = total * a.tn;
-  int want = expert_slot(nv, x, j, used);
-  const bool empty = want < 0;
-  if (empty) {
-    want = (j - used) * 8 + x;
-    if (j < used || want >= a.tiles - nv) return false;
-  }
-  int before = 0;
-  for (int e0 = 0; e0 < E; e0 += kWave) {
-    const int mine = e0 + lane < E ? (empty ? a.tm - tiles_of(e0 + lane) : tiles_of(e0 + lane)) : 0;
-    int sum = mine;
+struct ExpertTiles {
+  int nv;    // tiles with work
+  int used;  // slots per XCD that serve them
+  int g;     // tiles per group
+  int* before;  // LDS [E]: m tiles with work up to and with each expert (where counts cut M)
+  int* rows;    // LDS [E]: rows in use
+
+  // The whole block calls this; one barrier.
+  __device__ __forceinline__ void init(const ExpertGemmArgs& a, int* before_, int* rows_) {
+    before = before_;
+    rows = rows_;
+    const int lane = lane_id();
+    int total = 0;
+    if (threadIdx.x < kWave) {
+      for (int e0 = 0; e0 < a.E; e0 += kWave) {
+        const int e = e0 + lane;
+        const int n = e < a.E ? expert_count(a.counts, e, a.C) : 0;
+        int sum = a.k_is_rows ? (e < a.E ? a.tm : 0) : (n + BM - 1) / BM;
 #pragma unroll
-    for (int s = 1; s < kWave; s <<= 1) {
-      const int up = __shfl_up(sum, s);
-      sum += lane >= s ? up : 0;
+        for (int s = 1; s < kWave; s <<= 1) {
+          const int up = __shfl_up(sum, s);
+          sum += lane >= s ? up : 0;
+        }
+        if (e < a.E) {
+          before[e] = total + sum;
+          rows[e] = n;
+        }
+        total += __builtin_amdgcn_readlane(sum, kWave - 1);
+      }
     }
-    const uint64_t past = __ballot((before + sum) * a.tn > want);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      const int mt = __builtin_amdgcn_readlane(mine, l);
-      const int r = want - (before + __builtin_amdgcn_readlane(sum, l) - mt) * a.tn;
-      e = e0 + l;
-      bn = r / mt;
-      bm = r - bn * mt + (empty ? a.tm - mt : 0);
-      return true;
-    }
-    before += __builtin_amdgcn_readlane(sum, kWave - 1);
+    __syncthreads();
+    nv = __builtin_amdgcn_readfirstlane(before[a.E - 1]) * a.tn;
+    g = nv >= 8 * kTileGroup ? kTileGroup : nv >= 8 ? (nv + 7) / 8 : 1;
+    used = ((nv + g - 1) / g + 7) / 8 * g;
   }
-  return false;
+
+  // The next slot from `j` on, by `step`, of XCD x that holds a tile with work (j is moved
+  // to it); false behind the last one.
+  __device__ __forceinline__ bool work(const ExpertGemmArgs& a, int x, int step, int& j, ExpertTile& t) const {
+    for (; j < used; j += step) {
+      const int q = j / g;
+      const int v = (q * 8 + x) * g + (j - q * g);
+      if (v < nv) return find(a, v, false, t);
+    }
+    return false;
+  }
+  // Tile `i` of those without work.
+  __device__ __forceinline__ bool clear(const ExpertGemmArgs& a, int i, ExpertTile& t) const {
+    return i < a.tiles - nv && find(a, i, true, t);
+  }
+
+  __device__ __forceinline__ bool find(const ExpertGemmArgs& a, int want, bool empty, ExpertTile& t) const {
+    const int lane = lane_id();
+    for (int e0 = 0; e0 < a.E; e0 += kWave) {
+      const int i = min(e0 + lane, a.E - 1);
+      // tiles along M up to and with expert i
+      const int upto = empty ? (i + 1) * a.tm - before[i] : before[i];
+      const uint64_t past = __ballot(e0 + lane < a.E && upto * a.tn > want);
+      if (past) {
+        const int e = e0 + __builtin_ctzll(past);
+        const int last = __builtin_amdgcn_readfirstlane(before[e]);
+        const int first = e > 0 ? __builtin_amdgcn_readfirstlane(before[e - 1]) : 0;
+        const int mt = empty ? a.tm - (last - first) : last - first;
+        const int r = want - (empty ? e * a.tm - first : first) * a.tn;
+        const int bn = r / mt;
+        t.e = __builtin_amdgcn_readfirstlane(e);
+        t.bn = __builtin_amdgcn_readfirstlane(bn);
+        t.bm = __builtin_amdgcn_readfirstlane(r - bn * mt + (empty ? a.tm - mt : 0));
+        return true;
+      }
+    }
+    return false;
+  }
+};
+
+// Blocks: at most `resident`, a multiple of 8.
+inline unsigned expert_blocks(int tiles, int resident) {
+  const int need = (tiles + 7) / 8 * 8;
+  return static_cast<unsigned>(need < resident ? need : (resident + 7) / 8 * 8);
 }
 
 }  // namespace hetumoe

@@ -1,18 +1,19 @@
 // Batched bf16 products of the expert networks on v_mfma_f32_16x16x32_bf16.
 //
 // A block forms BM x BN of one expert's product, WM x WN waves, 64 columns each.
-// Per stage of 64 K elements both operands go straight from memory to LDS as
-// they lie there (16 bytes per lane, no registers), two stages in turn.  Operands
+// Per stage of 32 K elements both operands go straight from memory to LDS as
+// they lie there (16 bytes per lane, no registers), four stages in turn.  Operands
 // whose rows run along K are read as 16-byte fragments, the others through LDS
 // transpose reads.  16-byte pieces are placed by an exclusive-or with bits of
 // their row, so that the 16 lanes of a fragment read touch different banks; since
 // a load to LDS fills it in lane order, the lane fetches the piece that belongs
 // where it writes.
 //
-// While one half of a stage (32 K) is multiplied the fragments of the next half are
-// read, so the reads' latency and the one barrier per stage lie behind products; the
-// stage after next is requested as soon as every wave has read the last half of
-// the stage in its place.
+// While one stage is multiplied the fragments of the next one are read, so the reads'
+// latency and the barrier per stage lie behind products; the fourth stage ahead is
+// requested as soon as every wave has read the one in its place.  Towards the end of a
+// tile those are the next tile's, so that its first loads lie behind the products and the
+// stores of this one.
 //
 // The product is formed transposed (columns n are the rows of the matrix unit), so a lane
 // holds 4 neighbouring columns of one row; a swap with the neighbouring 16 lanes over a
@@ -28,27 +29,27 @@ namespace hetumoe {
 
 constexpr int kEBK = kExpertBk<bf16_t>;
 
-// Fragments: of K step ks (32 elements) lane (g, m) gets K 8 g .. 8 g + 7 of row (or
-// column) x0 + 16 i + m, i = 0 .. MT - 1, x0 a multiple of 16 MT.
+// Fragments: lane (g, m) gets K 8 g .. 8 g + 7 of the stage's 32 of row (or column)
+// x0 + 16 i + m, i = 0 .. MT - 1, x0 a multiple of 16 MT.
 template <int KIND, bool RIGHT, int W, int MT>
 struct ExpertFrag {
-  unsigned at;  // byte of (i = 0, ks = 0)
+  unsigned at;  // byte of i = 0
   __device__ __forceinline__ void init(int x0, int g, int m) {
     if constexpr (KIND == kRows) {
-      at = (x0 + m) * 128 + ((g ^ expert_swz<bf16_t, KIND, RIGHT, W>(m)) * 16);
+      at = (x0 + m) * 64 + ((g ^ expert_swz<bf16_t, KIND, RIGHT, W>(m)) * 16);
     } else {
       const int row = 8 * g + m / 4;
       at = row * W * 2 + (((x0 / 8 + m % 4 / 2) ^ expert_swz<bf16_t, KIND, RIGHT, W>(row)) * 16) + m % 2 * 8;
     }
   }
-  // kRows: tiles are 16 rows apart, the steps' pieces differ in bit 2 of their place.
-  // kCols: a tile is 32 bytes, bits that are free of carries; rows 4 and 32 on keep their order.
-  __device__ __forceinline__ u32x4 read(const bf16_t* lds, unsigned from, int ks, int i) const {
+  // kRows: tiles are 16 rows apart.  kCols: a tile is 32 bytes, bits that are free of
+  // carries; the row 4 on keeps the order.
+  __device__ __forceinline__ u32x4 read(const bf16_t* lds, unsigned from, int i) const {
     const char* p = reinterpret_cast<const char*>(lds);
     if constexpr (KIND == kRows) {
-      return *reinterpret_cast<const u32x4*>(p + (from ^ (ks * 64)) + i * 2048);
+      return *reinterpret_cast<const u32x4*>(p + from + i * 1024);
     } else {
-      const char* q = p + (from ^ (i * 32)) + ks * 64 * W;
+      const char* q = p + (from ^ (i * 32));
       const uint2 lo = expert_tr16(reinterpret_cast<const bf16_t*>(q));
       const uint2 hi = expert_tr16(reinterpret_cast<const bf16_t*>(q + 8 * W));
       return u32x4{lo.x, lo.y, hi.x, hi.y};
@@ -65,31 +66,33 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
   constexpr bool kSplit = EPI == kEpiAct && GATED;
   constexpr int BNO = kSplit ? BN / 2 : BN;
-  __shared__ __align__(1024) bf16_t A0[BM * kEBK], B0[BN * kEBK], A1[BM * kEBK], B1[BN * kEBK];
+  __shared__ __align__(1024) bf16_t A0[BM * kEBK], A1[BM * kEBK], A2[BM * kEBK], A3[BM * kEBK];
+  __shared__ __align__(1024) bf16_t B0[BN * kEBK], B1[BN * kEBK], B2[BN * kEBK], B3[BN * kEBK];
+  __shared__ int tile_before[kMaxExperts], tile_rows[kMaxExperts];
 
-  int e, bm, bn;
-  if (!expert_tile<BM>(a, e, bm, bn)) return;
   const int lane = lane_id(), g = lane / 16, m = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave / WN, wn = wave % WN;
-  const int cnt = expert_count(a.counts, e, a.C);
-  const int K = a.k_is_rows ? cnt : a.K;
-  const int rows = a.k_is_rows ? a.M : cnt;  // rows of the output that are sums
-  const int m0 = bm * BM, n0 = bn * BNO;
-  const int mvalid = max(0, min(BM, rows - m0));
+  const int xcd = blockIdx.x % 8, step = gridDim.x / 8;
+  int slot = blockIdx.x / 8;
+  ExpertTiles<BM> tiles;
+  tiles.init(a, tile_before, tile_rows);
 
-  f32x4 acc[MT][NT];
-#pragma unroll
-  for (int i = 0; i < MT; ++i)
-#pragma unroll
-    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-
-  if (mvalid > 0 && K > 0) {
-    ExpertOperand<bf16_t, KA, false, BM, WAVES> oa;
-    ExpertOperand<bf16_t, KB, true, BN, WAVES> ob;
-    oa.init(reinterpret_cast<const bf16_t*>(a.A) + e * a.sA, a.lda, m0, mvalid, K, wave,
+  ExpertOperand<bf16_t, KA, false, BM, WAVES> oa;
+  ExpertOperand<bf16_t, KB, true, BN, WAVES> ob;
+  int left = 0;  // K elements of the loads' tile from the next stage on
+  // Points the loads at tile t (none: zeros).
+  auto aim = [&](bool any, ExpertTile t) {
+    // known to be the same on all lanes: the resources then stay in scalar registers
+    t.e = __builtin_amdgcn_readfirstlane(t.e);
+    t.bm = __builtin_amdgcn_readfirstlane(t.bm);
+    t.bn = __builtin_amdgcn_readfirstlane(t.bn);
+    const int n = any ? __builtin_amdgcn_readfirstlane(tile_rows[t.e]) : 0;
+    const int m0 = t.bm * BM, n0 = t.bn * BNO;
+    const int K = a.k_is_rows ? n : any ? a.K : 0;
+    oa.init(reinterpret_cast<const bf16_t*>(a.A) + t.e * a.sA, a.lda, m0, a.k_is_rows ? BM : min(BM, n - m0), wave,
             [&](int piece) { return m0 + piece * 8 < a.M ? m0 + piece * 8 : -1; });
-    ob.init(reinterpret_cast<const bf16_t*>(a.B) + e * a.sB, a.ldb, n0, min(BN, a.N - n0), K, wave, [&](int piece) {
+    ob.init(reinterpret_cast<const bf16_t*>(a.B) + t.e * a.sB, a.ldb, n0, min(BN, a.N - n0), wave, [&](int piece) {
       if constexpr (kSplit) {
         // pieces 0..3 of each wave's 8 are the gate's
         const int c = n0 + (piece / 8) * 32 + (piece % 4) * 8;
@@ -98,59 +101,88 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         return n0 + piece * 8 < a.N ? n0 + piece * 8 : -1;
       }
     });
-    ExpertFrag<KA, false, BM, MT> ra;
-    ExpertFrag<KB, true, BN, NT> rb;
-    ra.init(wm * MT * 16, g, m);
-    rb.init(wn * NT * 16, g, m);
-    constexpr int kLoads = ExpertOperand<bf16_t, KA, false, BM, WAVES>::N + ExpertOperand<bf16_t, KB, true, BN, WAVES>::N;
-    u32x4 fa[MT], fb[NT], fn[NT];
-    // Products of the half stage in fa and fb; each left fragment makes room for the one of
-    // the next half, step ks of (As, Bs), as soon as it is used.
-    auto half = [&](u32x4 (&cur)[NT], u32x4 (&next)[NT], const bf16_t* As, const bf16_t* Bs, int ks) {
-      const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
+    left = __builtin_amdgcn_readfirstlane(K);
+  };
+  ExpertFrag<KA, false, BM, MT> ra;
+  ExpertFrag<KB, true, BN, NT> rb;
+  ra.init(wm * MT * 16, g, m);
+  rb.init(wn * NT * 16, g, m);
+  constexpr int kLoads = ExpertOperand<bf16_t, KA, false, BM, WAVES>::N + ExpertOperand<bf16_t, KB, true, BN, WAVES>::N;
+  f32x4 acc[MT][NT];
+  u32x4 fa[MT], fb[NT], fn[NT];
+  auto load = [&](bf16_t* As, bf16_t* Bs) {
+    oa.load(As, wave, left);
+    ob.load(Bs, wave, left);
+    left -= kEBK;
+  };
+  // Products of the stage in fa and cur.  Behind the barrier the next stage, (An, Bn), is in
+  // LDS, and the stage's own place, (As, Bs), is free for the fourth one ahead.  Each left
+  // fragment makes room for the next stage's as soon as it is used (READ; the registers of
+  // a tile's last fragments serve its epilogue).
+  auto stage = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], bf16_t* As, bf16_t* Bs, const bf16_t* An,
+                   const bf16_t* Bn) {
+    constexpr bool READ = decltype(read)::v;
+    expert_stage_barrier<2 * kLoads>();
+    load(As, Bs);
+    const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
+    if constexpr (READ) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) next[j] = rb.read(Bs, at_b, ks, j);
-#pragma unroll
-      for (int i = 0; i < MT; ++i) {
-#pragma unroll
-        for (int j = 0; j < NT; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, cur[j]),
-                                                              __builtin_bit_cast(bf16x8, fa[i]), acc[i][j], 0, 0, 0);
-        fa[i] = ra.read(As, at_a, ks, i);
-      }
-    };
-    // One stage in (As, Bs), its first half in fa and fb; `left` K elements from its
-    // start.  Leaves the first half of the next stage, (An, Bn), there (after the last
-    // stage: what that buffer holds, unused).
-    auto stage = [&](bf16_t* As, bf16_t* Bs, bf16_t* An, bf16_t* Bn, int left) {
-      half(fb, fn, As, Bs, 1);
-      expert_stage_barrier();
-      if (left > 2 * kEBK) {
-        oa.load(As, wave, left - 2 * kEBK);
-        ob.load(Bs, wave, left - 2 * kEBK);
-      }
-      half(fn, fb, An, Bn, 0);
-    };
-    oa.load(A0, wave, K);
-    ob.load(B0, wave, K);
-    if (K > kEBK) {
-      oa.load(A1, wave, K - kEBK);
-      ob.load(B1, wave, K - kEBK);
-      expert_stage_barrier<kLoads>();
-    } else {
-      expert_stage_barrier();
+      for (int j = 0; j < NT; ++j) next[j] = rb.read(Bn, at_b, j);
     }
 #pragma unroll
-    for (int j = 0; j < NT; ++j) fb[j] = rb.read(B0, rb.at, 0, j);
+    for (int i = 0; i < MT; ++i) {
 #pragma unroll
-    for (int i = 0; i < MT; ++i) fa[i] = ra.read(A0, ra.at, 0, i);
-    int left = K;
-    for (; left > kEBK; left -= 2 * kEBK) {
-      stage(A0, B0, A1, B1, left);
-      stage(A1, B1, A0, B0, left - kEBK);
+      for (int j = 0; j < NT; ++j)
+        asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc[i][j]) : "v"(cur[j]), "v"(fa[i]));
+      if constexpr (READ) fa[i] = ra.read(An, at_a, i);
     }
-    if (left > 0) stage(A0, B0, A1, B1, left);
+  };
+  auto four_stages = [&](auto read_last) {
+    stage(ExpertInt<1>(), fb, fn, A0, B0, A1, B1);
+    stage(ExpertInt<1>(), fn, fb, A1, B1, A2, B2);
+    stage(ExpertInt<1>(), fb, fn, A2, B2, A3, B3);
+    stage(read_last, fn, fb, A3, B3, A0, B0);
+  };
+
+  ExpertTile at{0, 0, 0}, next{0, 0, 0};
+  bool work = __builtin_amdgcn_readfirstlane(tiles.work(a, xcd, step, slot, at)) != 0;
+  if (work) {
+    aim(true, at);
+    load(A0, B0);
+    load(A1, B1);
+    load(A2, B2);
+    load(A3, B3);
+    expert_stage_barrier<3 * kLoads>();
   }
+  // the tiles without work that this block clears
+  int idle = blockIdx.x;
+  if (!work && !tiles.clear(a, idle, at)) return;
+  for (;;) {
+  bool more = false;
+#pragma unroll
+  for (int i = 0; i < MT; ++i)
+#pragma unroll
+    for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (work) {
+    // the first four stages of the next tile are on their way before this one's results
+    // are stored; behind the last tile: zeros, so that the count of loads stays the same
+    const int K = a.k_is_rows ? __builtin_amdgcn_readfirstlane(tile_rows[at.e]) : a.K;
+    slot += step;
+    more = __builtin_amdgcn_readfirstlane(tiles.work(a, xcd, step, slot, next)) != 0;
+    slot = __builtin_amdgcn_readfirstlane(slot);
+    const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
+#pragma unroll
+    for (int j = 0; j < NT; ++j) fb[j] = rb.read(B0, at_b, j);
+#pragma unroll
+    for (int i = 0; i < MT; ++i) fa[i] = ra.read(A0, at_a, i);
+    for (int k = 4 * kEBK; k < K; k += 4 * kEBK) four_stages(ExpertInt<1>());
+    aim(more, next);
+    four_stages(ExpertInt<0>());
+    asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
+  }
+  const int e = at.e, bm = at.bm;
+  const int m0 = bm * BM, n0 = at.bn * BNO;
+  const int rows = a.k_is_rows ? a.M : work ? __builtin_amdgcn_readfirstlane(tile_rows[e]) : 0;
 
   // lane (g, m): row m of tile i, columns 4 g .. 4 g + 3 of each tile.  Odd groups of 16
   // lanes swap their first tile of a pair for the second one of the group before:
@@ -166,8 +198,9 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         acc[i][2 * p][q] = __uint_as_float(r[0]);
         acc[i][2 * p + 1][q] = __uint_as_float(r[1]);
       }
-  const int row0 = m0 + wm * MT * 16 + m;
-  const int col0 = n0 + (kSplit ? wn * 32 : wn * 64) + 16 * (g % 2) + 8 * (g / 2);
+  const int ln = expert_opaque(lane), lm = ln % 16, lg = ln / 16;
+  const int row0 = m0 + wm * MT * 16 + lm;
+  const int col0 = n0 + (kSplit ? wn * 32 : wn * 64) + 16 * (lg % 2) + 8 * (lg / 2);
   auto value = [&](int i, int p, int q) { return acc[i][2 * p + q / 4][q % 4]; };
   if constexpr (EPI == kEpiStore) {
     float bias[NP][8];
@@ -276,7 +309,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
             s0[q] = group_reduce<16>(s0[q], OpAdd());
             if constexpr (GATED) s1[q] = group_reduce<16>(s1[q], OpAdd());
           }
-          if (m == 0 && c < a.N) {
+          if (lm == 0 && c < a.N) {
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
               part[c + q] = s0[q];
@@ -286,6 +319,15 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         }
       }
     });
+  }
+  if (more) {
+    at = next;
+    continue;
+  }
+  if (work) expert_stage_barrier();  // nothing is on its way to LDS when the block ends
+  else idle += gridDim.x;
+  work = false;
+  if (!tiles.clear(a, idle, at)) return;
   }
 }
 

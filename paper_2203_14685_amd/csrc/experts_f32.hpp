@@ -57,12 +57,27 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_f32_kernel(ExpertGem
   constexpr int BNO = kSplit ? BN / 2 : BN;
   __shared__ __align__(1024) float A0[BM * kFBK], B0[BN * kFBK], A1[BM * kFBK], B1[BN * kFBK];
 
-  int e, bm, bn;
-  if (!expert_tile<BM>(a, e, bm, bn)) return;
+  __shared__ int tile_before[kMaxExperts], tile_rows[kMaxExperts];
+
   const int lane = lane_id(), g = lane / 16, m = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave / WN, wn = wave % WN;
-  const int cnt = expert_count(a.counts, e, a.C);
+  const int xcd = blockIdx.x % 8, step = gridDim.x / 8;
+  int slot = blockIdx.x / 8, idle = blockIdx.x;
+  ExpertTiles<BM> tiles;
+  tiles.init(a, tile_before, tile_rows);
+  for (;;) {
+  // the tiles with work, then those that are only cleared
+  ExpertTile at{0, 0, 0};
+  const bool work = tiles.work(a, xcd, step, slot, at);
+  if (work) {
+    slot += step;
+  } else {
+    if (!tiles.clear(a, idle, at)) return;
+    idle += gridDim.x;
+  }
+  const int e = at.e, bm = at.bm, bn = at.bn;
+  const int cnt = __builtin_amdgcn_readfirstlane(tile_rows[e]);
   const int K = a.k_is_rows ? cnt : a.K;
   const int rows = a.k_is_rows ? a.M : cnt;
   const int m0 = bm * BM, n0 = bn * BNO;
@@ -77,9 +92,9 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_f32_kernel(ExpertGem
   if (mvalid > 0 && K > 0) {
     ExpertOperand<float, KA, false, BM, WAVES> oa;
     ExpertOperand<float, KB, true, BN, WAVES> ob;
-    oa.init(reinterpret_cast<const float*>(a.A) + e * a.sA, a.lda, m0, mvalid, K, wave,
+    oa.init(reinterpret_cast<const float*>(a.A) + e * a.sA, a.lda, m0, mvalid, wave,
             [&](int piece) { return m0 + piece * 4 < a.M ? m0 + piece * 4 : -1; });
-    ob.init(reinterpret_cast<const float*>(a.B) + e * a.sB, a.ldb, n0, min(BN, a.N - n0), K, wave, [&](int piece) {
+    ob.init(reinterpret_cast<const float*>(a.B) + e * a.sB, a.ldb, n0, min(BN, a.N - n0), wave, [&](int piece) {
       if constexpr (kSplit) {
         // lane group g of a wave ends with pieces 4 g .. 4 g + 3 of its 16: two of
         // the gate, the same two of the other factor
@@ -115,6 +130,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_f32_kernel(ExpertGem
           acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     };
+    expert_stage_barrier();  // the tile before is read
     oa.load(A0, wave, K);
     ob.load(B0, wave, K);
     int stage = 0;
@@ -250,6 +266,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_f32_kernel(ExpertGem
         }
       }
     });
+  }
   }
 }
 

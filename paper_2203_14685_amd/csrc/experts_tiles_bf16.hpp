@@ -6,26 +6,27 @@
 
 namespace hetumoe {
 
-template <int BM, int BN, int WM, int WN>
+// PER: blocks that a CU holds.
+template <int BM, int BN, int WM, int WN, int PER>
 struct Tile {
-  static constexpr int bm = BM, bn = BN, wm = WM, wn = WN;
+  static constexpr int bm = BM, bn = BN, wm = WM, wn = WN, per_cu = PER;
 };
 
 template <class Fn>
 static hipError_t by_tile(const ExpertArgs& x, int M, int N, Fn fn) {
   // tiles of 256 x 256 once they fill the CUs, 64 x 256 where an expert has few
   // rows, else 128 x 128
-  if (M <= 64) return fn(Tile<64, 256, 1, 4>());
+  if (M <= 64) return fn(Tile<64, 256, 1, 4, 1>());
   const int64_t big = static_cast<int64_t>(x.E) * ((M + 255) / 256) * ((N + 255) / 256);
-  if (big >= 256) return fn(Tile<256, 256, 2, 4>());
-  return fn(Tile<128, 128, 2, 2>());
+  if (big >= 256) return fn(Tile<256, 256, 2, 4, 1>());
+  return fn(Tile<128, 128, 2, 2, 2>());
 }
 
 template <class TL, int KA, int KB, int EPI, bool GATED>
 static hipError_t launch_tile_bf16(const ExpertArgs& x, ExpertGemmArgs a, hipStream_t st) {
   expert_set_tiles(a, x.E, TL::bm, EPI == kEpiAct && GATED ? TL::bn / 2 : TL::bn);
   experts_gemm_bf16_kernel<TL::bm, TL::bn, TL::wm, TL::wn, KA, KB, EPI, GATED>
-      <<<dim3(expert_blocks(a.tiles)), dim3(TL::wm * TL::wn * kWave), 0, st>>>(a);
+      <<<dim3(expert_blocks(a.tiles, TL::per_cu * device_cu_count())), dim3(TL::wm * TL::wn * kWave), 0, st>>>(a);
   return hipGetLastError();
 }
 
