@@ -58,23 +58,22 @@ __device__ __forceinline__ void expert_stage_barrier() {
 }
 
 // ---------------------------------------------------------------- operands
-// Bytes of a row that runs along K in one stage, and its K elements.
-template <class T> constexpr int kExpertRow = sizeof(T) == 2 ? 64 : 128;
-template <class T> constexpr int kExpertBk = kExpertRow<T> / static_cast<int>(sizeof(T));
+// Bytes of a row that runs along K in one stage, a cache line (with 64 bytes and twice the
+// stages the L2's requests bound the products: dxe of 64 x 512 x 2048 x 8192 841 -> 958 us),
+// and its K elements.
+constexpr int kExpertRow = 128;
+template <class T> constexpr int kExpertBk = kExpertRow / static_cast<int>(sizeof(T));
 // Elements of a 16-byte piece.
 template <class T> constexpr int kExpertPe = 16 / static_cast<int>(sizeof(T));
 
 // Which 16-byte piece of its row lies at place `c` of LDS row `row`: piece c ^ swz.
-//   kRows: bf16: 4 pieces per 64-byte row, four rows fill the 64 banks; fp32: 8 pieces per 128
-//          bytes.  A fragment read takes rows r .. r + 15 or, of the right operand in
-//          fp32, 4 i + t, i = 0..15; sixteen lanes at a time, of which half are rows 0-3 and
-//          12-15 (or 4-11) of one g and half the other rows of the next g.
+//   kRows: 8 pieces per 128-byte row; two rows fill the 64 banks.  A fragment read takes rows
+//          r .. r + 15 or, of the right operand in fp32, 4 i + t, i = 0..15.
 //   kCols: bf16: a transpose read takes k rows 8 g + 4 h + 0..3, g = 0..3, of each 32
 //          contiguous bytes; fp32 reads run along a row and need no other order.
 template <class T, int KIND, bool RIGHT, int W>
 __device__ __forceinline__ int expert_swz(int row) {
-  if constexpr (KIND == kRows && sizeof(T) == 2) return ((row >> 2) ^ (row >> 1)) & 3;
-  else if constexpr (KIND == kRows) return (RIGHT ? row >> 2 : row >> 1) & 7;
+  if constexpr (KIND == kRows) return (RIGHT && sizeof(T) == 4 ? row >> 2 : row >> 1) & 7;
   else if constexpr (sizeof(T) == 4) return 0;
   else if constexpr (W >= 128) return ((row & 3) << 1) | (row & 8);
   else return (((row >> 1) & 1) << 1) | ((row & 8) >> 1);
@@ -92,10 +91,10 @@ __device__ __forceinline__ V expert_opaque(V v) {
 template <class T, int KIND, bool RIGHT, int W, int WAVES>
 struct ExpertOperand {
   static constexpr int kBk = kExpertBk<T>, kPe = kExpertPe<T>, kElt = static_cast<int>(sizeof(T));
-  static constexpr int kBytes = W * kExpertRow<T>;
+  static constexpr int kBytes = W * kExpertRow;
   static constexpr int N = kBytes / 1024 / WAVES;  // loads per wave and stage
   static_assert(N * WAVES * 1024 == kBytes, "whole loads");
-  static constexpr int P = KIND == kRows ? kExpertRow<T> / 16 : W / kPe;  // pieces per LDS row
+  static constexpr int P = KIND == kRows ? kExpertRow / 16 : W / kPe;  // pieces per LDS row
   static constexpr int R = 64 / P;                       // rows per load
   // a lane's rows are R * WAVES apart: where that changes the order of the pieces, two offsets in turn
   static constexpr int kAlt = KIND == kCols && kElt == 2 && R * WAVES % 16 != 0 ? 2 : 1;
@@ -143,8 +142,8 @@ struct ExpertOperand {
 #pragma unroll
     for (int i = 0; i < N; ++i)
       expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, static_cast<int>(o[i % kAlt] + i * stride));
-    base += KIND == kRows ? kExpertRow<T> : kBk * pitch;
-    if constexpr (KIND == kRows) rows -= kExpertRow<T>;
+    base += KIND == kRows ? kExpertRow : kBk * pitch;
+    if constexpr (KIND == kRows) rows -= kExpertRow;
   }
 };
 

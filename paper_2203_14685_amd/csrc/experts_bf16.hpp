@@ -1,19 +1,19 @@
 // Batched bf16 products of the expert networks on v_mfma_f32_16x16x32_bf16.
 //
 // A block forms BM x BN of one expert's product, WM x WN waves, 64 columns each.
-// Per stage of 32 K elements both operands go straight from memory to LDS as
-// they lie there (16 bytes per lane, no registers), four stages in turn.  Operands
+// Per stage of 64 K elements both operands go straight from memory to LDS as
+// they lie there (16 bytes per lane, no registers), two stages in turn.  Operands
 // whose rows run along K are read as 16-byte fragments, the others through LDS
 // transpose reads.  16-byte pieces are placed by an exclusive-or with bits of
 // their row, so that the 16 lanes of a fragment read touch different banks; since
 // a load to LDS fills it in lane order, the lane fetches the piece that belongs
 // where it writes.
 //
-// While one stage is multiplied the fragments of the next one are read, so the reads'
-// latency and the barrier per stage lie behind products; the fourth stage ahead is
-// requested as soon as every wave has read the one in its place.  Towards the end of a
-// tile those are the next tile's, so that its first loads lie behind the products and the
-// stores of this one.
+// While one half of a stage (32 K) is multiplied the fragments of the next half are
+// read, so the reads' latency and the barrier per stage lie behind products; the
+// stage after next is requested as soon as every wave has read the last half of the
+// stage in its place.  Towards the end of a tile those are the next tile's, so that its
+// first loads lie behind the products and the stores of this one.
 //
 // The product is formed transposed (columns n are the rows of the matrix unit), so a lane
 // holds 4 neighbouring columns of one row; a swap with the neighbouring 16 lanes over a
@@ -29,27 +29,27 @@ namespace hetumoe {
 
 constexpr int kEBK = kExpertBk<bf16_t>;
 
-// Fragments: lane (g, m) gets K 8 g .. 8 g + 7 of the stage's 32 of row (or column)
-// x0 + 16 i + m, i = 0 .. MT - 1, x0 a multiple of 16 MT.
+// Fragments: of step ks (32 K elements) lane (g, m) gets K 8 g .. 8 g + 7 of row (or
+// column) x0 + 16 i + m, i = 0 .. MT - 1, x0 a multiple of 16 MT.
 template <int KIND, bool RIGHT, int W, int MT>
 struct ExpertFrag {
-  unsigned at;  // byte of i = 0
+  unsigned at;  // byte of (i = 0, ks = 0)
   __device__ __forceinline__ void init(int x0, int g, int m) {
     if constexpr (KIND == kRows) {
-      at = (x0 + m) * 64 + ((g ^ expert_swz<bf16_t, KIND, RIGHT, W>(m)) * 16);
+      at = (x0 + m) * 128 + ((g ^ expert_swz<bf16_t, KIND, RIGHT, W>(m)) * 16);
     } else {
       const int row = 8 * g + m / 4;
       at = row * W * 2 + (((x0 / 8 + m % 4 / 2) ^ expert_swz<bf16_t, KIND, RIGHT, W>(row)) * 16) + m % 2 * 8;
     }
   }
-  // kRows: tiles are 16 rows apart.  kCols: a tile is 32 bytes, bits that are free of
-  // carries; the row 4 on keeps the order.
-  __device__ __forceinline__ u32x4 read(const bf16_t* lds, unsigned from, int i) const {
+  // kRows: tiles are 16 rows apart, the steps' pieces differ in bit 2 of their place.
+  // kCols: a tile is 32 bytes, bits that are free of carries; rows 4 and 32 on keep their order.
+  __device__ __forceinline__ u32x4 read(const bf16_t* lds, unsigned from, int ks, int i) const {
     const char* p = reinterpret_cast<const char*>(lds);
     if constexpr (KIND == kRows) {
-      return *reinterpret_cast<const u32x4*>(p + from + i * 1024);
+      return *reinterpret_cast<const u32x4*>(p + (from ^ (ks * 64)) + i * 2048);
     } else {
-      const char* q = p + (from ^ (i * 32));
+      const char* q = p + (from ^ (i * 32)) + ks * 64 * W;
       const uint2 lo = expert_tr16(reinterpret_cast<const bf16_t*>(q));
       const uint2 hi = expert_tr16(reinterpret_cast<const bf16_t*>(q + 8 * W));
       return u32x4{lo.x, lo.y, hi.x, hi.y};
@@ -66,8 +66,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
   constexpr bool kSplit = EPI == kEpiAct && GATED;
   constexpr int BNO = kSplit ? BN / 2 : BN;
-  __shared__ __align__(1024) bf16_t A0[BM * kEBK], A1[BM * kEBK], A2[BM * kEBK], A3[BM * kEBK];
-  __shared__ __align__(1024) bf16_t B0[BN * kEBK], B1[BN * kEBK], B2[BN * kEBK], B3[BN * kEBK];
+  __shared__ __align__(1024) bf16_t A0[BM * kEBK], A1[BM * kEBK], B0[BN * kEBK], B1[BN * kEBK];
   __shared__ int tile_before[kMaxExperts], tile_rows[kMaxExperts];
 
   const int lane = lane_id(), g = lane / 16, m = lane % 16;
@@ -115,33 +114,34 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     ob.load(Bs, wave, left);
     left -= kEBK;
   };
-  // Products of the stage in fa and cur.  Behind the barrier the next stage, (An, Bn), is in
-  // LDS, and the stage's own place, (As, Bs), is free for the fourth one ahead.  Each left
-  // fragment makes room for the next stage's as soon as it is used (READ; the registers of
-  // a tile's last fragments serve its epilogue).
-  auto stage = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], bf16_t* As, bf16_t* Bs, const bf16_t* An,
-                   const bf16_t* Bn) {
+  // Products of the half stage in fa and cur.  Each left fragment makes room for the one of
+  // the half after it, step ks of (As, Bs), as soon as it is used (READ; the registers of a
+  // tile's last fragments serve its epilogue).  The products are written out to tie
+  // each sum to its registers and the reads to their places: left to the compiler, sums
+  // and fragments moved between registers and scratch memory.  The two empty slots cover
+  // a move into an operand right before.
+  auto half = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], const bf16_t* As, const bf16_t* Bs, int ks) {
     constexpr bool READ = decltype(read)::v;
-    expert_stage_barrier<2 * kLoads>();
-    load(As, Bs);
     const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
     if constexpr (READ) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j) next[j] = rb.read(Bn, at_b, j);
+      for (int j = 0; j < NT; ++j) next[j] = rb.read(Bs, at_b, ks, j);
     }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
 #pragma unroll
       for (int j = 0; j < NT; ++j)
         asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc[i][j]) : "v"(cur[j]), "v"(fa[i]));
-      if constexpr (READ) fa[i] = ra.read(An, at_a, i);
+      if constexpr (READ) fa[i] = ra.read(As, at_a, ks, i);
     }
   };
-  auto four_stages = [&](auto read_last) {
-    stage(ExpertInt<1>(), fb, fn, A0, B0, A1, B1);
-    stage(ExpertInt<1>(), fn, fb, A1, B1, A2, B2);
-    stage(ExpertInt<1>(), fb, fn, A2, B2, A3, B3);
-    stage(read_last, fn, fb, A3, B3, A0, B0);
+  // The stage in (As, Bs), its first half in fa and fb.  Behind the barrier the next stage,
+  // (An, Bn), is in LDS, and this one's place is free for the one after it.
+  auto stage = [&](auto read_last, bf16_t* As, bf16_t* Bs, const bf16_t* An, const bf16_t* Bn) {
+    half(ExpertInt<1>(), fb, fn, As, Bs, 1);
+    expert_stage_barrier();
+    load(As, Bs);
+    half(read_last, fn, fb, An, Bn, 0);
   };
 
   ExpertTile at{0, 0, 0}, next{0, 0, 0};
@@ -150,9 +150,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     aim(true, at);
     load(A0, B0);
     load(A1, B1);
-    load(A2, B2);
-    load(A3, B3);
-    expert_stage_barrier<3 * kLoads>();
+    expert_stage_barrier<kLoads>();
   }
   // the tiles without work that this block clears
   int idle = blockIdx.x;
@@ -164,7 +162,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (work) {
-    // the first four stages of the next tile are on their way before this one's results
+    // the first two stages of the next tile are on their way before this one's results
     // are stored; behind the last tile: zeros, so that the count of loads stays the same
     const int K = a.k_is_rows ? __builtin_amdgcn_readfirstlane(tile_rows[at.e]) : a.K;
     slot += step;
@@ -172,12 +170,17 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     slot = __builtin_amdgcn_readfirstlane(slot);
     const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
 #pragma unroll
-    for (int j = 0; j < NT; ++j) fb[j] = rb.read(B0, at_b, j);
+    for (int j = 0; j < NT; ++j) fb[j] = rb.read(B0, at_b, 0, j);
 #pragma unroll
-    for (int i = 0; i < MT; ++i) fa[i] = ra.read(A0, at_a, i);
-    for (int k = 4 * kEBK; k < K; k += 4 * kEBK) four_stages(ExpertInt<1>());
+    for (int i = 0; i < MT; ++i) fa[i] = ra.read(A0, at_a, 0, i);
+    for (int k = 2 * kEBK; k < K; k += 2 * kEBK) {
+      stage(ExpertInt<1>(), A0, B0, A1, B1);
+      stage(ExpertInt<1>(), A1, B1, A0, B0);
+    }
     aim(more, next);
-    four_stages(ExpertInt<0>());
+    stage(ExpertInt<1>(), A0, B0, A1, B1);
+    stage(ExpertInt<0>(), A1, B1, A0, B0);
+    // the last sums leave the matrix unit before they are read
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
   }
   const int e = at.e, bm = at.bm;
