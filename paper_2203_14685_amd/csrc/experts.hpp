@@ -88,10 +88,11 @@ __device__ __forceinline__ V expert_opaque(V v) {
 }
 
 // One operand's loads: W rows (kRows) or columns (kCols) of the tile.
-template <class T, int KIND, bool RIGHT, int W, int WAVES>
+template <class T, int KIND, bool RIGHT, int W, int WAVES, int BK = kExpertBk<T>>
 struct ExpertOperand {
-  static constexpr int kBk = kExpertBk<T>, kPe = kExpertPe<T>, kElt = static_cast<int>(sizeof(T));
-  static constexpr int kBytes = W * kExpertRow;
+  static constexpr int kBk = BK, kPe = kExpertPe<T>, kElt = static_cast<int>(sizeof(T));
+  static constexpr int kBytes = W * BK * kElt;
+  static_assert(KIND == kCols || BK == kExpertBk<T>, "whole cache lines along K");
   static constexpr int N = kBytes / 1024 / WAVES;  // loads per wave and stage
   static_assert(N * WAVES * 1024 == kBytes, "whole loads");
   static constexpr int P = KIND == kRows ? kExpertRow / 16 : W / kPe;  // pieces per LDS row
@@ -208,6 +209,8 @@ struct ExpertTile {
   int e, bm, bn;
 };
 
+constexpr int kTileList = 256;  // a block's next tiles, found together by its threads
+
 template <int BM>
 struct ExpertTiles {
   int nv;    // tiles with work
@@ -245,16 +248,23 @@ struct ExpertTiles {
     used = ((nv + g - 1) / g + 7) / 8 * g;
   }
 
-  // The next slot from `j` on, by `step`, of XCD x that holds a tile with work (j is moved
-  // to it); false behind the last one.
-  __device__ __forceinline__ bool work(const ExpertGemmArgs& a, int x, int step, int& j, ExpertTile& t) const {
-    for (; j < used; j += step) {
-      const int q = j / g;
-      const int v = (q * 8 + x) * g + (j - q * g);
-      if (v < nv) return find(a, v, false, t);
+  // The tile of slot j of XCD x; e = -1 behind the last one (and then for all later slots).
+  __device__ __forceinline__ int4 slot_tile(const ExpertGemmArgs& a, int x, int j) const {
+    const int q = j / g;
+    const int v = (q * 8 + x) * g + (j - q * g);
+    if (j >= used || v >= nv) return int4{-1, 0, 0, 0};
+    int lo = 0, hi = a.E - 1;  // the first expert whose tiles end behind v
+    while (lo < hi) {
+      const int mid = (lo + hi) / 2;
+      if (before[mid] * a.tn > v) hi = mid;
+      else lo = mid + 1;
     }
-    return false;
+    const int first = lo > 0 ? before[lo - 1] : 0;
+    const int mt = before[lo] - first;
+    const int r = v - first * a.tn;
+    return int4{lo, r % mt, r / mt, 0};
   }
+
   // Tile `i` of those without work.
   __device__ __forceinline__ bool clear(const ExpertGemmArgs& a, int i, ExpertTile& t) const {
     return i < a.tiles - nv && find(a, i, true, t);
@@ -283,6 +293,22 @@ struct ExpertTiles {
     return false;
   }
 };
+
+__device__ __forceinline__ bool expert_listed(const int4* list, int i, ExpertTile& t) {
+  const int4 q = list[i];
+  t.e = __builtin_amdgcn_readfirstlane(q.x);
+  t.bm = __builtin_amdgcn_readfirstlane(q.y);
+  t.bn = __builtin_amdgcn_readfirstlane(q.z);
+  return t.e >= 0;
+}
+
+// The rows of a tile in a row-major matrix of `ld` columns, for 16-byte accesses at
+// 32-bit offsets: those past `valid` rows, or at kExpertOob, read zeros and write nothing.
+template <class T>
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t expert_rows(const void* p, int64_t row0, int ld, int valid) {
+  return expert_rsrc(reinterpret_cast<const T*>(p) + row0 * ld,
+                     __builtin_amdgcn_readfirstlane(max(0, valid) * ld * static_cast<int>(sizeof(T))));
+}
 
 // Blocks: at most `resident`, a multiple of 8.
 inline unsigned expert_blocks(int tiles, int resident) {

@@ -12,8 +12,10 @@
 // While one half of a stage (32 K) is multiplied the fragments of the next half are
 // read, so the reads' latency and the barrier per stage lie behind products; the
 // stage after next is requested as soon as every wave has read the last half of the
-// stage in its place.  Towards the end of a tile those are the next tile's, so that its
-// first loads lie behind the products and the stores of this one.
+// stage in its place.  Where both operands are read through transposes, four stages of
+// 32 K take turns instead: the loads run further ahead, which the short sums over an
+// expert's rows need (dw of 64 x 512 x 2048 x 8192 1.31 -> 1.20 ms).  Towards the end of a
+// tile the loads are the next tile's, behind the products and the stores of this one.
 //
 // The product is formed transposed (columns n are the rows of the matrix unit), so a lane
 // holds 4 neighbouring columns of one row; a swap with the neighbouring 16 lanes over a
@@ -66,26 +68,32 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
   constexpr bool kSplit = EPI == kEpiAct && GATED;
   constexpr int BNO = kSplit ? BN / 2 : BN;
-  __shared__ __align__(1024) bf16_t A0[BM * kEBK], A1[BM * kEBK], B0[BN * kEBK], B1[BN * kEBK];
+  constexpr bool kRing = KA == kCols && KB == kCols;  // four stages of half the length
+  constexpr int BK = kRing ? kEBK / 2 : kEBK;
+  __shared__ __align__(1024) bf16_t A0[BM * BK], A1[BM * BK], B0[BN * BK], B1[BN * BK];
+  __shared__ __align__(1024) bf16_t A2[kRing ? BM * BK : 8], A3[kRing ? BM * BK : 8];
+  __shared__ __align__(1024) bf16_t B2[kRing ? BN * BK : 8], B3[kRing ? BN * BK : 8];
   __shared__ int tile_before[kMaxExperts], tile_rows[kMaxExperts];
+  __shared__ int4 tile_list[kTileList];
 
   const int lane = lane_id(), g = lane / 16, m = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int wm = wave / WN, wn = wave % WN;
   const int xcd = blockIdx.x % 8, step = gridDim.x / 8;
-  int slot = blockIdx.x / 8;
+  int slot = blockIdx.x / 8;  // of the list's first tile
   ExpertTiles<BM> tiles;
   tiles.init(a, tile_before, tile_rows);
+  auto list_tiles = [&]() {
+    for (int i = threadIdx.x; i < kTileList; i += WAVES * kWave) tile_list[i] = tiles.slot_tile(a, xcd, slot + i * step);
+    __syncthreads();
+  };
+  list_tiles();
 
-  ExpertOperand<bf16_t, KA, false, BM, WAVES> oa;
-  ExpertOperand<bf16_t, KB, true, BN, WAVES> ob;
+  ExpertOperand<bf16_t, KA, false, BM, WAVES, BK> oa;
+  ExpertOperand<bf16_t, KB, true, BN, WAVES, BK> ob;
   int left = 0;  // K elements of the loads' tile from the next stage on
   // Points the loads at tile t (none: zeros).
-  auto aim = [&](bool any, ExpertTile t) {
-    // known to be the same on all lanes: the resources then stay in scalar registers
-    t.e = __builtin_amdgcn_readfirstlane(t.e);
-    t.bm = __builtin_amdgcn_readfirstlane(t.bm);
-    t.bn = __builtin_amdgcn_readfirstlane(t.bn);
+  auto aim = [&](bool any, const ExpertTile& t) {
     const int n = any ? __builtin_amdgcn_readfirstlane(tile_rows[t.e]) : 0;
     const int m0 = t.bm * BM, n0 = t.bn * BNO;
     const int K = a.k_is_rows ? n : any ? a.K : 0;
@@ -106,13 +114,17 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   ExpertFrag<KB, true, BN, NT> rb;
   ra.init(wm * MT * 16, g, m);
   rb.init(wn * NT * 16, g, m);
-  constexpr int kLoads = ExpertOperand<bf16_t, KA, false, BM, WAVES>::N + ExpertOperand<bf16_t, KB, true, BN, WAVES>::N;
+  constexpr int kLoads = ExpertOperand<bf16_t, KA, false, BM, WAVES, BK>::N + ExpertOperand<bf16_t, KB, true, BN, WAVES, BK>::N;
+  // Stores that every tile's epilogue ends with at least, all issued whatever is masked.
+  constexpr int kStores = EPI == kEpiStore ? MT * NP : EPI == kEpiAct ? MT * (kSplit ? 1 : NP) : MT * NP * (GATED ? 2 : 1);
+  // and with pre written too
+  constexpr int kStoresPre = EPI == kEpiAct ? kStores + MT * NP : kStores;
   f32x4 acc[MT][NT];
   u32x4 fa[MT], fb[NT], fn[NT];
-  auto load = [&](bf16_t* As, bf16_t* Bs) {
+  auto load = [&](bf16_t* As, bf16_t* Bs) __attribute__((always_inline)) {
     oa.load(As, wave, left);
     ob.load(Bs, wave, left);
-    left -= kEBK;
+    left -= BK;
   };
   // Products of the half stage in fa and cur.  Each left fragment makes room for the one of
   // the half after it, step ks of (As, Bs), as soon as it is used (READ; the registers of a
@@ -120,7 +132,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   // each sum to its registers and the reads to their places: left to the compiler, sums
   // and fragments moved between registers and scratch memory.  The two empty slots cover
   // a move into an operand right before.
-  auto half = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], const bf16_t* As, const bf16_t* Bs, int ks) {
+  auto half = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], const bf16_t* As, const bf16_t* Bs, int ks) __attribute__((always_inline)) {
     constexpr bool READ = decltype(read)::v;
     const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
     if constexpr (READ) {
@@ -135,22 +147,59 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
       if constexpr (READ) fa[i] = ra.read(As, at_a, ks, i);
     }
   };
+  // Stores of the tile before may still be on their way where the loads waited for were
+  // issued ahead of them (the counter counts in order): `fresh`.
+  bool fresh = false;
+  auto barrier = [&](auto ahead) __attribute__((always_inline)) {
+    constexpr int N = decltype(ahead)::v;  // loads that may be on their way
+    if (!fresh) expert_stage_barrier<N>();
+    else if (kStoresPre > kStores && a.pre) expert_stage_barrier<N + kStoresPre>();
+    else expert_stage_barrier<N + kStores>();
+  };
   // The stage in (As, Bs), its first half in fa and fb.  Behind the barrier the next stage,
   // (An, Bn), is in LDS, and this one's place is free for the one after it.
-  auto stage = [&](auto read_last, bf16_t* As, bf16_t* Bs, const bf16_t* An, const bf16_t* Bn) {
+  auto stage = [&](auto read_last, bf16_t* As, bf16_t* Bs, const bf16_t* An, const bf16_t* Bn) __attribute__((always_inline)) {
     half(ExpertInt<1>(), fb, fn, As, Bs, 1);
-    expert_stage_barrier();
+    barrier(ExpertInt<0>());
+    fresh = false;
     load(As, Bs);
     half(read_last, fn, fb, An, Bn, 0);
   };
+  // One of four stages, in fa and cur; its place is free behind the barrier.
+  auto quarter = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], bf16_t* As, bf16_t* Bs, const bf16_t* An,
+                     const bf16_t* Bn) __attribute__((always_inline)) {
+    barrier(ExpertInt<2 * kLoads>());
+    load(As, Bs);
+    half(read, cur, next, An, Bn, 0);
+  };
+  // 128 K elements.
+  auto four_halves = [&](auto read_last) __attribute__((always_inline)) {
+    if constexpr (kRing) {
+      quarter(ExpertInt<1>(), fb, fn, A0, B0, A1, B1);
+      quarter(ExpertInt<1>(), fn, fb, A1, B1, A2, B2);
+      quarter(ExpertInt<1>(), fb, fn, A2, B2, A3, B3);
+      fresh = false;
+      quarter(read_last, fn, fb, A3, B3, A0, B0);
+    } else {
+      stage(ExpertInt<1>(), A0, B0, A1, B1);
+      stage(read_last, A1, B1, A0, B0);
+    }
+  };
 
   ExpertTile at{0, 0, 0}, next{0, 0, 0};
-  bool work = __builtin_amdgcn_readfirstlane(tiles.work(a, xcd, step, slot, at)) != 0;
+  int index = 0;  // in the list
+  bool work = expert_listed(tile_list, 0, at);
   if (work) {
     aim(true, at);
     load(A0, B0);
     load(A1, B1);
-    expert_stage_barrier<kLoads>();
+    if constexpr (kRing) {
+      load(A2, B2);
+      load(A3, B3);
+      expert_stage_barrier<3 * kLoads>();
+    } else {
+      expert_stage_barrier<kLoads>();
+    }
   }
   // the tiles without work that this block clears
   int idle = blockIdx.x;
@@ -162,24 +211,24 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (work) {
-    // the first two stages of the next tile are on their way before this one's results
-    // are stored; behind the last tile: zeros, so that the count of loads stays the same
+    // the first 128 K of the next tile are on their way before this one's results are
+    // stored; behind the last tile: zeros, so that the count of loads stays the same
     const int K = a.k_is_rows ? __builtin_amdgcn_readfirstlane(tile_rows[at.e]) : a.K;
-    slot += step;
-    more = __builtin_amdgcn_readfirstlane(tiles.work(a, xcd, step, slot, next)) != 0;
-    slot = __builtin_amdgcn_readfirstlane(slot);
+    if (++index == kTileList) {
+      __syncthreads();
+      slot += kTileList * step;
+      index = 0;
+      list_tiles();
+    }
+    more = expert_listed(tile_list, index, next);
     const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
 #pragma unroll
     for (int j = 0; j < NT; ++j) fb[j] = rb.read(B0, at_b, 0, j);
 #pragma unroll
     for (int i = 0; i < MT; ++i) fa[i] = ra.read(A0, at_a, 0, i);
-    for (int k = 2 * kEBK; k < K; k += 2 * kEBK) {
-      stage(ExpertInt<1>(), A0, B0, A1, B1);
-      stage(ExpertInt<1>(), A1, B1, A0, B0);
-    }
+    for (int k = 2 * kEBK; k < K; k += 2 * kEBK) four_halves(ExpertInt<1>());
     aim(more, next);
-    stage(ExpertInt<1>(), A0, B0, A1, B1);
-    stage(ExpertInt<0>(), A1, B1, A0, B0);
+    four_halves(ExpertInt<0>());
     // the last sums leave the matrix unit before they are read
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
   }
@@ -202,10 +251,18 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         acc[i][2 * p + 1][q] = __uint_as_float(r[1]);
       }
   const int ln = expert_opaque(lane), lm = ln % 16, lg = ln / 16;
-  const int row0 = m0 + wm * MT * 16 + lm;
+  const int lrow = wm * MT * 16 + lm;  // of the tile; 16 i on
   const int col0 = n0 + (kSplit ? wn * 32 : wn * 64) + 16 * (lg % 2) + 8 * (lg / 2);
   auto value = [&](int i, int p, int q) { return acc[i][2 * p + q / 4][q % 4]; };
+  // byte of (lrow, column c) in rows of ld, or past everything
+  auto place = [&](int ld, int c, bool in) { return in ? (lrow * ld + c) * 2 : kExpertOob; };
+  auto put = [&](__amdgpu_buffer_rsrc_t r, int off, const float (&v)[8]) {
+    __builtin_amdgcn_raw_buffer_store_b128(Chunk<bf16_t>::pack(v), r, off, 0, 0);
+  };
+  const int valid = min(BM, a.M - m0);  // rows of the output
   if constexpr (EPI == kEpiStore) {
+    const __amdgpu_buffer_rsrc_t out =
+        expert_rows<bf16_t>(reinterpret_cast<const bf16_t*>(a.out) + e * a.sO, m0, a.ldo, valid);
     float bias[NP][8];
 #pragma unroll
     for (int p = 0; p < NP; ++p)
@@ -214,21 +271,22 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         bias[p][q] = a.bias && col0 + 32 * p < a.N ? a.bias[static_cast<int64_t>(e) * a.N + col0 + 32 * p + q] : 0.f;
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      const int row = row0 + 16 * i;
-      if (row >= a.M) continue;
-      uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + e * a.sO + static_cast<int64_t>(row) * a.ldo;
+      const bool used = m0 + lrow + 16 * i < rows;
 #pragma unroll
       for (int p = 0; p < NP; ++p) {
-        if (col0 + 32 * p >= a.N) continue;
         float v[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = row < rows ? value(i, p, q) + bias[p][q] : 0.f;
-        *reinterpret_cast<u32x4*>(out + col0 + 32 * p) = Chunk<bf16_t>::pack(v);
+        for (int q = 0; q < 8; ++q) v[q] = used ? value(i, p, q) + bias[p][q] : 0.f;
+        put(out, place(a.ldo, col0 + 32 * p, col0 + 32 * p < a.N) + i * 32 * a.ldo, v);
       }
     }
   } else if constexpr (EPI == kEpiAct) {
     const int N1 = GATED ? 2 * a.N : a.N;
     constexpr int NPO = kSplit ? 1 : NP;
+    const __amdgpu_buffer_rsrc_t hid =
+        expert_rows<bf16_t>(reinterpret_cast<const bf16_t*>(a.out) + e * a.sO, m0, a.ldo, valid);
+    const __amdgpu_buffer_rsrc_t pre =
+        expert_rows<bf16_t>(a.pre, static_cast<int64_t>(e) * a.C + m0, N1, a.pre ? valid : 0);
     float bias[NP][8];
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -241,29 +299,26 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
       constexpr int ACT = decltype(which)::v;
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
-        const int row = row0 + 16 * i;
-        if (row >= a.M) continue;
-        uint16_t* hid = reinterpret_cast<uint16_t*>(a.out) + e * a.sO + static_cast<int64_t>(row) * a.ldo;
-        uint16_t* pre = reinterpret_cast<uint16_t*>(a.pre) + (static_cast<int64_t>(e) * a.C + row) * N1;
+        const bool used = m0 + lrow + 16 * i < rows;
 #pragma unroll
         for (int p = 0; p < NPO; ++p) {
           const int c = col0 + 32 * p;
-          if (c >= a.N) continue;
           float v[8], u[8], f[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
-            v[q] = row < rows ? value(i, p, q) + bias[p][q] : 0.f;
+            v[q] = used ? value(i, p, q) + bias[p][q] : 0.f;
             f[q] = expert_act<ACT>(v[q]);
             if constexpr (kSplit) {
-              u[q] = row < rows ? value(i, 1, q) + bias[1][q] : 0.f;
+              u[q] = used ? value(i, 1, q) + bias[1][q] : 0.f;
               f[q] *= u[q];
             }
           }
           if (a.pre) {
-            *reinterpret_cast<u32x4*>(pre + c) = Chunk<bf16_t>::pack(v);
-            if constexpr (kSplit) *reinterpret_cast<u32x4*>(pre + a.N + c) = Chunk<bf16_t>::pack(u);
+            const int at_pre = place(N1, c, c < a.N) + i * 32 * N1;
+            put(pre, at_pre, v);
+            if constexpr (kSplit) put(pre, at_pre + 2 * a.N, u);
           }
-          *reinterpret_cast<u32x4*>(hid + c) = Chunk<bf16_t>::pack(f);
+          put(hid, place(a.ldo, c, c < a.N) + i * 32 * a.ldo, f);
         }
       }
     });
@@ -271,6 +326,10 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     // dpre, and its sums over the wave's rows before the rounding: [E, tm * WM, N1]
     const int N1 = GATED ? 2 * a.N : a.N;
     float* part = a.colsum ? a.colsum + (static_cast<int64_t>(e) * a.tm * WM + bm * WM + wm) * N1 : nullptr;
+    const __amdgpu_buffer_rsrc_t out = expert_rows<bf16_t>(a.out, static_cast<int64_t>(e) * a.C + m0, N1, valid);
+    // rows behind the count read as zeros, and so does their dhidden
+    const __amdgpu_buffer_rsrc_t pre =
+        expert_rows<bf16_t>(a.pre, static_cast<int64_t>(e) * a.C + m0, N1, min(BM, rows - m0));
     expert_by_act(a.act, [&](auto which) {
       constexpr int ACT = decltype(which)::v;
 #pragma unroll
@@ -281,30 +340,22 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         for (int q = 0; q < 8; ++q) s0[q] = s1[q] = 0.f;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
-          const int row = row0 + 16 * i;
-          if (row >= a.M || c >= a.N) continue;
-          const int64_t at = (static_cast<int64_t>(e) * a.C + row) * N1 + c;
-          uint16_t* out = reinterpret_cast<uint16_t*>(a.out) + at;
+          const int off = place(N1, c, c < a.N) + i * 32 * N1;
           float v[8], u[8];
+          Chunk<bf16_t>::unpack(__builtin_amdgcn_raw_buffer_load_b128(pre, off, 0, 0), v);
+          if constexpr (GATED) Chunk<bf16_t>::unpack(__builtin_amdgcn_raw_buffer_load_b128(pre, off + 2 * a.N, 0, 0), u);
 #pragma unroll
-          for (int q = 0; q < 8; ++q) v[q] = u[q] = 0.f;
-          if (row < rows) {
-            const uint16_t* src = reinterpret_cast<const uint16_t*>(a.pre) + at;
-            Chunk<bf16_t>::unpack(*reinterpret_cast<const u32x4*>(src), v);
-            if constexpr (GATED) Chunk<bf16_t>::unpack(*reinterpret_cast<const u32x4*>(src + a.N), u);
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              float f, df;
-              expert_act_grad<ACT>(v[q], f, df);
-              const float dh = value(i, p, q);
-              v[q] = GATED ? dh * u[q] * df : dh * df;
-              u[q] = dh * f;
-              s0[q] += v[q];
-              if constexpr (GATED) s1[q] += u[q];
-            }
+          for (int q = 0; q < 8; ++q) {
+            float f, df;
+            expert_act_grad<ACT>(v[q], f, df);
+            const float dh = value(i, p, q);
+            v[q] = GATED ? dh * u[q] * df : dh * df;
+            u[q] = dh * f;
+            s0[q] += v[q];
+            if constexpr (GATED) s1[q] += u[q];
           }
-          *reinterpret_cast<u32x4*>(out) = Chunk<bf16_t>::pack(v);
-          if constexpr (GATED) *reinterpret_cast<u32x4*>(out + a.N) = Chunk<bf16_t>::pack(u);
+          put(out, off, v);
+          if constexpr (GATED) put(out, off + 2 * a.N, u);
         }
         if (part) {
 #pragma unroll
@@ -325,6 +376,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   }
   if (more) {
     at = next;
+    fresh = true;
     continue;
   }
   if (work) expert_stage_barrier();  // nothing is on its way to LDS when the block ends

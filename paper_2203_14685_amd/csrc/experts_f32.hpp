@@ -69,8 +69,11 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_f32_kernel(ExpertGem
   for (;;) {
   // the tiles with work, then those that are only cleared
   ExpertTile at{0, 0, 0};
-  const bool work = tiles.work(a, xcd, step, slot, at);
+  const int4 found = tiles.slot_tile(a, xcd, slot);
+  const bool work = __builtin_amdgcn_readfirstlane(found.x) >= 0;
   if (work) {
+    at = {__builtin_amdgcn_readfirstlane(found.x), __builtin_amdgcn_readfirstlane(found.y),
+          __builtin_amdgcn_readfirstlane(found.z)};
     slot += step;
   } else {
     if (!tiles.clear(a, idle, at)) return;
