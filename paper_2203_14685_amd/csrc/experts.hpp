@@ -128,23 +128,33 @@ struct ExpertOperand {
       }
     }
   }
-  // The stage `base` points at; `left` K elements remain (none: zeros).  An offset past the resource
-  // stays past it (below 2^32) with the rows' strides added.
-  __device__ __forceinline__ void load(T* lds, int wave, int left) {
-    const __amdgpu_buffer_rsrc_t r = expert_rsrc(
-        base, __builtin_amdgcn_readfirstlane(KIND == kRows ? max(rows, 0) : max(0, min(left, kBk)) * pitch));
-    const unsigned stride = static_cast<unsigned>(R * WAVES) * static_cast<unsigned>(pitch);
-    unsigned o[kAlt];
+  // The loads of the stage `base` points at; `left` K elements remain (none: zeros).  An
+  // offset past the resource stays past it (below 2^32) with the rows' strides added.
+  struct Stage {
+    __amdgpu_buffer_rsrc_t r;
+    unsigned o[kAlt], stride;
+    __device__ __forceinline__ void issue(T* lds, int wave, int i) const {
+      expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, static_cast<int>(o[i % kAlt] + i * stride));
+    }
+  };
+  __device__ __forceinline__ Stage next(int left) {
+    Stage s;
+    s.r = expert_rsrc(base,
+                      __builtin_amdgcn_readfirstlane(KIND == kRows ? max(rows, 0) : max(0, min(left, kBk)) * pitch));
+    s.stride = static_cast<unsigned>(R * WAVES) * static_cast<unsigned>(pitch);
 #pragma unroll
     for (int i = 0; i < kAlt; ++i) {
-      o[i] = expert_opaque(off[i]);
-      if constexpr (KIND == kRows) o[i] = kc < left ? o[i] : static_cast<unsigned>(kExpertOob);
+      s.o[i] = expert_opaque(off[i]);
+      if constexpr (KIND == kRows) s.o[i] = kc < left ? s.o[i] : static_cast<unsigned>(kExpertOob);
     }
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, static_cast<int>(o[i % kAlt] + i * stride));
     base += KIND == kRows ? kExpertRow : kBk * pitch;
     if constexpr (KIND == kRows) rows -= kExpertRow;
+    return s;
+  }
+  __device__ __forceinline__ void load(T* lds, int wave, int left) {
+    const Stage s = next(left);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s.issue(lds, wave, i);
   }
 };
 

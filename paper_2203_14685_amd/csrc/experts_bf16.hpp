@@ -10,7 +10,7 @@
 // where it writes.
 //
 // While one half of a stage (32 K) is multiplied the fragments of the next half are
-// read, so the reads' latency and the barrier per stage lie behind products; the
+// read between them, so the reads' latency and the barrier lie behind products; the
 // stage after next is requested as soon as every wave has read the last half of the
 // stage in its place.  Where both operands are read through transposes, four stages of
 // 32 K take turns instead: the loads run further ahead, which the short sums over an
@@ -126,27 +126,6 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     ob.load(Bs, wave, left);
     left -= BK;
   };
-  // Products of the half stage in fa and cur.  Each left fragment makes room for the one of
-  // the half after it, step ks of (As, Bs), as soon as it is used (READ; the registers of a
-  // tile's last fragments serve its epilogue).  The products are written out to tie
-  // each sum to its registers and the reads to their places: left to the compiler, sums
-  // and fragments moved between registers and scratch memory.  The two empty slots cover
-  // a move into an operand right before.
-  auto half = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], const bf16_t* As, const bf16_t* Bs, int ks) __attribute__((always_inline)) {
-    constexpr bool READ = decltype(read)::v;
-    const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
-    if constexpr (READ) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j) next[j] = rb.read(Bs, at_b, ks, j);
-    }
-#pragma unroll
-    for (int i = 0; i < MT; ++i) {
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-        asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc[i][j]) : "v"(cur[j]), "v"(fa[i]));
-      if constexpr (READ) fa[i] = ra.read(As, at_a, ks, i);
-    }
-  };
   // Stores of the tile before may still be on their way where the loads waited for were
   // issued ahead of them (the counter counts in order): `fresh`.
   bool fresh = false;
@@ -156,21 +135,66 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     else if (kStoresPre > kStores && a.pre) expert_stage_barrier<N + kStoresPre>();
     else expert_stage_barrier<N + kStores>();
   };
-  // The stage in (As, Bs), its first half in fa and fb.  Behind the barrier the next stage,
-  // (An, Bn), is in LDS, and this one's place is free for the one after it.
-  auto stage = [&](auto read_last, bf16_t* As, bf16_t* Bs, const bf16_t* An, const bf16_t* Bn) __attribute__((always_inline)) {
-    half(ExpertInt<1>(), fb, fn, As, Bs, 1);
-    barrier(ExpertInt<0>());
-    fresh = false;
-    load(As, Bs);
-    half(read_last, fn, fb, An, Bn, 0);
+  // Products of 32 K, their fragments in fa and cur, in MT groups of NT; between them
+  //   SYNC  behind the first groups, the barrier after which the next fragments' stage is in
+  //         LDS and the place (As, Bs) free, and the loads of the stage that goes there;
+  //   READ  the fragments of the next 32 K, step ks of (An, Bn), the left ones into the
+  //         registers of those already used (a tile's last fragments make room for its epilogue).
+  // All in their places so that products follow products: the barrier finds the reads
+  // before it returned.  The products are written out to tie each sum to its registers
+  // and to keep that order: left to the compiler, sums and fragments moved between
+  // registers and scratch memory.  The empty slots cover a move into an operand right before.
+  auto half = [&](auto read, auto sync, u32x4 (&cur)[NT], u32x4 (&next)[NT], bf16_t* As, bf16_t* Bs, const bf16_t* An,
+                  const bf16_t* Bn, int ks) __attribute__((always_inline)) {
+    constexpr bool READ = decltype(read)::v != 0, SYNC = decltype(sync)::v >= 0;
+    constexpr int kFirst = SYNC ? (MT >= 8 ? 1 : 0) : 0;  // group behind which the rest begins
+    constexpr int kParts = MT - kFirst > 1 ? MT - kFirst - 1 : 1;
+    const unsigned at_a = expert_opaque(ra.at), at_b = expert_opaque(rb.at);
+    typename decltype(oa)::Stage la;
+    typename decltype(ob)::Stage lb;
+#pragma unroll
+    for (int i = 0; i < MT; ++i) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+        asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc[i][j]) : "v"(cur[j]), "v"(fa[i]));
+      if constexpr (SYNC) {
+        if (i == kFirst) {
+          barrier(sync);
+          la = oa.next(left);
+          lb = ob.next(left);
+          left -= BK;
+        }
+      }
+      if (i < kFirst) continue;
+      const int part = i - kFirst;
+      if constexpr (READ) {
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+          if (j * kParts / NT == part) next[j] = rb.read(Bn, at_b, ks, j);
+#pragma unroll
+        for (int q = 0; q <= i; ++q)
+          if (q == i || part == 0) fa[q] = ra.read(An, at_a, ks, q);
+      }
+      if constexpr (SYNC) {
+#pragma unroll
+        for (int q = 0; q < kLoads; ++q)
+          if (q * kParts / kLoads == part) {
+            if (q < decltype(oa)::N) la.issue(As, wave, q);
+            else lb.issue(Bs, wave, q - decltype(oa)::N);
+          }
+      }
+    }
   };
-  // One of four stages, in fa and cur; its place is free behind the barrier.
+  // The stage in (As, Bs), its first half in fa and fb; the next one in (An, Bn).
+  auto stage = [&](auto read_last, bf16_t* As, bf16_t* Bs, const bf16_t* An, const bf16_t* Bn) __attribute__((always_inline)) {
+    half(ExpertInt<1>(), ExpertInt<-1>(), fb, fn, nullptr, nullptr, As, Bs, 1);
+    half(read_last, ExpertInt<0>(), fn, fb, As, Bs, An, Bn, 0);
+    fresh = false;
+  };
+  // One of four stages, in fa and cur.
   auto quarter = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], bf16_t* As, bf16_t* Bs, const bf16_t* An,
                      const bf16_t* Bn) __attribute__((always_inline)) {
-    barrier(ExpertInt<2 * kLoads>());
-    load(As, Bs);
-    half(read, cur, next, An, Bn, 0);
+    half(read, ExpertInt<2 * kLoads>(), cur, next, As, Bs, An, Bn, 0);
   };
   // 128 K elements.
   auto four_halves = [&](auto read_last) __attribute__((always_inline)) {
@@ -330,49 +354,65 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     // rows behind the count read as zeros, and so does their dhidden
     const __amdgpu_buffer_rsrc_t pre =
         expert_rows<bf16_t>(a.pre, static_cast<int64_t>(e) * a.C + m0, N1, min(BM, rows - m0));
-    expert_by_act(a.act, [&](auto which) {
-      constexpr int ACT = decltype(which)::v;
 #pragma unroll
-      for (int p = 0; p < NP; ++p) {
-        const int c = col0 + 32 * p;
-        float s0[8], s1[8];
+    for (int p = 0; p < NP; ++p) {
+      const int c = col0 + 32 * p;
+      const int off0 = place(N1, c, c < a.N);
+      constexpr int kRowsAhead = GATED && MT > 1 ? MT / 2 : MT;  // rows requested together
+      float s0[8], s1[8];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) s0[q] = s1[q] = 0.f;
+      for (int q = 0; q < 8; ++q) s0[q] = s1[q] = 0.f;
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          const int off = place(N1, c, c < a.N) + i * 32 * N1;
+      for (int i0 = 0; i0 < MT; i0 += kRowsAhead) {
+        u32x4 pv[kRowsAhead], pu[kRowsAhead];
+#pragma unroll
+        for (int i = 0; i < kRowsAhead; ++i) {
+          const int off = off0 + (i0 + i) * 32 * N1;
+          pv[i] = __builtin_amdgcn_raw_buffer_load_b128(pre, off, 0, 0);
+          if constexpr (GATED) pu[i] = __builtin_amdgcn_raw_buffer_load_b128(pre, off + 2 * a.N, 0, 0);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < kRowsAhead; ++i) {
           float v[8], u[8];
-          Chunk<bf16_t>::unpack(__builtin_amdgcn_raw_buffer_load_b128(pre, off, 0, 0), v);
-          if constexpr (GATED) Chunk<bf16_t>::unpack(__builtin_amdgcn_raw_buffer_load_b128(pre, off + 2 * a.N, 0, 0), u);
+          Chunk<bf16_t>::unpack(pv[i], v);
+          if constexpr (GATED) Chunk<bf16_t>::unpack(pu[i], u);
+          // chosen per row: branches around all rows would hold all their loads at once
+          expert_by_act(a.act, [&](auto which) {
+            constexpr int ACT = decltype(which)::v;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+              float f, df;
+              expert_act_grad<ACT>(v[q], f, df);
+              const float dh = value(i0 + i, p, q);
+              v[q] = GATED ? dh * u[q] * df : dh * df;
+              if constexpr (GATED) u[q] = dh * f;
+            }
+          });
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
-            float f, df;
-            expert_act_grad<ACT>(v[q], f, df);
-            const float dh = value(i, p, q);
-            v[q] = GATED ? dh * u[q] * df : dh * df;
-            u[q] = dh * f;
             s0[q] += v[q];
             if constexpr (GATED) s1[q] += u[q];
           }
-          put(out, off, v);
-          if constexpr (GATED) put(out, off + 2 * a.N, u);
+          put(out, off0 + (i0 + i) * 32 * N1, v);
+          if constexpr (GATED) put(out, off0 + (i0 + i) * 32 * N1 + 2 * a.N, u);
         }
-        if (part) {
+      }
+      if (part) {
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          s0[q] = group_reduce<16>(s0[q], OpAdd());
+          if constexpr (GATED) s1[q] = group_reduce<16>(s1[q], OpAdd());
+        }
+        if (lm == 0 && c < a.N) {
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
-            s0[q] = group_reduce<16>(s0[q], OpAdd());
-            if constexpr (GATED) s1[q] = group_reduce<16>(s1[q], OpAdd());
-          }
-          if (lm == 0 && c < a.N) {
-#pragma unroll
-            for (int q = 0; q < 8; ++q) {
-              part[c + q] = s0[q];
-              if constexpr (GATED) part[a.N + c + q] = s1[q];
-            }
+            part[c + q] = s0[q];
+            if constexpr (GATED) part[a.N + c + q] = s1[q];
           }
         }
       }
-    });
+    }
   }
   if (more) {
     at = next;

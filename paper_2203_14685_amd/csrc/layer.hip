@@ -42,7 +42,7 @@ __device__ __forceinline__ void columns_of(const Piece<8>::T (&in)[8], u32x4 (&o
 
 // One expert's strip: the rows of A that `list` names times NB columns of its matrix.
 // FIRST: A = x (row list / k), out = hidden; else A = hidden (row list), out = partial sums.
-template <class T, int CB, int MT, int WAVES, bool FIRST, bool GATED>
+template <class T, int CB, int MAXT, int WAVES, bool FIRST, bool GATED>
 __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) {
   constexpr int ELT = static_cast<int>(sizeof(T));
   constexpr int NC = CB / ELT, NB = 16 * NC;   // columns per lane and strip
@@ -99,8 +99,9 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) 
   const int steps = (K + kStep - 1) / kStep;
   const int stride = gridDim.z * WAVES;
 
-  for (int r0 = 0; r0 < n; r0 += 16 * MT) {
-    const int mts = min(MT, (n - r0 + 15) / 16);
+  // MT tiles of 16 rows of the list, from r0 on
+  auto run = [&](auto tiles, int r0) {
+    constexpr int MT = decltype(tiles)::v;
     int arow[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
@@ -167,7 +168,6 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) 
     // sums of the waves, 16 rows at a time: lane (g, m) holds rows 4 g + r, columns NC m + j
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-      if (i >= mts) break;
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -202,6 +202,15 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) 
       }
       __syncthreads();
     }
+  };
+  // no more row tiles than the list has: matrix units idle beside them cost nothing, but
+  // in fp32 the products of 64 rows take longer than the weights that they share
+  for (int r0 = 0; r0 < n; r0 += 16 * MAXT) {
+    const int left = n - r0;
+    if (MAXT == 1 || left <= 16) run(ExpertInt<1>(), r0);
+    else if (MAXT == 2 || left <= 32) run(ExpertInt<(MAXT > 1 ? 2 : 1)>(), r0);
+    else if (MAXT == 3 || left <= 48) run(ExpertInt<(MAXT > 2 ? 3 : 1)>(), r0);
+    else run(ExpertInt<(MAXT > 3 ? 4 : 1)>(), r0);
   }
 }
 
@@ -264,7 +273,8 @@ hipError_t strips(const LayerArgs& a, hipStream_t st) {
   if (narrow(a, FIRST)) return strip<T, 8, 1, 16, FIRST>(a, z, st);
   if (a.S <= 16) return strip<T, 16, 1, 8, FIRST>(a, z, st);
   if (a.S <= 32) return strip<T, 16, 2, 8, FIRST>(a, z, st);
-  return strip<T, 16, 4, 8, FIRST>(a, z, st);
+  // 48 rows are what the registers hold in bf16
+  return strip<T, 16, sizeof(T) == 2 ? 3 : 4, 8, FIRST>(a, z, st);
 }
 
 template <class T>
