@@ -527,8 +527,9 @@ MOE_API moe_status moe_token_layer_workspace_size(const moe_token_layer_params* 
  * moe_token_layer -- the whole layer for a few tokens (a decoding step), without
  * slots: nothing is dropped.
  *   y[s] = sum_r weights[s,r] * expert_{ids[s,r]}(x[s])
- * with ids and weights as moe_gate gives them for the same parameters and inputs,
- * and the expert networks of moe_experts (hidden rounded once to dtype).  Only the
+ * with ids and weights by moe_gate's rules for the same parameters and inputs (its
+ * logits' last bits may differ from a moe_gate call's, as between two batches), and
+ * the expert networks of moe_experts (hidden rounded once to dtype).  Only the
  * weights of experts that a token chose are read.  fp32 sums, rounded once.
  *
  * Inputs   x [S,d], S <= MOE_TOKEN_LAYER_MAX; wg, bias, token_ids, noise, hash_table

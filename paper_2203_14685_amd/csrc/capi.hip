@@ -904,6 +904,8 @@ TokenLayerPlan plan_token_layer(const moe_token_layer_params* p) {
   a.z2 = layer_splits(a);
   const size_t choices = static_cast<size_t>(g.S) * static_cast<size_t>(g.k);
   w.gate = p->routed ? 0 : std::max(gate_workspace_bytes(&g), gate_split_bytes(&g));
+  if (!p->routed && g.kind != MOE_GATE_HASH)
+    w.gate = std::max(w.gate, static_cast<size_t>(layer_gate_splits(g.d)) * static_cast<size_t>(g.S) * static_cast<size_t>(g.E) * 4);
   w.off_hidden = align256(w.gate);
   w.off_part = w.off_hidden + align256(choices * static_cast<size_t>(p->h) * elt_size(g.dtype));
   w.total = w.off_part + align256(static_cast<size_t>(a.z2) * choices * static_cast<size_t>(g.d) * 4);
@@ -1107,8 +1109,19 @@ moe_status moe_token_layer(const moe_token_layer_params* p, const void* x, const
   CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
   if (S == 0) return ok();
   char* ws = static_cast<char*>(workspace);
-  if (!p->routed)
-    CHECK(gate_select(&g, hash ? nullptr : x, wg, bias, token_ids, noise, hash_table, nullptr, ids, weights, ws, w.gate, stream));
+  if (!p->routed) {
+    LayerGateArgs q{};
+    q.S = g.S; q.d = g.d; q.E = g.E; q.k = g.k; q.kind = g.kind; q.normalize = g.normalize; q.groups = g.groups;
+    q.dtype = g.dtype; q.temperature = g.temperature;
+    q.z = layer_gate_splits(g.d); q.part = reinterpret_cast<float*>(ws);
+    q.x = x; q.wg = wg; q.bias = bias; q.noise = noise; q.ids = ids; q.weights = weights;
+    if (learned && layer_gate_fits(q)) {
+      const hipError_t err = launch_layer_gate(q, stream);
+      if (err != hipSuccess) return hip_fail(err, "moe_token_layer: gate kernel launch");
+    } else {
+      CHECK(gate_select(&g, hash ? nullptr : x, wg, bias, token_ids, noise, hash_table, nullptr, ids, weights, ws, w.gate, stream));
+    }
+  }
   LayerArgs& a = w.a;
   a.x = x; a.w1 = w1; a.w2 = w2; a.b1 = b1; a.b2 = b2; a.ids = ids; a.weights = weights; a.y = y;
   a.hidden = ws + w.off_hidden;

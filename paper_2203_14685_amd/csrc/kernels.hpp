@@ -284,6 +284,22 @@ struct LayerArgs {
   float* part;              // workspace [z2, S * k, d]
   void* y;                  // [S, d]
 };
+// Its gate (learned gates).
+constexpr int kLayerGateWaves = 4;    // per block
+constexpr int kLayerGateSplits = 16;  // most ranges of K
+struct LayerGateArgs {
+  int S, d, E, k, kind, normalize, groups, dtype;
+  int z;                    // ranges of K
+  float temperature;
+  const void *x, *wg;
+  const float *bias, *noise;
+  float* part;              // workspace [z, S, E]
+  int32_t* ids;
+  float* weights;
+};
+int layer_gate_splits(int d);
+bool layer_gate_fits(const LayerGateArgs& a);
+hipError_t launch_layer_gate(const LayerGateArgs& a, hipStream_t st);
 int layer_splits(const LayerArgs& a);
 hipError_t launch_layer(const LayerArgs& a, hipStream_t st);
 
