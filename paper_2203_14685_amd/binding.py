@@ -709,15 +709,12 @@ def grad_tensors(grads, out=None):
     n = len(grads)
     if out is not None and len(out) != n:
         raise ValueError(f"{n} gradients, {len(out)} outputs")
-    arr = (GradTensor * n)()
+    flat = []  # src, dst, n, dtype (its pad is the upper half)
     for i, g in enumerate(grads):
-        t = arr[i]
-        t.dtype = _dtype_code(g)
-        t.n = g.numel()
-        t.src = t.dst = _ptr(g, None, "gradient")
-        if out is not None:
-            t.dst = _ptr(out[i], g.dtype, "output", t.n)
-    return arr
+        code, size = _dtype_code(g), g.numel()
+        src = _ptr(g, None, "gradient") or 0
+        flat += (src, src if out is None else _ptr(out[i], g.dtype, "output", size) or 0, size, code)
+    return (GradTensor * n).from_buffer((ctypes.c_int64 * (4 * n))(*flat)) if n else (GradTensor * 0)()
 
 
 def moe_grad_norm_workspace_size(tensors):

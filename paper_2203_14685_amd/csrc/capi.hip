@@ -987,6 +987,14 @@ hipError_t by_grad_list(const moe_grad_tensor* t, int32_t count, Fn fn) {
   return hipSuccess;
 }
 
+// Whether the tensors exceed the Infinity Cache (256 MB), so that no pass finds what the one
+// before read.
+bool grads_beyond_cache(const moe_grad_tensor* t, int32_t count) {
+  int64_t bytes = 0;
+  for (int32_t i = 0; i < count; ++i) bytes += t[i].n * static_cast<int64_t>(elt_size(t[i].dtype));
+  return bytes > (int64_t(256) << 20);
+}
+
 // Partial sums: one per block of each list.
 size_t grad_parts(const moe_grad_tensor* t, int32_t count) {
   size_t n = 0;
@@ -1147,9 +1155,10 @@ moe_status moe_grad_norm(const moe_grad_tensor* tensors, int32_t count, double* 
   const size_t n = grad_parts(tensors, count);
   CHECK(check_workspace(who, workspace, workspace_bytes, n * sizeof(double)));
   double* part = static_cast<double*>(workspace);
+  const bool nt = grads_beyond_cache(tensors, count);
   size_t at = 0;
   hipError_t err = by_grad_list(tensors, count, [&](const GradList& l) {
-    const hipError_t e = launch_grad_squares(l, part + at, stream);
+    const hipError_t e = launch_grad_squares(l, nt, part + at, stream);
     at += static_cast<size_t>(grad_blocks(l.chunks));
     return e;
   });
@@ -1166,13 +1175,14 @@ moe_status moe_grad_clip(const moe_grad_tensor* tensors, int32_t count, const do
   CHECK(need(sumsq, 1, 8, who, "sumsq"));
   CHECK(need(norm, 0, 4, who, "norm"));
   CHECK(check_grad_overlap(tensors, count, who));
+  const bool nt = grads_beyond_cache(tensors, count);
   bool first = true;
   hipError_t err = by_grad_list(tensors, count, [&](const GradList& l) {
-    const hipError_t e = launch_grad_scale(l, sumsq, max_norm, first ? norm : nullptr, stream);
+    const hipError_t e = launch_grad_scale(l, nt, sumsq, max_norm, first ? norm : nullptr, stream);
     first = false;
     return e;
   });
-  if (err == hipSuccess && first && norm) err = launch_grad_scale(GradList{}, sumsq, max_norm, norm, stream);
+  if (err == hipSuccess && first && norm) err = launch_grad_scale(GradList{}, false, sumsq, max_norm, norm, stream);
   if (err != hipSuccess) return hip_fail(err, "moe_grad_clip: kernel launch");
   return ok();
 }

@@ -128,6 +128,11 @@ struct ExpertOperand {
       }
     }
   }
+  // Passes over n stages.
+  __device__ __forceinline__ void skip(int n) {
+    base += static_cast<int64_t>(n) * (KIND == kRows ? kExpertRow : kBk * pitch);
+    if constexpr (KIND == kRows) rows -= n * kExpertRow;
+  }
   // The loads of the stage `base` points at; `left` K elements remain (none: zeros).  An
   // offset past the resource stays past it (below 2^32) with the rows' strides added.
   struct Stage {

@@ -6,6 +6,9 @@
 // K 4 g + i; an operand whose rows run the other way is read four columns at a
 // time, tile j taking column 4 m + j, so a lane ends with 4 neighbouring columns.
 // Each 256 K are summed on their own and then added to the running sum.
+//
+// Small products leave most CUs idle, and a wave's sums over K are what they take: there
+// KG groups of waves take every KG-th stage each, and their sums are added pairwise.
 #pragma once
 
 #include "experts.hpp"
@@ -13,7 +16,7 @@
 namespace hetumoe {
 
 constexpr int kFBK = kExpertBk<float>;
-constexpr int kFSum = 8;  // stages summed on their own
+constexpr int kFSum = 8;  // stages summed on their own (a multiple of 2)
 
 // Left operand, step ks of 16: lane (g, m) gets K 4 g + 0..3 of row (column) x0 + m.
 template <int KIND, int W>
@@ -48,20 +51,22 @@ __device__ __forceinline__ void expert_right_f32(const float* lds, int x0, int k
   }
 }
 
-template <int BM, int BN, int WM, int WN, int KA, int KB, int EPI, bool GATED>
-__global__ __launch_bounds__(WM* WN * 64) void experts_gemm_f32_kernel(ExpertGemmArgs a) {
+template <int BM, int BN, int WM, int WN, int KG, int KA, int KB, int EPI, bool GATED>
+__global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(ExpertGemmArgs a) {
   constexpr int WAVES = WM * WN;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   static_assert(NT == 4, "64 columns per wave");
   constexpr bool kSplit = EPI == kEpiAct && GATED;  // 32 columns of the gate and 32 of the other factor per wave
   constexpr int BNO = kSplit ? BN / 2 : BN;
-  __shared__ __align__(1024) float A0[BM * kFBK], B0[BN * kFBK], A1[BM * kFBK], B1[BN * kFBK];
+  __shared__ __align__(1024) float A0_[KG * BM * kFBK], B0_[KG * BN * kFBK], A1_[KG * BM * kFBK], B1_[KG * BN * kFBK];
 
   __shared__ int tile_before[kMaxExperts], tile_rows[kMaxExperts];
 
   const int lane = lane_id(), g = lane / 16, m = lane % 16;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int kg = __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * kWave));
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) - kg * WAVES;
   const int wm = wave / WN, wn = wave % WN;
+  float *A0 = A0_ + kg * BM * kFBK, *B0 = B0_ + kg * BN * kFBK, *A1 = A1_ + kg * BM * kFBK, *B1 = B1_ + kg * BN * kFBK;
   const int xcd = blockIdx.x % 8, step = gridDim.x / 8;
   int slot = blockIdx.x / 8, idle = blockIdx.x;
   ExpertTiles<BM> tiles;
@@ -134,31 +139,62 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_f32_kernel(ExpertGem
         }
     };
     expert_stage_barrier();  // the tile before is read
-    oa.load(A0, wave, K);
-    ob.load(B0, wave, K);
-    int stage = 0;
-    int left = K;
-    for (; left > kFBK; left -= 2 * kFBK) {
+    oa.skip(kg);
+    ob.skip(kg);
+    const int stages = (K + KG * kFBK - 1) / (KG * kFBK);  // per group
+    int left = K - kg * kFBK;
+    auto load = [&](float* As, float* Bs) {
+      oa.load(As, wave, left);
+      ob.load(Bs, wave, left);
+      oa.skip(KG - 1);
+      ob.skip(KG - 1);
+      left -= KG * kFBK;
+    };
+    load(A0, B0);
+    int s = 0;
+    for (; s + 1 < stages; s += 2) {
       expert_stage_barrier();
-      oa.load(A1, wave, left - kFBK);
-      ob.load(B1, wave, left - kFBK);
+      load(A1, B1);
       multiply(A0, B0);
       expert_stage_barrier();
-      if (left > 2 * kFBK) {
-        oa.load(A0, wave, left - 2 * kFBK);
-        ob.load(B0, wave, left - 2 * kFBK);
-      }
+      if (s + 2 < stages) load(A0, B0);
       multiply(A1, B1);
-      stage += 2;
-      if (stage % kFSum == 0) flush();
+      if ((s + 2) % kFSum == 0) flush();
     }
-    if (left > 0) {
+    if (s < stages) {
       expert_stage_barrier();
       multiply(A0, B0);
     }
     flush();
+    if constexpr (KG > 1) {
+      // the upper half of the groups hands its sums to the lower one, until one is left
+      float* part = A0_;
+      static_assert(KG / 2 * WAVES * kWave * MT * NT * 4 <= KG * BM * kFBK, "room for half of the sums");
+      const int at = wave * kWave + lane;
+      auto place = [&](int q, int i, int j) {
+        return reinterpret_cast<f32x4*>(part + ((q * MT * NT + i * NT + j) * WAVES * kWave + at) * 4);
+      };
+#pragma unroll
+      for (int h = KG / 2; h >= 1; h /= 2) {
+        expert_stage_barrier();
+        if (kg >= h && kg < 2 * h) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) *place(kg - h, i, j) = sum[i][j];
+        }
+        expert_stage_barrier();
+        if (kg < h) {
+#pragma unroll
+          for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) sum[i][j] += *place(kg, i, j);
+        }
+      }
+    }
   }
 
+  if (kg > 0) continue;
   // lane (g, m): row m of tile i, columns 16 g + 4 r + 0..3, r = 0..3
   const int row0 = m0 + wm * MT * 16 + m;
   const int col0 = n0 + (kSplit ? wn * 32 + 8 * g : wn * 64 + 16 * g);

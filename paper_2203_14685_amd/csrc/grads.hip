@@ -27,7 +27,13 @@ __device__ __forceinline__ int tensor_of(const GradList& l, int c) {
 
 __device__ __forceinline__ double square(float v) { return static_cast<double>(v) * static_cast<double>(v); }
 
-template <class T>
+// NT: non-temporal, for gradients that no cache holds from one pass to the next.
+template <bool NT>
+__device__ __forceinline__ u32x4 load_piece(const u32x4* p) {
+  return NT ? __builtin_nontemporal_load(p) : *p;
+}
+
+template <class T, bool NT>
 __device__ __forceinline__ double chunk_squares(const T* p, int64_t n, bool vec) {
   constexpr int PE = Chunk<T>::kElems;
   double s = 0.0;
@@ -39,7 +45,7 @@ __device__ __forceinline__ double chunk_squares(const T* p, int64_t n, bool vec)
       u32x4 v[kGradUnroll];
 #pragma unroll
       for (int u = 0; u < kGradUnroll; ++u)
-        if (i + u * kBlock < pieces) v[u] = q[i + u * kBlock];
+        if (i + u * kBlock < pieces) v[u] = load_piece<NT>(q + i + u * kBlock);
 #pragma unroll
       for (int u = 0; u < kGradUnroll; ++u) {
         if (i + u * kBlock >= pieces) continue;
@@ -67,14 +73,15 @@ __device__ __forceinline__ double block_sum(double s) {
   return t;
 }
 
+template <bool NT>
 __global__ __launch_bounds__(kBlock) void grad_squares_kernel(GradList l, double* part) {
   double s = 0.0;
   for (int c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     const GradTensor& t = l.t[tensor_of(l, c)];
     const int64_t at = static_cast<int64_t>(c - t.first) * kGradChunk;
     const int64_t n = min(static_cast<int64_t>(kGradChunk), t.n - at);
-    s += t.dtype == 1 ? chunk_squares(static_cast<const bf16_t*>(t.src) + at, n, t.vec_src)
-                      : chunk_squares(static_cast<const float*>(t.src) + at, n, t.vec_src);
+    s += t.dtype == 1 ? chunk_squares<bf16_t, NT>(static_cast<const bf16_t*>(t.src) + at, n, t.vec_src)
+                      : chunk_squares<float, NT>(static_cast<const float*>(t.src) + at, n, t.vec_src);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -90,7 +97,7 @@ __global__ __launch_bounds__(kBlock) void grad_finish_kernel(const double* part,
   }
 }
 
-template <class T>
+template <class T, bool NT>
 __device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, bool vec, float scale) {
   constexpr int PE = Chunk<T>::kElems;
   int64_t done = 0;
@@ -102,7 +109,7 @@ __device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, boo
       u32x4 v[kGradUnroll];
 #pragma unroll
       for (int u = 0; u < kGradUnroll; ++u)
-        if (i + u * kBlock < pieces) v[u] = q[i + u * kBlock];
+        if (i + u * kBlock < pieces) v[u] = load_piece<NT>(q + i + u * kBlock);
 #pragma unroll
       for (int u = 0; u < kGradUnroll; ++u) {
         if (i + u * kBlock >= pieces) continue;
@@ -110,7 +117,8 @@ __device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, boo
         Chunk<T>::unpack(v[u], f);
 #pragma unroll
         for (int e = 0; e < PE; ++e) f[e] *= scale;
-        o[i + u * kBlock] = Chunk<T>::pack(f);
+        if constexpr (NT) __builtin_nontemporal_store(Chunk<T>::pack(f), o + i + u * kBlock);
+        else o[i + u * kBlock] = Chunk<T>::pack(f);
       }
     }
     done = pieces * PE;
@@ -122,6 +130,7 @@ __device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, boo
   }
 }
 
+template <bool NT>
 __global__ __launch_bounds__(kBlock) void grad_scale_kernel(GradList l, const double* sumsq, float max_norm, float* norm) {
   const double nm = sqrt(*sumsq);
   // a NaN norm makes the scale NaN
@@ -133,16 +142,17 @@ __global__ __launch_bounds__(kBlock) void grad_scale_kernel(GradList l, const do
     const int64_t at = static_cast<int64_t>(c - t.first) * kGradChunk;
     const int64_t n = min(static_cast<int64_t>(kGradChunk), t.n - at);
     if (t.dtype == 1)
-      chunk_scale(static_cast<const bf16_t*>(t.src) + at, static_cast<bf16_t*>(t.dst) + at, n, t.vec_both, scale);
+      chunk_scale<bf16_t, NT>(static_cast<const bf16_t*>(t.src) + at, static_cast<bf16_t*>(t.dst) + at, n, t.vec_both, scale);
     else
-      chunk_scale(static_cast<const float*>(t.src) + at, static_cast<float*>(t.dst) + at, n, t.vec_both, scale);
+      chunk_scale<float, NT>(static_cast<const float*>(t.src) + at, static_cast<float*>(t.dst) + at, n, t.vec_both, scale);
   }
 }
 
 }  // namespace
 
-hipError_t launch_grad_squares(const GradList& l, double* part, hipStream_t st) {
-  grad_squares_kernel<<<grad_blocks(l.chunks), kBlock, 0, st>>>(l, part);
+hipError_t launch_grad_squares(const GradList& l, bool nt, double* part, hipStream_t st) {
+  if (nt) grad_squares_kernel<true><<<grad_blocks(l.chunks), kBlock, 0, st>>>(l, part);
+  else grad_squares_kernel<false><<<grad_blocks(l.chunks), kBlock, 0, st>>>(l, part);
   return hipGetLastError();
 }
 
@@ -151,8 +161,10 @@ hipError_t launch_grad_finish(const double* part, int n, double* sumsq, float* n
   return hipGetLastError();
 }
 
-hipError_t launch_grad_scale(const GradList& l, const double* sumsq, float max_norm, float* norm, hipStream_t st) {
-  grad_scale_kernel<<<l.chunks > 0 ? grad_blocks(l.chunks) : 1, kBlock, 0, st>>>(l, sumsq, max_norm, norm);
+hipError_t launch_grad_scale(const GradList& l, bool nt, const double* sumsq, float max_norm, float* norm, hipStream_t st) {
+  const int blocks = l.chunks > 0 ? grad_blocks(l.chunks) : 1;
+  if (nt) grad_scale_kernel<true><<<blocks, kBlock, 0, st>>>(l, sumsq, max_norm, norm);
+  else grad_scale_kernel<false><<<blocks, kBlock, 0, st>>>(l, sumsq, max_norm, norm);
   return hipGetLastError();
 }
 

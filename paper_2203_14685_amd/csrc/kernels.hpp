@@ -305,7 +305,7 @@ hipError_t launch_layer(const LayerArgs& a, hipStream_t st);
 
 // Gradients by chunks (grads.hip).  A list holds as many tensors as fit a launch's
 // arguments; longer ones take several launches.
-constexpr int kGradChunk = 16384;
+constexpr int kGradChunk = 8192;
 constexpr int kGradListMax = 64;
 constexpr int kGradMaxBlocks = 2048;
 struct GradTensor {
@@ -320,8 +320,9 @@ struct GradList {
   int n, chunks;
 };
 inline int grad_blocks(int chunks) { return chunks < kGradMaxBlocks ? chunks : kGradMaxBlocks; }
-hipError_t launch_grad_squares(const GradList& l, double* part, hipStream_t st);
+// nt: non-temporal accesses (the whole call's tensors exceed the Infinity Cache).
+hipError_t launch_grad_squares(const GradList& l, bool nt, double* part, hipStream_t st);
 hipError_t launch_grad_finish(const double* part, int n, double* sumsq, float* norm, hipStream_t st);
-hipError_t launch_grad_scale(const GradList& l, const double* sumsq, float max_norm, float* norm, hipStream_t st);
+hipError_t launch_grad_scale(const GradList& l, bool nt, const double* sumsq, float max_norm, float* norm, hipStream_t st);
 
 }  // namespace hetumoe

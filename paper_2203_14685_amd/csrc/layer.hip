@@ -245,13 +245,12 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) 
     }
   };
   // no more row tiles than the list has: matrix units idle beside them cost nothing, but
-  // in fp32 the products of 64 rows take longer than the weights that they share
+  // in fp32 the products of 48 rows take longer than the weights that they share
   for (int r0 = 0; r0 < n; r0 += 16 * MAXT) {
     const int left = n - r0;
     if (MAXT == 1 || left <= 16) run(ExpertInt<1>(), r0);
     else if (MAXT == 2 || left <= 32) run(ExpertInt<(MAXT > 1 ? 2 : 1)>(), r0);
-    else if (MAXT == 3 || left <= 48) run(ExpertInt<(MAXT > 2 ? 3 : 1)>(), r0);
-    else run(ExpertInt<(MAXT > 3 ? 4 : 1)>(), r0);
+    else run(ExpertInt<(MAXT > 2 ? 3 : 1)>(), r0);
   }
 }
 
@@ -371,7 +370,7 @@ hipError_t strip(const LayerArgs& a, int z, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Strips of 256 bytes by eight waves; of 128 bytes by sixteen where the wide ones are
+// Strips of 256 bytes by four waves; of 128 bytes by sixteen where the wide ones are
 // too few to occupy the chip and few rows leave the registers for it.
 bool narrow(const LayerArgs& a, bool first) {
   const int elt = a.dtype == 1 ? 2 : 4;
@@ -388,9 +387,11 @@ hipError_t strips(const LayerArgs& a, hipStream_t st) {
   // second pass over their weights: fewer tiles leave room for more waves
   const int64_t rows = std::min<int64_t>(a.S, 2 * ((static_cast<int64_t>(a.S) * a.k + a.E - 1) / a.E));
   if (rows <= 16) return strip<T, 16, 1, 4, FIRST>(a, z, st);
-  if (rows <= 64) return strip<T, 16, 2, 8, FIRST>(a, z, st);
-  // 48 rows are what the registers hold in bf16
-  return strip<T, 16, sizeof(T) == 2 ? 3 : 4, 8, FIRST>(a, z, st);
+  if (rows <= 32) return strip<T, 16, 2, 4, FIRST>(a, z, st);
+  // (16 experts of 1024 x 4096 in fp32, 100 tokens of four choices: 48 rows by four waves 75
+  // and 69 us, 32 rows, where some experts take two passes, 87 and 92).  In bf16 eight
+  // waves: four would leave a SIMD one.
+  return strip<T, 16, 3, sizeof(T) == 2 ? 8 : 4, FIRST>(a, z, st);
 }
 
 template <class T>
@@ -411,7 +412,7 @@ int layer_splits(const LayerArgs& a) {
   const bool nar = narrow(a, false);
   const int64_t slots = a.by_choice ? a.S * a.k : a.E;
   const int64_t blocks = slots * ((static_cast<int64_t>(a.d) * elt + (nar ? 127 : 255)) / (nar ? 128 : 256));
-  const int64_t most = a.h / (kStep * 4 * (nar ? 16 : 8));
+  const int64_t most = a.h / (kStep * 4 * (nar ? 16 : 4));
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, most, 512 / std::max<int64_t>(1, blocks)})));
 }
 
