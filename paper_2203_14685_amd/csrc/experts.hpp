@@ -68,12 +68,12 @@ template <class T> constexpr int kExpertPe = 16 / static_cast<int>(sizeof(T));
 
 // Which 16-byte piece of its row lies at place `c` of LDS row `row`: piece c ^ swz.
 //   kRows: 8 pieces per 128-byte row; two rows fill the 64 banks.  A fragment read takes rows
-//          r .. r + 15 or, of the right operand in fp32, 4 i + t, i = 0..15.
+//          r .. r + 15 or, of the right operand in fp32, 4 i + t (with W = 32: 2 i + t), i = 0..15.
 //   kCols: bf16: a transpose read takes k rows 8 g + 4 h + 0..3, g = 0..3, of each 32
 //          contiguous bytes; fp32 reads run along a row and need no other order.
 template <class T, int KIND, bool RIGHT, int W>
 __device__ __forceinline__ int expert_swz(int row) {
-  if constexpr (KIND == kRows) return (RIGHT && sizeof(T) == 4 ? row >> 2 : row >> 1) & 7;
+  if constexpr (KIND == kRows) return (RIGHT && sizeof(T) == 4 && W > 32 ? row >> 2 : row >> 1) & 7;
   else if constexpr (sizeof(T) == 4) return 0;
   else if constexpr (W >= 128) return ((row & 3) << 1) | (row & 8);
   else return (((row >> 1) & 1) << 1) | ((row & 8) >> 1);
@@ -99,7 +99,8 @@ struct ExpertOperand {
   static constexpr int R = 64 / P;                       // rows per load
   // a lane's rows are R * WAVES apart: where that changes the order of the pieces, two offsets in turn
   static constexpr int kAlt = KIND == kCols && kElt == 2 && R * WAVES % 16 != 0 ? 2 : 1;
-  static_assert(KIND == kCols || R * WAVES % 32 == 0, "one order of the pieces per lane");
+  static_assert(KIND == kCols || R * WAVES % (RIGHT && kElt == 4 && W > 32 ? 32 : 16) == 0,
+                "one order of the pieces per lane");
   const char* base;   // (first row or column, k = 0), moved on by the stages
   int rows;           // kRows: bytes behind base that may be read
   int pitch;          // bytes per row of the matrix

@@ -3,8 +3,8 @@
 //
 // The order of K inside a product is free, so lane group g of a step of 16 takes
 // K 4 g .. 4 g + 3, one 16-byte read where rows run along K, and its i-th product
-// K 4 g + i; an operand whose rows run the other way is read four columns at a
-// time, tile j taking column 4 m + j, so a lane ends with 4 neighbouring columns.
+// K 4 g + i; an operand whose rows run the other way is read NT (2 or 4) columns at a
+// time, tile j taking column NT m + j, so a lane ends with 4 NT neighbouring columns.
 // Each 256 K are summed on their own and then added to the running sum.
 //
 // Small products leave most CUs idle, and a wave's sums over K are what they take: there
@@ -31,22 +31,23 @@ __device__ __forceinline__ f32x4 expert_left_f32(const float* lds, int x0, int k
   }
 }
 
-// Right operand: fb[j][i] is K 4 g + i of row (column) x0 + 4 m + j.
-template <int KIND, int W>
-__device__ __forceinline__ void expert_right_f32(const float* lds, int x0, int ks, int g, int m, f32x4 (&fb)[4]) {
+// Right operand: fb[j][i] is K 4 g + i of row (column) x0 + NT m + j.
+template <int KIND, int W, int NT>
+__device__ __forceinline__ void expert_right_f32(const float* lds, int x0, int ks, int g, int m, f32x4 (&fb)[NT]) {
+  typedef float fv __attribute__((ext_vector_type(NT)));
   if constexpr (KIND == kRows) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int row = x0 + 4 * m + j;
+    for (int j = 0; j < NT; ++j) {
+      const int row = x0 + NT * m + j;
       const int piece = (4 * ks + g) ^ expert_swz<float, KIND, true, W>(row);
       fb[j] = *reinterpret_cast<const f32x4*>(lds + row * kFBK + piece * 4);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(lds + (16 * ks + 4 * g + i) * W + x0 + 4 * m);
+      const fv v = *reinterpret_cast<const fv*>(lds + (16 * ks + 4 * g + i) * W + x0 + NT * m);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) fb[j][i] = v[j];
+      for (int j = 0; j < NT; ++j) fb[j][i] = v[j];
     }
   }
 }
@@ -55,8 +56,8 @@ template <int BM, int BN, int WM, int WN, int KG, int KA, int KB, int EPI, bool 
 __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(ExpertGemmArgs a) {
   constexpr int WAVES = WM * WN;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
-  static_assert(NT == 4, "64 columns per wave");
-  constexpr bool kSplit = EPI == kEpiAct && GATED;  // 32 columns of the gate and 32 of the other factor per wave
+  static_assert(NT == 4 || NT == 2, "64 or 32 columns per wave");
+  constexpr bool kSplit = EPI == kEpiAct && GATED;  // half of a wave's columns are the gate's
   constexpr int BNO = kSplit ? BN / 2 : BN;
   __shared__ __align__(1024) float A0_[KG * BM * kFBK], B0_[KG * BN * kFBK], A1_[KG * BM * kFBK], B1_[KG * BN * kFBK];
 
@@ -104,11 +105,11 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
             [&](int piece) { return m0 + piece * 4 < a.M ? m0 + piece * 4 : -1; });
     ob.init(reinterpret_cast<const float*>(a.B) + e * a.sB, a.ldb, n0, min(BN, a.N - n0), wave, [&](int piece) {
       if constexpr (kSplit) {
-        // lane group g of a wave ends with pieces 4 g .. 4 g + 3 of its 16: two of
-        // the gate, the same two of the other factor
-        const int pp = piece % 16;
-        const int c = n0 + (piece / 16) * 32 + ((pp / 4) * 2 + (pp & 1)) * 4;
-        return c < a.N ? c + (pp & 2 ? a.N : 0) : -1;
+        // lane group g of a wave ends with pieces NT g .. NT g + NT - 1 of its 4 NT: the
+        // first half of them the gate's, the same ones of the other factor
+        const int pp = piece % (4 * NT), t = pp % NT;
+        const int c = n0 + (piece / (4 * NT)) * 8 * NT + (pp / NT * (NT / 2) + t % (NT / 2)) * 4;
+        return c < a.N ? c + (t >= NT / 2 ? a.N : 0) : -1;
       } else {
         return n0 + piece * 4 < a.N ? n0 + piece * 4 : -1;
       }
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
 #pragma unroll
       for (int ks = 0; ks < kFBK / 16; ++ks) {
         f32x4 fb[NT], fa[MT];
-        expert_right_f32<KB, BN>(Bs, wn * 64, ks, g, m, fb);
+        expert_right_f32<KB, BN, NT>(Bs, wn * 16 * NT, ks, g, m, fb);
 #pragma unroll
         for (int i = 0; i < MT; ++i) fa[i] = expert_left_f32<KA, BM>(As, (wm * MT + i) * 16, ks, g, m);
 #pragma unroll
@@ -195,14 +196,14 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
   }
 
   if (kg > 0) continue;
-  // lane (g, m): row m of tile i, columns 16 g + 4 r + 0..3, r = 0..3
+  // lane (g, m): row m of tile i, columns 4 NT g + 4 r + 0..3, r = 0 .. NT - 1
   const int row0 = m0 + wm * MT * 16 + m;
-  const int col0 = n0 + (kSplit ? wn * 32 + 8 * g : wn * 64 + 16 * g);
-  auto value = [&](int i, int r, int q) { return sum[i][q][r]; };
+  const int col0 = n0 + (kSplit ? 2 * NT : 4 * NT) * (4 * wn + g);
+  auto value = [&](int i, int r, int q) { return sum[i][(4 * r + q) % NT][(4 * r + q) / NT]; };
   auto put = [](float* p, const float (&v)[4]) { *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]}; };
   if constexpr (EPI == kEpiStore) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < NT; ++r) {
       const int c = col0 + 4 * r;
       if (c >= a.N) continue;
       float bias[4];
@@ -220,7 +221,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
     }
   } else if constexpr (EPI == kEpiAct) {
     const int N1 = GATED ? 2 * a.N : a.N;
-    constexpr int R = kSplit ? 2 : 4;
+    constexpr int R = kSplit ? NT / 2 : NT;
     expert_by_act(a.act, [&](auto which) {
       constexpr int ACT = decltype(which)::v;
 #pragma unroll
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
             v[q] = row < rows ? value(i, r, q) + b0[q] : 0.f;
             f[q] = expert_act<ACT>(v[q]);
             if constexpr (kSplit) {
-              u[q] = row < rows ? value(i, r + 2, q) + b1[q] : 0.f;
+              u[q] = row < rows ? value(i, r + NT / 2, q) + b1[q] : 0.f;
               f[q] *= u[q];
             }
           }
@@ -262,7 +263,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
     expert_by_act(a.act, [&](auto which) {
       constexpr int ACT = decltype(which)::v;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
+      for (int r = 0; r < NT; ++r) {
         const int c = col0 + 4 * r;
         float s0[4] = {0.f, 0.f, 0.f, 0.f}, s1[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll

@@ -13,7 +13,8 @@ struct Tile {
 };
 
 template <class Fn>
-static hipError_t by_tile(const ExpertArgs& x, int M, int N, Fn fn) {
+static hipError_t by_tile(const ExpertArgs& x, int M, int N, int K, Fn fn) {
+  (void)K;
   // tiles of 256 x 256 once they fill the CUs, 64 x 256 where an expert has few
   // rows, else 128 x 128
   if (M <= 64) return fn(Tile<64, 256, 1, 4, 1>());

@@ -13,11 +13,17 @@ struct Tile {
 };
 
 template <class Fn>
-static hipError_t by_tile(const ExpertArgs& x, int M, int N, Fn fn) {
-  // tiles of 128 x 128 once they fill the CUs, else 64 x 64
-  const int64_t big = static_cast<int64_t>(x.E) * ((M + 127) / 128) * ((N + 127) / 128);
-  if (M > 64 && big >= 256) return fn(Tile<128, 128, 2, 2, 1, 2>());
-  return fn(Tile<64, 64, 4, 1, 4, 1>());
+static hipError_t by_tile(const ExpertArgs& x, int M, int N, int K, Fn fn) {
+  // Tiles of 128 x 128 once they fill the CUs, else of 64 x 64; for sums over 512 and more
+  // by four groups of waves, and where even these tiles are fewer than the CUs, of 32 x 32
+  // by eight: what a CU has on its way from memory is what such products wait for (8 x 128 x
+  // 256, K = 1024: one group 27 us, four 26, 32 x 32 by eight 12; 8 x 128 x 1024, K = 256: one
+  // group 13.6 us, four 17.4).
+  auto tiles = [&](int t) { return static_cast<int64_t>(x.E) * ((M + t - 1) / t) * ((N + t - 1) / t); };
+  if (M > 64 && tiles(128) >= 256) return fn(Tile<128, 128, 2, 2, 1, 2>());
+  if (K < 512) return fn(Tile<64, 64, 4, 1, 1, 4>());
+  if (tiles(64) >= 256) return fn(Tile<64, 64, 4, 1, 4, 1>());
+  return fn(Tile<32, 32, 2, 1, 8, 1>());
 }
 
 template <class TL, int KA, int KB, int EPI, bool GATED>
