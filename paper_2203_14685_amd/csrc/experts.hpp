@@ -218,6 +218,10 @@ __device__ __forceinline__ int expert_count(const int32_t* counts, int e, int C)
 // groups round the XCDs in order, so that experts of any load spread evenly (64 experts of
 // uneven load, one contiguous piece of the tiles per XCD: CUs busy 62 % of the time).
 // Tiles without rows in use, which are only cleared, come behind all others.
+//
+// Only the device knows the counts, and so how many tiles there are.  Where the last round
+// of tiles would leave half the CUs idle or more, a launch may leave it out (a.round); a
+// second one (a.quarters) then forms its tiles as four each.
 constexpr int kTileGroup = 32;
 constexpr int kMaxExperts = 1024;
 
@@ -230,6 +234,8 @@ constexpr int kTileList = 256;  // a block's next tiles, found together by its t
 template <int BM>
 struct ExpertTiles {
   int nv;    // tiles with work
+  int end;   // listed ones
+  int from;  // quarters: the first tile's number
   int used;  // slots per XCD that serve them
   int g;     // tiles per group
   int* before;  // LDS [E]: m tiles with work up to and with each expert (where counts cut M)
@@ -240,12 +246,13 @@ struct ExpertTiles {
     before = before_;
     rows = rows_;
     const int lane = lane_id();
+    const int rows_per = a.quarters ? 2 * BM : BM;
     int total = 0;
     if (threadIdx.x < kWave) {
       for (int e0 = 0; e0 < a.E; e0 += kWave) {
         const int e = e0 + lane;
         const int n = e < a.E ? expert_count(a.counts, e, a.C) : 0;
-        int sum = a.k_is_rows ? (e < a.E ? a.tm : 0) : (n + BM - 1) / BM;
+        int sum = a.k_is_rows ? (e < a.E ? a.tm : 0) : (n + rows_per - 1) / rows_per;
 #pragma unroll
         for (int s = 1; s < kWave; s <<= 1) {
           const int up = __shfl_up(sum, s);
@@ -260,15 +267,24 @@ struct ExpertTiles {
     }
     __syncthreads();
     nv = __builtin_amdgcn_readfirstlane(before[a.E - 1]) * a.tn;
-    g = nv >= 8 * kTileGroup ? kTileGroup : nv >= 8 ? (nv + 7) / 8 : 1;
-    used = ((nv + g - 1) / g + 7) / 8 * g;
+    end = nv;
+    from = 0;
+    if (a.round) {
+      const int last = nv % a.round, left_out = 2 * last <= a.round ? last : 0;
+      from = nv - left_out;
+      end = a.quarters ? 4 * left_out : from;
+    }
+    g = end >= 8 * kTileGroup ? kTileGroup : end >= 8 ? (end + 7) / 8 : 1;
+    used = ((end + g - 1) / g + 7) / 8 * g;
   }
 
   // The tile of slot j of XCD x; e = -1 behind the last one (and then for all later slots).
   __device__ __forceinline__ int4 slot_tile(const ExpertGemmArgs& a, int x, int j) const {
     const int q = j / g;
-    const int v = (q * 8 + x) * g + (j - q * g);
-    if (j >= used || v >= nv) return int4{-1, 0, 0, 0};
+    int v = (q * 8 + x) * g + (j - q * g);
+    if (j >= used || v >= end) return int4{-1, 0, 0, 0};
+    const int quarter = v % 4;
+    if (a.quarters) v = from + v / 4;
     int lo = 0, hi = a.E - 1;  // the first expert whose tiles end behind v
     while (lo < hi) {
       const int mid = (lo + hi) / 2;
@@ -278,12 +294,13 @@ struct ExpertTiles {
     const int first = lo > 0 ? before[lo - 1] : 0;
     const int mt = before[lo] - first;
     const int r = v - first * a.tn;
+    if (a.quarters) return int4{lo, 2 * (r % mt) + quarter % 2, 2 * (r / mt) + quarter / 2, 0};
     return int4{lo, r % mt, r / mt, 0};
   }
 
   // Tile `i` of those without work.
   __device__ __forceinline__ bool clear(const ExpertGemmArgs& a, int i, ExpertTile& t) const {
-    return i < a.tiles - nv && find(a, i, true, t);
+    return !a.quarters && i < a.tiles - nv && find(a, i, true, t);
   }
 
   __device__ __forceinline__ bool find(const ExpertGemmArgs& a, int want, bool empty, ExpertTile& t) const {

@@ -83,6 +83,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   int slot = blockIdx.x / 8;  // of the list's first tile
   ExpertTiles<BM> tiles;
   tiles.init(a, tile_before, tile_rows);
+  if (a.quarters && tiles.end == 0) return;
   auto list_tiles = [&]() {
     for (int i = threadIdx.x; i < kTileList; i += WAVES * kWave) tile_list[i] = tiles.slot_tile(a, xcd, slot + i * step);
     __syncthreads();
@@ -96,7 +97,8 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   auto aim = [&](bool any, const ExpertTile& t) {
     const int n = any ? __builtin_amdgcn_readfirstlane(tile_rows[t.e]) : 0;
     const int m0 = t.bm * BM, n0 = t.bn * BNO;
-    const int K = a.k_is_rows ? n : any ? a.K : 0;
+    // a quarter tile may lie behind the rows in use: zeros are all it writes
+    const int K = a.k_is_rows ? n : any && m0 < n ? a.K : 0;
     oa.init(reinterpret_cast<const bf16_t*>(a.A) + t.e * a.sA, a.lda, m0, a.k_is_rows ? BM : min(BM, n - m0), wave,
             [&](int piece) { return m0 + piece * 8 < a.M ? m0 + piece * 8 : -1; });
     ob.init(reinterpret_cast<const bf16_t*>(a.B) + t.e * a.sB, a.ldb, n0, min(BN, a.N - n0), wave, [&](int piece) {
@@ -237,7 +239,8 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   if (work) {
     // the first 128 K of the next tile are on their way before this one's results are
     // stored; behind the last tile: zeros, so that the count of loads stays the same
-    const int K = a.k_is_rows ? __builtin_amdgcn_readfirstlane(tile_rows[at.e]) : a.K;
+    const int n = __builtin_amdgcn_readfirstlane(tile_rows[at.e]);
+    const int K = a.k_is_rows ? n : at.bm * BM < n ? a.K : 0;
     if (++index == kTileList) {
       __syncthreads();
       slot += kTileList * step;

@@ -239,6 +239,9 @@ struct ExpertGemmArgs {
   int M, N, K;              // of the product; N: columns of out (gated forward: of hidden)
   int k_is_rows;            // K is the expert's rows in use (weight gradients), else M is cut at them
   int tm, tn, tiles;        // blocks along M and N, all blocks
+  int round;                // blocks that run together if the last, partly filled round of
+                            // tiles is left to another launch in quarter tiles, else 0
+  int quarters;             // this is that other launch
   const int32_t* counts;    // [E] or null (all C)
   const void *A, *B;
   int64_t sA, sB, sO;       // elements from one expert's matrix to the next
