@@ -68,11 +68,13 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
   constexpr bool kSplit = EPI == kEpiAct && GATED;
   constexpr int BNO = kSplit ? BN / 2 : BN;
-  constexpr bool kRing = KA == kCols && KB == kCols;  // four stages of half the length
+  constexpr bool kDeep = BM * BN <= 64 * 128;                   // four stages
+  constexpr bool kRing = !kDeep && KA == kCols && KB == kCols;  // four stages of half the length
   constexpr int BK = kRing ? kEBK / 2 : kEBK;
+  constexpr int kTurn = kDeep ? 4 * kEBK : 2 * kEBK;  // K elements in which all stages had their turn
   __shared__ __align__(1024) bf16_t A0[BM * BK], A1[BM * BK], B0[BN * BK], B1[BN * BK];
-  __shared__ __align__(1024) bf16_t A2[kRing ? BM * BK : 8], A3[kRing ? BM * BK : 8];
-  __shared__ __align__(1024) bf16_t B2[kRing ? BN * BK : 8], B3[kRing ? BN * BK : 8];
+  __shared__ __align__(1024) bf16_t A2[kDeep || kRing ? BM * BK : 8], A3[kDeep || kRing ? BM * BK : 8];
+  __shared__ __align__(1024) bf16_t B2[kDeep || kRing ? BN * BK : 8], B3[kDeep || kRing ? BN * BK : 8];
   __shared__ int tile_before[kMaxExperts], tile_rows[kMaxExperts];
   __shared__ int4 tile_list[kTileList];
 
@@ -190,22 +192,28 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   // The stage in (As, Bs), its first half in fa and fb; the next one in (An, Bn).
   auto stage = [&](auto read_last, bf16_t* As, bf16_t* Bs, const bf16_t* An, const bf16_t* Bn) __attribute__((always_inline)) {
     half(ExpertInt<1>(), ExpertInt<-1>(), fb, fn, nullptr, nullptr, As, Bs, 1);
-    half(read_last, ExpertInt<0>(), fn, fb, As, Bs, An, Bn, 0);
-    fresh = false;
+    half(read_last, ExpertInt<kDeep ? 2 * kLoads : 0>(), fn, fb, As, Bs, An, Bn, 0);
+    if (!kDeep) fresh = false;
   };
   // One of four stages, in fa and cur.
   auto quarter = [&](auto read, u32x4 (&cur)[NT], u32x4 (&next)[NT], bf16_t* As, bf16_t* Bs, const bf16_t* An,
                      const bf16_t* Bn) __attribute__((always_inline)) {
     half(read, ExpertInt<2 * kLoads>(), cur, next, As, Bs, An, Bn, 0);
   };
-  // 128 K elements.
-  auto four_halves = [&](auto read_last) __attribute__((always_inline)) {
+  // All stages' turn.
+  auto turn = [&](auto read_last) __attribute__((always_inline)) {
     if constexpr (kRing) {
       quarter(ExpertInt<1>(), fb, fn, A0, B0, A1, B1);
       quarter(ExpertInt<1>(), fn, fb, A1, B1, A2, B2);
       quarter(ExpertInt<1>(), fb, fn, A2, B2, A3, B3);
       fresh = false;
       quarter(read_last, fn, fb, A3, B3, A0, B0);
+    } else if constexpr (kDeep) {
+      stage(ExpertInt<1>(), A0, B0, A1, B1);
+      stage(ExpertInt<1>(), A1, B1, A2, B2);
+      stage(ExpertInt<1>(), A2, B2, A3, B3);
+      fresh = false;
+      stage(read_last, A3, B3, A0, B0);
     } else {
       stage(ExpertInt<1>(), A0, B0, A1, B1);
       stage(read_last, A1, B1, A0, B0);
@@ -219,7 +227,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     aim(true, at);
     load(A0, B0);
     load(A1, B1);
-    if constexpr (kRing) {
+    if constexpr (kDeep || kRing) {
       load(A2, B2);
       load(A3, B3);
       expert_stage_barrier<3 * kLoads>();
@@ -237,7 +245,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
 #pragma unroll
     for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (work) {
-    // the first 128 K of the next tile are on their way before this one's results are
+    // the first stages of the next tile are on their way before this one's results are
     // stored; behind the last tile: zeros, so that the count of loads stays the same
     const int n = __builtin_amdgcn_readfirstlane(tile_rows[at.e]);
     const int K = a.k_is_rows ? n : at.bm * BM < n ? a.K : 0;
@@ -253,9 +261,9 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     for (int j = 0; j < NT; ++j) fb[j] = rb.read(B0, at_b, 0, j);
 #pragma unroll
     for (int i = 0; i < MT; ++i) fa[i] = ra.read(A0, at_a, 0, i);
-    for (int k = 2 * kEBK; k < K; k += 2 * kEBK) four_halves(ExpertInt<1>());
+    for (int k = kTurn; k < K; k += kTurn) turn(ExpertInt<1>());
     aim(more, next);
-    four_halves(ExpertInt<0>());
+    turn(ExpertInt<0>());
     // the last sums leave the matrix unit before they are read
     asm volatile("s_nop 15\n\ts_nop 15" ::: "memory");
   }

@@ -15,14 +15,17 @@ struct Tile {
 // Rounds of tiles up to which the last one is worth a launch of its own.
 constexpr int kMaxRounds = 16;
 
+using SMALL = Tile<64, 64, 2, 1, 2>;
 template <class Fn>
 static hipError_t by_tile(const ExpertArgs& x, int M, int N, int K, Fn fn) {
   (void)K;
   // tiles of 256 x 256 once they fill the CUs, 64 x 256 where an expert has few
   // rows, else 128 x 128
-  if (M <= 64) return fn(Tile<64, 256, 1, 4, 1>());
+  if (M <= 64) return fn(SMALL());
   const int64_t big = static_cast<int64_t>(x.E) * ((M + 255) / 256) * ((N + 255) / 256);
   if (big >= 256) return fn(Tile<256, 256, 2, 4, 1>());
+  const int64_t mid = static_cast<int64_t>(x.E) * ((M + 127) / 128) * ((N + 127) / 128);
+  if (mid < 256) return fn(SMALL());
   return fn(Tile<128, 128, 2, 2, 2>());
 }
 
