@@ -4,7 +4,7 @@
 namespace hetumoe {
 
 hipError_t expert_act_bf16(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st) {
-  return by_tile(x, a.M, x.gated ? 2 * a.N : a.N, a.K, [&](auto tile) {
+  return by_tile(x, a.M, x.gated ? 2 * a.N : a.N, [&](auto tile) {
     using TL = decltype(tile);
     return x.gated ? launch_tile_bf16<TL, kRows, kCols, kEpiAct, true>(x, a, st)
                    : launch_tile_bf16<TL, kRows, kCols, kEpiAct, false>(x, a, st);

@@ -12,21 +12,23 @@ struct Tile {
   static constexpr int bm = BM, bn = BN, wm = WM, wn = WN, per_cu = PER;
 };
 
-// Rounds of tiles up to which the last one is worth a launch of its own.
+// Rounds of tiles up to which the last one is worth a launch of its own, which costs 4 to 5 us
+// where it finds nothing to do (dxe of 16 x 1280 x 1024 x 4096 gated, 1024 rows in use: 407 us in
+// whole tiles, 237 + 108 with the second round in quarters).
 constexpr int kMaxRounds = 16;
 
-using SMALL = Tile<64, 64, 2, 1, 2>;
+// Tiles of 256 x 256 once they fill the CUs (dw of 64 x 512 x 2048 x 8192: 1.12 ms, 128 x 128
+// 1.47; 8 x 1024 x 1024 x 1024, where they do not: forward 52 us, 128 x 128 47), of 128 x 128
+// once those do, and else, or where an expert has few rows, of 64 x 64, whose four stages
+// keep memory busy from few blocks (forward of 8 x 128 x 1024 x 4096 44 us, 128 x 128 61; of
+// 32 x 128 x 1024 x 1024, where 128 x 128 fill the CUs, 45 and 35; dpre of 36 x 2 x 64, K =
+// 2760: 21 us, two stages of 64 x 256 35).
 template <class Fn>
-static hipError_t by_tile(const ExpertArgs& x, int M, int N, int K, Fn fn) {
-  (void)K;
-  // tiles of 256 x 256 once they fill the CUs, 64 x 256 where an expert has few
-  // rows, else 128 x 128
-  if (M <= 64) return fn(SMALL());
-  const int64_t big = static_cast<int64_t>(x.E) * ((M + 255) / 256) * ((N + 255) / 256);
-  if (big >= 256) return fn(Tile<256, 256, 2, 4, 1>());
-  const int64_t mid = static_cast<int64_t>(x.E) * ((M + 127) / 128) * ((N + 127) / 128);
-  if (mid < 256) return fn(SMALL());
-  return fn(Tile<128, 128, 2, 2, 2>());
+static hipError_t by_tile(const ExpertArgs& x, int M, int N, Fn fn) {
+  auto tiles = [&](int t) { return static_cast<int64_t>(x.E) * ((M + t - 1) / t) * ((N + t - 1) / t); };
+  if (M > 64 && tiles(256) >= 256) return fn(Tile<256, 256, 2, 4, 1>());
+  if (M > 64 && tiles(128) >= 256) return fn(Tile<128, 128, 2, 2, 2>());
+  return fn(Tile<64, 64, 2, 1, 2>());
 }
 
 template <class TL, int KA, int KB, int EPI, bool GATED>

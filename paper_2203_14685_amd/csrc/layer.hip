@@ -127,8 +127,9 @@ struct StripSums {
 
 // One expert's strip: the rows of A that `list` names times NB columns of its matrix.
 // FIRST: A = x (row list / k), out = hidden; else A = hidden (row list), out = partial sums.
+// Rows past those that fit the registers take further passes, dealt to `shares` blocks.
 template <class T, int CB, int MAXT, int WAVES, bool FIRST, bool GATED>
-__global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) {
+__global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a, int shares) {
   constexpr int ELT = static_cast<int>(sizeof(T));
   constexpr int NC = CB / ELT, NB = 16 * NC;   // columns per lane and strip
   constexpr bool kSplit = FIRST && GATED;      // half of the strip's lanes take the gate's columns
@@ -185,7 +186,8 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) 
     }
     list = lists;
   }
-  if (n == 0) return;
+  const int share = blockIdx.z % shares, z = blockIdx.z / shares, zs = gridDim.z / shares;
+  if (n <= 16 * MAXT * share) return;
 
   const int K = FIRST ? a.d : a.h;
   const int N = FIRST ? a.h : a.d;             // columns of the output
@@ -207,7 +209,7 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) 
       arow[i] = li < n ? (FIRST ? list[li] / a.k : list[li]) * K * ELT : -1;
     }
     StripSums<T, CB, MT> sums;
-    sums.run(wsrc, wcol, N1 * ELT, asrc, arow, K, blockIdx.z * WAVES + wave, gridDim.z * WAVES);
+    sums.run(wsrc, wcol, N1 * ELT, asrc, arow, K, z * WAVES + wave, zs * WAVES);
 
     // added over the waves, 16 rows at a time
 #pragma unroll
@@ -238,7 +240,7 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) 
           if constexpr (ELT == 2) out->bits = static_cast<uint16_t>(f32_to_bf16_bits(f));
           else *out = f;
         } else {
-          a.part[(static_cast<int64_t>(blockIdx.z) * choices + list[li]) * N + n0 + c] = v;
+          a.part[(static_cast<int64_t>(z) * choices + list[li]) * N + n0 + c] = v;
         }
       }
       __syncthreads();
@@ -246,7 +248,7 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a) 
   };
   // no more row tiles than the list has: matrix units idle beside them cost nothing, but
   // in fp32 the products of 48 rows take longer than the weights that they share
-  for (int r0 = 0; r0 < n; r0 += 16 * MAXT) {
+  for (int r0 = 16 * MAXT * share; r0 < n; r0 += 16 * MAXT * shares) {
     const int left = n - r0;
     if (MAXT == 1 || left <= 16) run(ExpertInt<1>(), r0);
     else if (MAXT == 2 || left <= 32) run(ExpertInt<(MAXT > 1 ? 2 : 1)>(), r0);
@@ -361,12 +363,16 @@ hipError_t strip(const LayerArgs& a, int z, hipStream_t st) {
   constexpr int NB = 16 * CB / static_cast<int>(sizeof(T));
   const int slots = a.by_choice ? a.S * a.k : a.E;
   const int N = FIRST ? a.h : a.d;
-  if (FIRST && a.gated) {
-    layer_strip_kernel<T, CB, MT, WAVES, FIRST, true>
-        <<<dim3((N + NB / 2 - 1) / (NB / 2), slots, z), WAVES * kWave, 0, st>>>(a);
-  } else {
-    layer_strip_kernel<T, CB, MT, WAVES, FIRST, false><<<dim3((N + NB - 1) / NB, slots, z), WAVES * kWave, 0, st>>>(a);
-  }
+  const int nbo = FIRST && a.gated ? NB / 2 : NB;
+  const int64_t blocks = static_cast<int64_t>((N + nbo - 1) / nbo) * slots * z;
+  // passes side by side where the blocks are fewer than two per CU (bf16, 256 tokens of one
+  // choice, 2 experts of 1024 x 4096: the layer 80 -> 47 us; 8 experts of 1024 x 2048, two
+  // choices: 64 -> 51), one after the other on the same weights where they are more
+  const int passes = (a.S + 16 * MT - 1) / (16 * MT);
+  const int shares = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(passes, 512 / blocks)));
+  const dim3 grid((N + nbo - 1) / nbo, slots, z * shares);
+  if (FIRST && a.gated) layer_strip_kernel<T, CB, MT, WAVES, FIRST, true><<<grid, WAVES * kWave, 0, st>>>(a, shares);
+  else layer_strip_kernel<T, CB, MT, WAVES, FIRST, false><<<grid, WAVES * kWave, 0, st>>>(a, shares);
   return hipGetLastError();
 }
 
