@@ -113,6 +113,90 @@ def test_large_tiles(dtype, E, C, d, h, act, gated):
         check(g[key], ref[key], key)
 
 
+def _both_ways(dtype, E, C, d, h, act, gated, counts, seed):
+    """Forward and backward, rows behind the counts NaN, against the oracle."""
+    rng, x, xv, ((w1, w1v), (b1, b1v), (w2, w2v), (b2, b2v)), _ = _setup(E, C, d, h, dtype, gated, seed, garbage=False)
+    dye, dv = normal(rng, (E, C, d), dtype)
+    dye = dye.to(DEV)
+    cd = None
+    if counts is not None:
+        cd = torch.from_numpy(counts).to(DEV)
+        for e in range(E):
+            x[e, counts[e]:] = float("nan")
+            dye[e, counts[e]:] = float("nan")
+    o = hm.experts(x, w1, w2, b1=b1, b2=b2, counts=cd, act=ACTS[act], gated=gated, want_pre=True)
+    torch.cuda.synchronize()
+    ref = ox.experts(xv, w1v, b1v, w2v, b2v, counts, ACTS[act], gated, ROUND[dtype])
+    for key in ("pre", "hidden", "ye"):
+        check(o[key], ref[key], key)
+    g = hm.experts_bwd(dye, x, w1, w2, o["pre"], o["hidden"], counts=cd, act=ACTS[act], gated=gated)
+    torch.cuda.synchronize()
+    ref = ox.experts_bwd(dv, xv, w1v, w2v, counts, f64(o["pre"]), f64(o["hidden"]), ACTS[act], gated, ROUND[dtype])
+    for key in ("dxe", "dw1", "db1", "dw2", "db2"):
+        check(g[key], ref[key], key)
+
+
+@pytest.mark.parametrize("full,act,gated", [(70, "gelu", False), (35, "silu", True), (30, "relu", False)])
+def test_last_round_of_tiles(full, act, gated):
+    """bf16 tiles of 256 x 256 in every product, with a last round that fills less than half of 256
+    CUs: 280 tiles where all experts are full (of the gated first product: where half of them are),
+    120 where 30 are.  The experts' second row of tiles holds 4 rows, its lower half none."""
+    E, C, d, h = 70, 260, 400, 400
+    counts = np.zeros(E, dtype=np.int32)
+    counts[E - full:] = C
+    counts[E - full:E - full + 3] = (C - 1, C - 2, C - 3) if full < E else C
+    announce(f"experts_last_round bf16 E={E} C={C} d={d} h={h} full={full} {act} gated={gated}")
+    _both_ways("bf16", E, C, d, h, act, gated, None if full == E else counts, 51)
+
+
+@pytest.mark.parametrize("E,C,d,h,act,gated", [(16, 100, 512, 520, "silu", True), (9, 600, 512, 256, "gelu", False),
+                                               (2, 600, 40, 72, "relu", True)])
+def test_long_sums_in_fp32(E, C, d, h, act, gated):
+    """Sums over 512 and more elements in groups of waves, in every product."""
+    announce(f"experts_long f32 E={E} C={C} d={d} h={h} {act} gated={gated}")
+    _both_ways("f32", E, C, d, h, act, gated, _counts(np.random.default_rng(E), E, C), 53)
+
+
+def test_many_experts_and_more_tiles_than_a_list_holds():
+    """1024 experts of one row, 129 tiles each: more than 256 tiles for each of 512 blocks."""
+    E, C, d, h = 1024, 1, 8, 8256
+    announce(f"experts_many bf16 E={E} C={C} d={d} h={h}")
+    _, x, xv, ((w1, w1v), _, (w2, w2v), _), _ = _setup(E, C, d, h, "bf16", False, 57, bias=False, garbage=False)
+    counts = np.ones(E, dtype=np.int32)
+    counts[5] = 0
+    o = hm.experts(x, w1, w2, counts=torch.from_numpy(counts).to(DEV), want_pre=True)
+    torch.cuda.synchronize()
+    ref = ox.experts(xv, w1v, None, w2v, None, counts, ox.RELU, False, ROUND["bf16"])
+    for key in ("pre", "hidden", "ye"):
+        check(o[key], ref[key], key)
+
+
+def test_two_calls_at_once():
+    """Two streams run the same weights on their own rows at the same time, several times."""
+    E, C, d, h = 24, 200, 256, 512
+    runs = []
+    for seed in (61, 63):
+        rng, x, _, ((w1, _), (b1, _), (w2, _), (b2, _)), counts = _setup(E, C, d, h, "bf16", True, seed)
+        dye = normal(rng, (E, C, d), "bf16")[0].to(DEV)
+        runs.append((x, w1, b1, w2, b2, torch.from_numpy(counts).to(DEV), dye, torch.cuda.Stream()))
+
+    def run(x, w1, b1, w2, b2, cd, dye, _):
+        o = hm.experts(x, w1, w2, b1=b1, b2=b2, counts=cd, act=hm.MOE_ACT_SILU, gated=True, want_pre=True)
+        return {**o, **hm.experts_bwd(dye, x, w1, w2, o["pre"], o["hidden"], counts=cd, act=hm.MOE_ACT_SILU, gated=True)}
+
+    alone = [run(*r) for r in runs]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out = []
+        for r in runs:
+            with torch.cuda.stream(r[-1]):
+                out.append(run(*r))
+        torch.cuda.synchronize()
+        for a, b in zip(alone, out):
+            for key in a:
+                assert torch.equal(a[key], b[key]), key
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_optional_arguments(dtype):
     """No counts, no biases, no pre; each gradient asked for alone equals the one of all."""
