@@ -378,3 +378,27 @@ def test_training_step_of_a_layer(dtype):
         scale = 0.5 / total
         half = (ox.U_BF16 if t.dtype == torch.bfloat16 else ox.U32) + 3 * ox.U32
         check(t, (v * scale, np.abs(v * scale) * half + 1e-40), "clipped")
+
+
+def test_workspaces_of_a_call_on_another_stream():
+    """What a call with stream= allocates for itself is not handed out again before it ran."""
+    E, C, d, h = 4, 150, 64, 128
+    rng, x, _, ((w1, _), (b1, _), (w2, _), (b2, _)), counts = _setup(E, C, d, h, "bf16", False, 71)
+    cd = torch.from_numpy(counts).to(DEV)
+    pre, hid, dye = (normal(rng, s, "bf16")[0].to(DEV) for s in ((E, C, h), (E, C, h), (E, C, d)))
+    ref = hm.experts_bwd(dye, x, w1, w2, pre, hid, counts=cd)
+    grads = [ref["db1"], ref["db2"]]
+    total, _ = hm.grad_norm(grads)
+    side = torch.cuda.Stream()
+    size = hm.moe_experts_bwd_workspace_size(hm.experts_params(E, C, d, h, 0, False, hm.MOE_BF16))
+    for stream in (side, side.cuda_stream):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)  # the calls below are still waiting when they return
+        out = hm.experts_bwd(dye, x, w1, w2, pre, hid, counts=cd, stream=stream)
+        norm, sumsq = hm.grad_norm(grads, stream=stream)
+        junk = [torch.full((n,), 255, dtype=torch.uint8, device=DEV) for n in (size, size, 8, 16, 512, 4096)]
+        torch.cuda.synchronize()
+        for key in ref:
+            assert torch.equal(out[key], ref[key]), key
+        assert torch.equal(norm, total) and len(junk) == 6
