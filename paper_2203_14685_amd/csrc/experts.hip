@@ -9,16 +9,18 @@ namespace {
 constexpr int kSumRows = 256;  // rows of dye summed per block
 
 // Sums of kSumRows rows of dye: 16 lanes of one 16-byte piece each along the row, 16 row
-// groups; [E, ranges, d].
+// groups; [E, ranges, d].  Blocks along a row first, then the ranges, in one grid dimension (the
+// second holds 65536).
 template <class T>
 __global__ __launch_bounds__(kBlock) void experts_colsum_kernel(const T* dye, const int32_t* counts, float* part, int C,
                                                                 int d) {
   constexpr int PE = Chunk<T>::kElems;
   __shared__ float lds[16][16 * PE + 1];
   const int e = blockIdx.z, l = threadIdx.x % 16, r = threadIdx.x / 16;
-  const int c = (blockIdx.x * 16 + l) * PE;
+  const int strips = (d + 16 * PE - 1) / (16 * PE), range = blockIdx.x / strips, strip = blockIdx.x - range * strips;
+  const int c = (strip * 16 + l) * PE;
   const int cnt = expert_count(counts, e, C);
-  const int lo = blockIdx.y * kSumRows, hi = min(cnt, lo + kSumRows);
+  const int lo = range * kSumRows, hi = min(cnt, lo + kSumRows);
   float s[PE];
 #pragma unroll
   for (int q = 0; q < PE; ++q) s[q] = 0.f;
@@ -43,12 +45,12 @@ __global__ __launch_bounds__(kBlock) void experts_colsum_kernel(const T* dye, co
   for (int q = 0; q < PE; ++q) lds[r][l * PE + q] = s[q];
   __syncthreads();
   for (int i = threadIdx.x; i < 16 * PE; i += kBlock) {
-    const int col = blockIdx.x * 16 * PE + i;
+    const int col = strip * 16 * PE + i;
     if (col >= d) continue;
     float t = 0.f;
 #pragma unroll
     for (int q = 0; q < 16; ++q) t += lds[q][i];
-    part[(static_cast<int64_t>(e) * gridDim.y + blockIdx.y) * d + col] = t;
+    part[(static_cast<int64_t>(e) * (gridDim.x / strips) + range) * d + col] = t;
   }
 }
 
@@ -151,7 +153,7 @@ hipError_t launch_experts_bwd(const ExpertArgs& x, hipStream_t st) {
     PartSum s1{x.colsum, x.db1, expert_parts(x), x.db1 ? h1 : 0}, s2{x.rowsum, x.db2, expert_row_parts(x), x.db2 ? x.d : 0};
     if (x.db2 && rows) {
       const int pe = x.dtype == 1 ? 8 : 4;
-      const dim3 grid((x.d + 16 * pe - 1) / (16 * pe), s2.parts, x.E);
+      const dim3 grid((x.d + 16 * pe - 1) / (16 * pe) * s2.parts, 1, x.E);
       if (x.dtype == 1)
         experts_colsum_kernel<bf16_t><<<grid, kBlock, 0, st>>>(static_cast<const bf16_t*>(x.dye), x.counts, x.rowsum, x.C, x.d);
       else

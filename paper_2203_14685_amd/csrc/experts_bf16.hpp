@@ -290,9 +290,9 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   const int col0 = n0 + (kSplit ? wn * 32 : wn * 64) + 16 * (lg % 2) + 8 * (lg / 2);
   auto value = [&](int i, int p, int q) { return acc[i][2 * p + q / 4][q % 4]; };
   // byte of (lrow, column c) in rows of ld, or past everything
-  auto place = [&](int ld, int c, bool in) { return in ? (lrow * ld + c) * 2 : kExpertOob; };
-  auto put = [&](__amdgpu_buffer_rsrc_t r, int off, const float (&v)[8]) {
-    __builtin_amdgcn_raw_buffer_store_b128(Chunk<bf16_t>::pack(v), r, off, 0, 0);
+  auto place = [&](int ld, int c, bool in) { return static_cast<unsigned>(in ? (lrow * ld + c) * 2 : kExpertOob); };
+  auto put = [&](__amdgpu_buffer_rsrc_t r, unsigned off, const float (&v)[8]) {
+    __builtin_amdgcn_raw_buffer_store_b128(Chunk<bf16_t>::pack(v), r, static_cast<int>(off), 0, 0);
   };
   const int valid = min(BM, a.M - m0);  // rows of the output
   if constexpr (EPI == kEpiStore) {
@@ -349,7 +349,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
             }
           }
           if (a.pre) {
-            const int at_pre = place(N1, c, c < a.N) + i * 32 * N1;
+            const unsigned at_pre = place(N1, c, c < a.N) + i * 32 * N1;
             put(pre, at_pre, v);
             if constexpr (kSplit) put(pre, at_pre + 2 * a.N, u);
           }
@@ -368,7 +368,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       const int c = col0 + 32 * p;
-      const int off0 = place(N1, c, c < a.N);
+      const unsigned off0 = place(N1, c, c < a.N);
       constexpr int kRowsAhead = GATED && MT > 1 ? MT / 2 : MT;  // rows requested together
       float s0[8], s1[8];
 #pragma unroll
@@ -378,9 +378,9 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         u32x4 pv[kRowsAhead], pu[kRowsAhead];
 #pragma unroll
         for (int i = 0; i < kRowsAhead; ++i) {
-          const int off = off0 + (i0 + i) * 32 * N1;
+          const int off = static_cast<int>(off0 + (i0 + i) * 32 * N1);
           pv[i] = __builtin_amdgcn_raw_buffer_load_b128(pre, off, 0, 0);
-          if constexpr (GATED) pu[i] = __builtin_amdgcn_raw_buffer_load_b128(pre, off + 2 * a.N, 0, 0);
+          if constexpr (GATED) pu[i] = __builtin_amdgcn_raw_buffer_load_b128(pre, static_cast<int>(off + 2u * a.N), 0, 0);
         }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll

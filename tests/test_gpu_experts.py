@@ -402,3 +402,17 @@ def test_workspaces_of_a_call_on_another_stream():
         for key in ref:
             assert torch.equal(out[key], ref[key]), key
         assert torch.equal(norm, total) and len(junk) == 6
+
+
+def test_bias_gradient_of_more_row_ranges_than_a_grid_dimension():
+    """65537 ranges of 256 rows; the sums of a few rows of small whole numbers are exact."""
+    C = 65536 * 256 + 100
+    dye = torch.zeros((1, C, 8), dtype=torch.bfloat16, device=DEV)
+    for i, row in enumerate((0, 255, 70_000, 65536 * 256 - 1, 65536 * 256, C - 1)):
+        dye[0, row] = 2.0 ** i
+    p = hm.experts_params(1, C, 8, 8, hm.MOE_ACT_RELU, False, hm.MOE_BF16)
+    ws = torch.empty((hm.moe_experts_bwd_workspace_size(p),), dtype=torch.uint8, device=DEV)
+    db2 = torch.full((1, 8), -1.0, device=DEV)
+    hm.moe_experts_bwd(p, dye, None, None, None, None, None, None, None, None, None, None, db2, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(db2, torch.full_like(db2, 63.0))
