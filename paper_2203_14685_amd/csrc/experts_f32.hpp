@@ -18,34 +18,37 @@ namespace hetumoe {
 constexpr int kFBK = kExpertBk<float>;
 constexpr int kFSum = 8;  // stages summed on their own (a multiple of 2)
 
-// Left operand, step ks of 16: lane (g, m) gets K 4 g + 0..3 of row (column) x0 + m.
+// Left operand, step ks of 16: lane (g, m) gets K 4 g + 0..3 of row (column) x0 + m.  `off`:
+// of the group's part of the array.  (The array itself is passed, and added to once: only
+// so does the compiler see that loads on their way to the other stage's arrays are none of
+// this read's business, and does not wait for them.)
 template <int KIND, int W>
-__device__ __forceinline__ f32x4 expert_left_f32(const float* lds, int x0, int ks, int g, int m) {
+__device__ __forceinline__ f32x4 expert_left_f32(const float* lds, int off, int x0, int ks, int g, int m) {
   if constexpr (KIND == kRows) {
     const int row = x0 + m;
     const int piece = (4 * ks + g) ^ expert_swz<float, KIND, false, W>(row);
-    return *reinterpret_cast<const f32x4*>(lds + row * kFBK + piece * 4);
+    return *reinterpret_cast<const f32x4*>(lds + (off + row * kFBK + piece * 4));
   } else {
-    const float* p = lds + (16 * ks + 4 * g) * W + x0 + m;
+    const float* p = lds + (off + (16 * ks + 4 * g) * W + x0 + m);
     return f32x4{p[0], p[W], p[2 * W], p[3 * W]};
   }
 }
 
 // Right operand: fb[j][i] is K 4 g + i of row (column) x0 + NT m + j.
 template <int KIND, int W, int NT>
-__device__ __forceinline__ void expert_right_f32(const float* lds, int x0, int ks, int g, int m, f32x4 (&fb)[NT]) {
+__device__ __forceinline__ void expert_right_f32(const float* lds, int off, int x0, int ks, int g, int m, f32x4 (&fb)[NT]) {
   typedef float fv __attribute__((ext_vector_type(NT)));
   if constexpr (KIND == kRows) {
 #pragma unroll
     for (int j = 0; j < NT; ++j) {
       const int row = x0 + NT * m + j;
       const int piece = (4 * ks + g) ^ expert_swz<float, KIND, true, W>(row);
-      fb[j] = *reinterpret_cast<const f32x4*>(lds + row * kFBK + piece * 4);
+      fb[j] = *reinterpret_cast<const f32x4*>(lds + (off + row * kFBK + piece * 4));
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const fv v = *reinterpret_cast<const fv*>(lds + (16 * ks + 4 * g + i) * W + x0 + NT * m);
+      const fv v = *reinterpret_cast<const fv*>(lds + (off + (16 * ks + 4 * g + i) * W + x0 + NT * m));
 #pragma unroll
       for (int j = 0; j < NT; ++j) fb[j][i] = v[j];
     }
@@ -53,21 +56,19 @@ __device__ __forceinline__ void expert_right_f32(const float* lds, int x0, int k
 }
 
 template <int BM, int BN, int WM, int WN, int KG, int KA, int KB, int EPI, bool GATED>
-__global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(ExpertGemmArgs a) {
+__global__ __launch_bounds__(WM* WN* KG * 64, BM == 128 ? 2 : 4) void experts_gemm_f32_kernel(ExpertGemmArgs a) {
   constexpr int WAVES = WM * WN;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   static_assert(NT == 4 || NT == 2, "64 or 32 columns per wave");
   constexpr bool kSplit = EPI == kEpiAct && GATED;  // half of a wave's columns are the gate's
   constexpr int BNO = kSplit ? BN / 2 : BN;
-  __shared__ __align__(1024) float A0_[KG * BM * kFBK], B0_[KG * BN * kFBK], A1_[KG * BM * kFBK], B1_[KG * BN * kFBK];
-
+  __shared__ __align__(1024) float A0[KG * BM * kFBK], B0[KG * BN * kFBK], A1[KG * BM * kFBK], B1[KG * BN * kFBK];
   __shared__ int tile_before[kMaxExperts], tile_rows[kMaxExperts];
 
   const int lane = lane_id(), g = lane / 16, m = lane % 16;
-  const int kg = __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * kWave));
+  const int kg = KG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / (WAVES * kWave)) : 0;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) - kg * WAVES;
   const int wm = wave / WN, wn = wave % WN;
-  float *A0 = A0_ + kg * BM * kFBK, *B0 = B0_ + kg * BN * kFBK, *A1 = A1_ + kg * BM * kFBK, *B1 = B1_ + kg * BN * kFBK;
   const int xcd = blockIdx.x % 8, step = gridDim.x / 8;
   int slot = blockIdx.x / 8, idle = blockIdx.x;
   ExpertTiles<BM> tiles;
@@ -114,13 +115,13 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
         return n0 + piece * 4 < a.N ? n0 + piece * 4 : -1;
       }
     });
-    auto multiply = [&](const float* As, const float* Bs) {
+    auto multiply = [&](const float* As, const float* Bs) __attribute__((always_inline)) {
 #pragma unroll
       for (int ks = 0; ks < kFBK / 16; ++ks) {
         f32x4 fb[NT], fa[MT];
-        expert_right_f32<KB, BN, NT>(Bs, wn * 16 * NT, ks, g, m, fb);
+        expert_right_f32<KB, BN, NT>(Bs, kg * BN * kFBK, wn * 16 * NT, ks, g, m, fb);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) fa[i] = expert_left_f32<KA, BM>(As, (wm * MT + i) * 16, ks, g, m);
+        for (int i = 0; i < MT; ++i) fa[i] = expert_left_f32<KA, BM>(As, kg * BM * kFBK, (wm * MT + i) * 16, ks, g, m);
 #pragma unroll
         for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -144,9 +145,9 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
     ob.skip(kg);
     const int stages = (K + KG * kFBK - 1) / (KG * kFBK);  // per group
     int left = K - kg * kFBK;
-    auto load = [&](float* As, float* Bs) {
-      oa.load(As, wave, left);
-      ob.load(Bs, wave, left);
+    auto load = [&](float* As, float* Bs) __attribute__((always_inline)) {
+      oa.load(As, kg * oa.N * WAVES + wave, left);
+      ob.load(Bs, kg * ob.N * WAVES + wave, left);
       oa.skip(KG - 1);
       ob.skip(KG - 1);
       left -= KG * kFBK;
@@ -169,7 +170,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64) void experts_gemm_f32_kernel(Exper
     flush();
     if constexpr (KG > 1) {
       // the upper half of the groups hands its sums to the lower one, until one is left
-      float* part = A0_;
+      float* part = A0;
       static_assert(KG / 2 * WAVES * kWave * MT * NT * 4 <= KG * BM * kFBK, "room for half of the sums");
       const int at = wave * kWave + lane;
       auto place = [&](int q, int i, int j) {
