@@ -151,6 +151,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64, BM == 128 ? 2 : 4) void experts_ge
       oa.skip(KG - 1);
       ob.skip(KG - 1);
       left -= KG * kFBK;
+      __builtin_amdgcn_sched_barrier(0);  // ahead of the products, not just before the next barrier
     };
     load(A0, B0);
     int s = 0;
