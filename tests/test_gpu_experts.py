@@ -157,6 +157,14 @@ def test_long_sums_in_fp32(E, C, d, h, act, gated):
     _both_ways("f32", E, C, d, h, act, gated, _counts(np.random.default_rng(E), E, C), 53)
 
 
+@pytest.mark.parametrize("act,gated", [("gelu", False), ("silu", True)])
+def test_tiles_of_128_in_fp32(act, gated):
+    """512 and more tiles of 128 x 128 over 256 and more, cut at the edges, in every product."""
+    E, C, d, h = 64, 256, 500, 508
+    announce(f"experts_128 f32 E={E} C={C} d={d} h={h} {act} gated={gated}")
+    _both_ways("f32", E, C, d, h, act, gated, _counts(np.random.default_rng(59), E, C), 59)
+
+
 def test_many_experts_and_more_tiles_than_a_list_holds():
     """1024 experts of one row, 129 tiles each: more than 256 tiles for each of 512 blocks."""
     E, C, d, h = 1024, 1, 8, 8256
