@@ -68,7 +68,8 @@ template <class T> constexpr int kExpertPe = 16 / static_cast<int>(sizeof(T));
 
 // Which 16-byte piece of its row lies at place `c` of LDS row `row`: piece c ^ swz.
 //   kRows: 8 pieces per 128-byte row; two rows fill the 64 banks.  A fragment read takes rows
-//          r .. r + 15 or, of the right operand in fp32, 4 i + t (with W = 32: 2 i + t), i = 0..15.
+//          r .. r + 15 or, of the right operand in fp32, 4 i + t (with W = 32: 2 i + t), i = 0..15,
+//          in some order.
 //   kCols: bf16: a transpose read takes k rows 8 g + 4 h + 0..3, g = 0..3, of each 32
 //          contiguous bytes; fp32 reads run along a row and need no other order.
 template <class T, int KIND, bool RIGHT, int W>
