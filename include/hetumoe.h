@@ -529,15 +529,16 @@ MOE_API moe_status moe_token_layer_workspace_size(const moe_token_layer_params* 
  *   y[s] = sum_r weights[s,r] * expert_{ids[s,r]}(x[s])
  * with ids and weights by moe_gate's rules for the same parameters and inputs (its
  * logits' last bits may differ from a moe_gate call's, as between two batches), and
- * the expert networks of moe_experts (hidden rounded once to dtype).  Only the
- * weights of experts that a token chose are read.  fp32 sums, rounded once.
+ * the expert networks of moe_experts, but for bf16 with hidden kept as the sum of two
+ * bf16 (16 bits).  Only the weights of experts that a token chose are read.  fp32 sums,
+ * rounded once.
  *
  * Inputs   x [S,d], S <= MOE_TOKEN_LAYER_MAX; wg, bias, token_ids, noise, hash_table
  *          as moe_gate (x is required for HASH too); w1, b1, w2, b2 as moe_experts.
  *          With routed, ids [S,k] and weights [S,k] are inputs; an id outside [0, E)
  *          stands for no expert (padding) and adds nothing.
  * Outputs  y [S,d]; ids and weights [S,k] unless routed.
- * Range    d h1 and S k h elements within 2^31 bytes, else MOE_ERR_UNSUPPORTED.
+ * Range    d h1 elements and S k h of 4 bytes within 2^31 bytes, else MOE_ERR_UNSUPPORTED.
  * Workspace device memory of at least moe_token_layer_workspace_size() bytes,
  *          16-byte aligned; contents on entry are ignored.
  */

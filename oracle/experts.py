@@ -67,9 +67,11 @@ def _bias(v, err, b):
     return v + b, err + U32 * (np.abs(v) + np.abs(b) + err)
 
 
-def network(x, w1, b1, w2, b2, kind, gated, r):
+def network(x, w1, b1, w2, b2, kind, gated, r, terms=1):
     """One expert on rows x: dict of (value, bound) for pre, hidden, y; the stored ones
-    (pre and hidden) include their rounding, y its own."""
+    (pre and hidden) include their rounding, y its own.  With two terms hidden is the sum
+    of its rounding and the rounding of what that leaves, off by r^2, and the second
+    product has twice the terms."""
     h = w2.shape[0]
     pre, pe = _bias(*_product(x, w1, None, None), b1)
     if gated:
@@ -81,8 +83,8 @@ def network(x, w1, b1, w2, b2, kind, gated, r):
     else:
         hid = act(kind, pre)[0]
         he = act_error(kind, pre, pe)[0]
-    he = he + r * (np.abs(hid) + he)
-    y, ye = _bias(*_product(hid, w2, he, None), b2)
+    he = he + r ** terms * (np.abs(hid) + he)
+    y, ye = _bias(*_product(hid, w2, he, None, terms * h), b2)
     return dict(pre=(pre, pe + r * (np.abs(pre) + pe)), hidden=(hid, he), y=(y, ye + r * (np.abs(y) + ye)),
                 y_unrounded=(y, ye))
 
@@ -146,7 +148,7 @@ def token_layer(x, ids, weights, w1, b1, w2, b2, kind, gated, r):
         for e, w in zip(ids[s], weights[s]):
             if 0 <= e < E:
                 v, ve = network(x[s:s + 1], w1[e], None if b1 is None else b1[e], w2[e],
-                                None if b2 is None else b2[e], kind, gated, r)["y_unrounded"]
+                                None if b2 is None else b2[e], kind, gated, r, 2 if r else 1)["y_unrounded"]
                 y[s] += w * v[0]
                 err[s] += abs(w) * ve[0]
                 mag[s] += np.abs(w * v[0])

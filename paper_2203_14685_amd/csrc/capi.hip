@@ -886,7 +886,7 @@ moe_status check_token_layer(const moe_token_layer_params* p, const char* who) {
   // 32-bit offsets into one expert's matrices and into the rows
   const int64_t most = kI32Max - 65536, elt = static_cast<int64_t>(elt_size(g.dtype));
   const int64_t h1 = static_cast<int64_t>(p->h) * (p->gated ? 2 : 1);
-  if (g.d * h1 * elt > most || static_cast<int64_t>(g.S) * g.k * p->h * elt > most)
+  if (g.d * h1 * elt > most || static_cast<int64_t>(g.S) * g.k * p->h * 4 > most)
     return fail(MOE_ERR_UNSUPPORTED, "%s: an expert's matrix or the hidden rows exceed 2^31 bytes", who);
   return MOE_OK;
 }
@@ -907,7 +907,7 @@ TokenLayerPlan plan_token_layer(const moe_token_layer_params* p) {
   if (!p->routed && g.kind != MOE_GATE_HASH)
     w.gate = std::max(w.gate, static_cast<size_t>(layer_gate_splits(g.d)) * static_cast<size_t>(g.S) * static_cast<size_t>(g.E) * 4);
   w.off_hidden = align256(w.gate);
-  w.off_part = w.off_hidden + align256(choices * static_cast<size_t>(p->h) * elt_size(g.dtype));
+  w.off_part = w.off_hidden + align256(choices * static_cast<size_t>(p->h) * 4);  // bf16: the sum of two
   w.total = w.off_part + align256(static_cast<size_t>(a.z2) * choices * static_cast<size_t>(g.d) * 4);
   return w;
 }

@@ -283,7 +283,7 @@ struct LayerArgs {
   const float *b1, *b2;
   const int32_t* ids;       // [S, k]; outside [0, E): no expert
   const float* weights;     // [S, k]
-  void* hidden;             // workspace [S * k, h]
+  void* hidden;             // workspace [S * k, h], bf16: two of them that add up
   float* part;              // workspace [z2, S * k, d]
   void* y;                  // [S, d]
 };

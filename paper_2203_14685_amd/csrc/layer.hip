@@ -47,8 +47,9 @@ __device__ __forceinline__ void columns_of(const Piece<8>::T (&in)[8], u32x4 (&o
 
 // Sums of MT tiles of 16 rows of A times a strip of 16 NC columns of a matrix with K rows:
 // lane (g, m) holds rows 4 g + r of each tile, columns NC m + j.  A wave takes steps of
-// kStep rows of the matrix, from `step` on, `stride` apart.
-template <class T, int CB, int MT>
+// kStep rows of the matrix, from `step` on, `stride` apart.  TERMS 2: A is the sum of two
+// matrices, `plane` bytes apart.
+template <class T, int CB, int MT, int TERMS>
 struct StripSums {
   static constexpr int ELT = static_cast<int>(sizeof(T));
   static constexpr int NC = CB / ELT;
@@ -56,14 +57,14 @@ struct StripSums {
   typedef typename Piece<CB>::T piece_t;
   struct Regs {
     piece_t w[8];
-    u32x4 x[MT][AP];
+    u32x4 x[MT][TERMS * AP];
   };
   f32x4 acc[MT][NC];
 
   // wcol: byte of the lane's columns in a row of `pitch` bytes, or kExpertOob; arow: byte of
   // the lane's row of A per tile, or -1.
   __device__ __forceinline__ void run(__amdgpu_buffer_rsrc_t w, unsigned wcol, int pitch, __amdgpu_buffer_rsrc_t x,
-                                      const int (&arow)[MT], int K, int step, int stride) {
+                                      const int (&arow)[MT], int plane, int K, int step, int stride) {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -80,9 +81,11 @@ struct StripSums {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int q = 0; q < AP; ++q)
+        for (int q = 0; q < TERMS * AP; ++q) {
+          const int kq = k + q % AP * (16 / ELT);
           r.x[i][q] = __builtin_amdgcn_raw_buffer_load_b128(
-              x, arow[i] >= 0 && k + q * (16 / ELT) < K ? arow[i] + (k + q * (16 / ELT)) * ELT : kExpertOob, 0, 0);
+              x, arow[i] >= 0 && kq < K ? arow[i] + q / AP * plane + kq * ELT : kExpertOob, 0, 0);
+        }
     };
     auto multiply = [&](const Regs& r) __attribute__((always_inline)) {
       if constexpr (ELT == 2) {
@@ -91,9 +94,11 @@ struct StripSums {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
-          for (int j = 0; j < NC; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r.x[i][0]),
-                                                                __builtin_bit_cast(bf16x8, col[j]), acc[i][j], 0, 0, 0);
+          for (int q = 0; q < TERMS; ++q)
+#pragma unroll
+            for (int j = 0; j < NC; ++j)
+              acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, r.x[i][q]),
+                                                                  __builtin_bit_cast(bf16x8, col[j]), acc[i][j], 0, 0, 0);
       } else {
 #pragma unroll
         for (int i = 0; i < MT; ++i)
@@ -199,7 +204,11 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a, 
   const unsigned wcol = oc < N ? (oc + (kSplit && m >= 8 ? N : 0)) * ELT : kExpertOob;
   const __amdgpu_buffer_rsrc_t wsrc =
       expert_rsrc(reinterpret_cast<const T*>(FIRST ? a.w1 : a.w2) + static_cast<int64_t>(e) * K * N1, K * N1 * ELT);
-  const __amdgpu_buffer_rsrc_t asrc = expert_rsrc(FIRST ? a.x : a.hidden, (FIRST ? a.S : choices) * K * ELT);
+  // bf16: hidden as the sum of two, so that it keeps 16 bits on its way to the second product,
+  // which reads the weights all the same (one: y off by 1.4 times its own rounding)
+  constexpr int TERMS = ELT == 2 && !FIRST ? 2 : 1;
+  const int plane = choices * a.h * ELT;
+  const __amdgpu_buffer_rsrc_t asrc = expert_rsrc(FIRST ? a.x : a.hidden, FIRST ? a.S * K * ELT : TERMS * plane);
 
   // MT tiles of 16 rows of the list, from r0 on
   auto run = [&](auto tiles, int r0) {
@@ -210,8 +219,8 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a, 
       const int li = r0 + 16 * i + m;
       arow[i] = li < n ? (FIRST ? list[li] / a.k : list[li]) * K * ELT : -1;
     }
-    StripSums<T, CB, MT> sums;
-    sums.run(wsrc, wcol, N1 * ELT, asrc, arow, K, z * WAVES + wave, zs * WAVES);
+    StripSums<T, CB, MT, TERMS> sums;
+    sums.run(wsrc, wcol, N1 * ELT, asrc, arow, plane, K, z * WAVES + wave, zs * WAVES);
 
     // added over the waves, 16 rows at a time
 #pragma unroll
@@ -237,9 +246,14 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a, 
           expert_by_act(a.act, [&](auto which) { f = expert_act<decltype(which)::v>(v); });
           if constexpr (kSplit) f *= u;
           T* out = reinterpret_cast<T*>(a.hidden) + static_cast<int64_t>(list[li]) * N + n0 + c;
-          // rounded to the element type like the hidden rows of the experts call: the
-          // second product's operand
-          if constexpr (ELT == 2) out->bits = static_cast<uint16_t>(f32_to_bf16_bits(f));
+          if constexpr (ELT == 2) {
+            const uint32_t hi = f32_to_bf16_bits(f);
+            const float rest = f - __uint_as_float(hi << 16);
+            out->bits = static_cast<uint16_t>(hi);
+            // nothing is left of an infinity or a NaN
+            out[static_cast<int64_t>(choices) * a.h].bits =
+                (hi & 0x7f80u) == 0x7f80u ? uint16_t(0) : static_cast<uint16_t>(f32_to_bf16_bits(rest));
+          }
           else *out = f;
         } else {
           a.part[(static_cast<int64_t>(z) * choices + list[li]) * N + n0 + c] = v;
@@ -273,8 +287,8 @@ __global__ __launch_bounds__(kLayerGateWaves* kWave) void layer_logits_kernel(La
   const __amdgpu_buffer_rsrc_t w = expert_rsrc(a.wg, a.d * E * ELT), x = expert_rsrc(a.x, a.S * a.d * ELT);
   const int arow[1] = {tok0 + m < a.S ? (tok0 + m) * a.d * ELT : -1};
   const int col = n0 + CB / ELT * m;
-  StripSums<T, CB, 1> sums;
-  sums.run(w, col < E ? col * ELT : kExpertOob, E * ELT, x, arow, a.d, blockIdx.x * kLayerGateWaves + wave,
+  StripSums<T, CB, 1, 1> sums;
+  sums.run(w, col < E ? col * ELT : kExpertOob, E * ELT, x, arow, 0, a.d, blockIdx.x * kLayerGateWaves + wave,
            gridDim.x * kLayerGateWaves);
   sums.put(red + wave * 16 * NB, 0);
   __syncthreads();
