@@ -25,9 +25,15 @@ static hipError_t by_tile(const ExpertArgs& x, int M, int N, int K, Fn fn) {
   // K = 1024, 512 tiles: four groups 50 us, two 45; 4 x 202 x 1792, K = 3264, 448 tiles: 132 and
   // 178; 8 x 128 x 256, K = 1024: one group 27 us, four 26, 32 x 32 by eight 12; 8 x 128 x 1024,
   // K = 256: one group 13.6 us, four 17.4).
+  //
+  // For at most 32 rows, whose weights are what there is to read, tiles of 32 x 64 by two groups
+  // (forward of 82 x 1 x 3424 x 1216 752 us in tiles of 64, 517; of 64 x 32 x 1024 x 1024 158 and
+  // 122; of 20 x 11 x 128 x 4952, whose second product has 40 tiles of 64, 50 us with 32 x 32 there,
+  // 73 without).
   auto tiles = [&](int t) { return static_cast<int64_t>(x.E) * ((M + t - 1) / t) * ((N + t - 1) / t); };
   auto rounds = [&](int t) { return (tiles(t) + 255) / 256; };
   if (K >= 256 && tiles(128) >= 512 && 40 * rounds(128) <= 11 * rounds(64)) return fn(Tile<128, 128, 2, 2, 1, 2>());
+  if (M <= 32 && tiles(64) >= 256) return fn(Tile<32, 64, 2, 2, 2, 2>());
   if (K < 512) return fn(Tile<64, 64, 4, 1, 1, 4>());
   if (tiles(64) >= 512) return fn(Tile<64, 64, 4, 1, 2, 2>());
   if (tiles(64) >= 256) return fn(Tile<64, 64, 4, 1, 4, 1>());

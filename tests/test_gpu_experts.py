@@ -165,6 +165,15 @@ def test_tiles_of_128_in_fp32(act, gated):
     _both_ways("f32", E, C, d, h, act, gated, _counts(np.random.default_rng(59), E, C), 59)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,h,act,gated", [(264, 520, "relu", True), (24, 264, "silu", False)])
+def test_few_rows_of_many_experts(d, h, act, gated, dtype):
+    """At most 32 rows per expert (and, with d = 24, of a weight gradient) and more than 256 tiles."""
+    E, C = 70, 20
+    announce(f"experts_few {dtype} E={E} C={C} d={d} h={h} {act} gated={gated}")
+    _both_ways(dtype, E, C, d, h, act, gated, _counts(np.random.default_rng(67), E, C), 67)
+
+
 def test_many_experts_and_more_tiles_than_a_list_holds():
     """1024 experts of one row, 129 tiles each: more than 256 tiles for each of 512 blocks."""
     E, C, d, h = 1024, 1, 8, 8256
