@@ -18,15 +18,16 @@ struct Tile {
 constexpr int kMaxRounds = 16;
 
 // Tiles of 256 x 256 once they fill the CUs (dw of 64 x 512 x 2048 x 8192: 1.12 ms, 128 x 128
-// 1.47; 8 x 1024 x 1024 x 1024, where they do not: forward 52 us, 128 x 128 47), of 128 x 128
-// once those do, and else, or where an expert has few rows, of 64 x 64, whose four stages
+// 1.47; 8 x 1024 x 1024 x 1024, where they do not: forward 52 us, 128 x 128 47) and an expert fills
+// more than half of one's rows (forward of 64 x 128 x 1024 x 4096 289 us, 128 x 128 264), of 128 x
+// 128 once those fill the CUs, and else, or where an expert has few rows, of 64 x 64, whose four stages
 // keep memory busy from few blocks (forward of 8 x 128 x 1024 x 4096 44 us, 128 x 128 61; of
 // 32 x 128 x 1024 x 1024, where 128 x 128 fill the CUs, 45 and 35; dpre of 36 x 2 x 64, K =
 // 2760: 21 us, two stages of 64 x 256 35).
 template <class Fn>
 static hipError_t by_tile(const ExpertArgs& x, int M, int N, Fn fn) {
   auto tiles = [&](int t) { return static_cast<int64_t>(x.E) * ((M + t - 1) / t) * ((N + t - 1) / t); };
-  if (M > 64 && tiles(256) >= 256) return fn(Tile<256, 256, 2, 4, 1>());
+  if (M > 128 && tiles(256) >= 256) return fn(Tile<256, 256, 2, 4, 1>());
   if (M > 64 && tiles(128) >= 256) return fn(Tile<128, 128, 2, 2, 2>());
   return fn(Tile<64, 64, 2, 1, 2>());
 }
