@@ -2,7 +2,8 @@
 //
 // A block forms BM x BN of one expert's product, WM x WN waves, 64 columns each.
 // Per stage of 64 K elements both operands go straight from memory to LDS as
-// they lie there (16 bytes per lane, no registers), two stages in turn.  Operands
+// they lie there (16 bytes per lane, no registers), two stages in turn (four for small tiles
+// and where a block has a CU to itself).  Operands
 // whose rows run along K are read as 16-byte fragments, the others through LDS
 // transpose reads.  16-byte pieces are placed by an exclusive-or with bits of
 // their row, so that the 16 lanes of a fragment read touch different banks; since
@@ -74,7 +75,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
   constexpr bool kSplit = EPI == kEpiAct && GATED;
   constexpr int BNO = kSplit ? BN / 2 : BN;
-  constexpr bool kDeep = BM * BN <= 64 * 128;                   // four stages
+  constexpr bool kDeep = BM * BN <= 64 * 128 || WM == 4;        // four stages: few blocks
   constexpr bool kRing = !kDeep && KA == kCols && KB == kCols;  // four stages of half the length
   constexpr int BK = kRing ? kEBK / 2 : kEBK;
   constexpr int kTurn = kDeep ? 4 * kEBK : 2 * kEBK;  // K elements in which all stages had their turn

@@ -14,7 +14,9 @@ struct Tile {
 
 // Rounds of tiles up to which the last one is worth a launch of its own, which costs 4 to 5 us
 // where it finds nothing to do (dxe of 16 x 1280 x 1024 x 4096 gated, 1024 rows in use: 407 us in
-// whole tiles, 237 + 108 with the second round in quarters).
+// whole tiles, 237 + 71 with the second round in quarters).  Few blocks have only their own
+// loads to wait for: eight waves and four stages, one block per CU (these 32 quarter tiles of K =
+// 8192 71 us, by four waves with two stages, two blocks per CU, 108; 320 of them 148 and 130).
 constexpr int kMaxRounds = 16;
 
 // Tiles of 256 x 256 once they fill the CUs (dw of 64 x 512 x 2048 x 8192: 1.12 ms, 128 x 128
@@ -46,7 +48,7 @@ static hipError_t launch_tile_bf16(const ExpertArgs& x, ExpertGemmArgs a, hipStr
       <<<dim3(expert_blocks(a.tiles, resident)), dim3(TL::wm * TL::wn * kWave), 0, st>>>(a);
   if constexpr (kQuarters) {
     if (a.round) {
-      using Q = Tile<TL::bm / 2, TL::bn / 2, 2, 2, 2>;
+      using Q = Tile<TL::bm / 2, TL::bn / 2, 4, 2, 1>;
       a.quarters = 1;
       experts_gemm_bf16_kernel<Q::bm, Q::bn, Q::wm, Q::wn, KA, KB, EPI, GATED>
           <<<dim3(expert_blocks(2 * resident, Q::per_cu * device_cu_count())), dim3(Q::wm * Q::wn * kWave), 0, st>>>(a);
