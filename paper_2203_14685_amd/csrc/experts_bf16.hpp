@@ -369,7 +369,8 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     const int N1 = GATED ? 2 * a.N : a.N;
     float* part = a.colsum ? a.colsum + (static_cast<int64_t>(e) * a.tm * WM + bm * WM + wm) * N1 : nullptr;
     const __amdgpu_buffer_rsrc_t out = expert_rows<bf16_t>(a.out, static_cast<int64_t>(e) * a.C + m0, N1, valid);
-    // rows behind the count read as zeros, and so does their dhidden
+    // rows behind the count read as zeros; their products are chosen away below: zero rows
+    // times an infinite weight are NaN, which would reach the sums
     const __amdgpu_buffer_rsrc_t pre =
         expert_rows<bf16_t>(a.pre, static_cast<int64_t>(e) * a.C + m0, N1, min(BM, rows - m0));
 #pragma unroll
@@ -392,6 +393,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < kRowsAhead; ++i) {
+          const bool used = m0 + lrow + 16 * (i0 + i) < rows;
           float v[8], u[8];
           Chunk<bf16_t>::unpack(pv[i], v);
           if constexpr (GATED) Chunk<bf16_t>::unpack(pu[i], u);
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
             for (int q = 0; q < 8; ++q) {
               float f, df;
               expert_act_grad<ACT>(v[q], f, df);
-              const float dh = value(i0 + i, p, q);
+              const float dh = used ? value(i0 + i, p, q) : 0.f;
               v[q] = GATED ? dh * u[q] * df : dh * df;
               if constexpr (GATED) u[q] = dh * f;
             }
