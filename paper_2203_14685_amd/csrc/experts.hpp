@@ -194,7 +194,9 @@ __device__ __forceinline__ void expert_act_grad(float a, float& f, float& df) {
   } else {
     const float p = expert_sigmoid(2.f * kGeluA * (a + kGeluB * a * a * a));
     f = a * p;
-    df = p + f * (1.f - p) * (2.f * kGeluA) * (1.f + 3.f * kGeluB * a * a);
+    // p is exactly 0 or 1 long before 1e18; past 1.8e19 the square would be infinite, 0 times it NaN
+    const float c = fminf(fabsf(a), 1e18f);
+    df = p + f * (1.f - p) * (2.f * kGeluA) * (1.f + 3.f * kGeluB * c * c);
   }
 }
 

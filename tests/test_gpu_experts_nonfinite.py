@@ -1,5 +1,5 @@
-"""Weights that hold infinities or NaN: what is not finite shows in the sums it enters over
-the rows in use, and nowhere else."""
+"""Weights that hold infinities or NaN, and pre-activations of the largest magnitudes: what
+is not finite shows in the sums it enters over the rows in use, and nowhere else."""
 
 import numpy as np
 import pytest
@@ -110,3 +110,32 @@ def test_weights_that_are_not_finite_in_the_forward_pass(E, C, d, h, bad, dtype)
     assert not torch.isfinite(second["ye"][hit(d, c)]).any()
     if bad != bad:
         assert torch.isnan(first["pre"][hit(h, j)]).all() and torch.isnan(first["ye"][hit(d, None)]).all()
+
+
+# beyond 1.8e19 a square leaves fp32, beyond 7e12 a cube
+LARGE = [1e6, 7e12, 1e15, 1.7e19, 2e19, 6e19, 1e25, 3e38]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("act", sorted(ACTS))
+@pytest.mark.parametrize("gated", [False, True])
+def test_derivatives_of_large_pre_activations(act, gated, dtype):
+    """One row with dhidden = 1, so db1 is the activation's derivative: 1 to the right, 0 to the left
+    (gated, the other half's are the activation itself)."""
+    announce(f"experts_bwd large pre {dtype} {act} gated={gated}")
+    a = torch.tensor([[LARGE + [-v for v in LARGE]]]).to(TORCH[dtype])
+    h, d = 16, 8
+    pre = torch.cat([a, torch.ones_like(a)], dim=2) if gated else a
+    w1 = torch.zeros((1, d, pre.shape[2]), dtype=a.dtype, device=DEV)
+    w2 = torch.zeros((1, h, d), dtype=a.dtype, device=DEV)
+    w2[:, :, 0] = 1
+    dye = torch.zeros((1, 1, d), dtype=a.dtype, device=DEV)
+    dye[0, 0, 0] = 1
+    hid = torch.zeros((1, 1, h), dtype=a.dtype, device=DEV)
+    o = hm.experts_bwd(dye, torch.ones_like(dye), w1, w2, pre.to(DEV), hid, act=ACTS[act], gated=gated)
+    torch.cuda.synchronize()
+    # the sigmoid of such arguments is exactly 1 or 0
+    av = a.to(DEV).float()[0]
+    assert torch.equal(o["db1"][:, :h], (av > 0).float()), o["db1"]
+    if gated:
+        assert torch.equal(o["db1"][:, h:], av.clamp(min=0)), o["db1"]
