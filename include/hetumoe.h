@@ -580,14 +580,16 @@ MOE_API moe_status moe_grad_norm(const moe_grad_tensor* tensors, int32_t count, 
 
 /*
  * moe_grad_clip -- gradients scaled so that their norm is at most max_norm:
- *   dst = src * scale, scale = min(1, max_norm / sqrt(sumsq)) in fp32,
- * rounded once.  A norm of at most max_norm leaves the values as they are; a NaN
- * norm makes the scale NaN.  In place (dst == src) a scale of 1 writes nothing.
+ *   dst = src * scale, scale = min(1, max_norm / sqrt(sumsq)),
+ * the scale with fp32's 24 bits (also below its normal numbers), dst rounded once.  A
+ * norm of at most max_norm leaves the values as they are; a NaN norm makes the scale
+ * NaN.  In place (dst == src) a scale of 1 writes nothing.
  *
  * Inputs   sumsq [1] fp64 in device memory (moe_grad_norm's, or its sum over ranks);
  *          max_norm finite and >= 0.
- * Outputs  every dst; norm [1] fp32 = sqrt(sumsq), or NULL.  An output may overlap no
- *          other tensor's output or input: a tensor listed twice is refused.
+ * Outputs  every dst; norm [1] fp32 = sqrt(sumsq) (infinite beyond fp32, the scale is
+ *          not), or NULL.  An output may overlap no other tensor's output or input: a
+ *          tensor listed twice is refused.
  */
 MOE_API moe_status moe_grad_clip(const moe_grad_tensor* tensors, int32_t count, const double* sumsq,
                                  float max_norm, float* norm, hipStream_t stream);

@@ -98,8 +98,15 @@ __global__ __launch_bounds__(kBlock) void grad_finish_kernel(const double* part,
   }
 }
 
+// The scale as two factors: below 2^-126 one fp32 number would hold few of its bits, or none
+// (gradients near the largest fp32 numbers, or a tiny max_norm).  Else the second one is 1.
+struct Scale {
+  float a, b;
+  __device__ __forceinline__ float operator()(float v) const { return v * a * b; }
+};
+
 template <class T, bool NT>
-__device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, bool vec, float scale) {
+__device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, bool vec, Scale scale) {
   constexpr int PE = Chunk<T>::kElems;
   int64_t done = 0;
   if (vec) {
@@ -117,7 +124,7 @@ __device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, boo
         float f[PE];
         Chunk<T>::unpack(v[u], f);
 #pragma unroll
-        for (int e = 0; e < PE; ++e) f[e] *= scale;
+        for (int e = 0; e < PE; ++e) f[e] = scale(f[e]);
         if constexpr (NT) __builtin_nontemporal_store(Chunk<T>::pack(f), o + i + u * kBlock);
         else o[i + u * kBlock] = Chunk<T>::pack(f);
       }
@@ -125,7 +132,7 @@ __device__ __forceinline__ void chunk_scale(const T* src, T* dst, int64_t n, boo
     done = pieces * PE;
   }
   for (int64_t i = done + threadIdx.x; i < n; i += kBlock) {
-    const float v = load_elem(src, i) * scale;
+    const float v = scale(load_elem(src, i));
     if constexpr (sizeof(T) == 2) dst[i].bits = static_cast<uint16_t>(f32_to_bf16_bits(v));
     else dst[i] = v;
   }
@@ -135,11 +142,13 @@ template <bool NT>
 __global__ __launch_bounds__(kBlock) void grad_scale_kernel(GradList l, const double* sumsq, float max_norm, float* norm) {
   const double nm = sqrt(*sumsq);
   // a NaN norm makes the scale NaN
-  const float scale = nm <= max_norm ? 1.f : static_cast<float>(max_norm / nm);
+  const double exact = nm <= max_norm ? 1.0 : max_norm / nm;
+  const bool tiny = exact < 0x1p-126;
+  const Scale scale{static_cast<float>(tiny ? exact * 0x1p100 : exact), tiny ? 0x1p-100f : 1.f};
   if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = static_cast<float>(nm);
   for (int c = blockIdx.x; c < l.chunks; c += gridDim.x) {
     const GradTensor& t = l.t[tensor_of(l, c)];
-    if (scale == 1.f && t.src == t.dst) continue;
+    if (scale.a == 1.f && t.src == t.dst) continue;
     const int64_t at = static_cast<int64_t>(c - t.first) * kGradChunk;
     const int64_t n = min(static_cast<int64_t>(kGradChunk), t.n - at);
     if (t.dtype == 1)
