@@ -98,14 +98,14 @@ struct ExpertOperand {
   static_assert(N * WAVES * 1024 == kBytes, "whole loads");
   static constexpr int P = KIND == kRows ? kExpertRow / 16 : W / kPe;  // pieces per LDS row
   static constexpr int R = 64 / P;                       // rows per load
-  // a lane's rows are R * WAVES apart: where that changes the order of the pieces, two offsets in turn
-  static constexpr int kAlt = KIND == kCols && kElt == 2 && R * WAVES % 16 != 0 ? 2 : 1;
-  static_assert(KIND == kCols || R * WAVES % (RIGHT && kElt == 4 && W > 32 ? 32 : 16) == 0,
+  // a lane's rows are R * WAVES apart, which must not change the order of their pieces
+  static_assert((KIND == kCols && kElt == 4) ||
+                    R * WAVES % (KIND == kRows && RIGHT && kElt == 4 && W > 32 ? 32 : 16) == 0,
                 "one order of the pieces per lane");
   const char* base;   // (first row or column, k = 0), moved on by the stages
   int rows;           // kRows: bytes behind base that may be read
   int pitch;          // bytes per row of the matrix
-  unsigned off[kAlt];
+  unsigned off;       // of the lane's first piece in a stage
   int kc;             // kRows: the lane's K element in a stage
 
   // map(piece) gives the column of the tile's piece, or -1 behind the matrix.
@@ -120,14 +120,11 @@ struct ExpertOperand {
       rows = max(0, valid) * pitch;
       const int piece = (lane % P) ^ expert_swz<T, KIND, RIGHT, W>(row0);
       kc = piece * kPe;
-      off[0] = static_cast<unsigned>(row0 * ld * kElt + piece * 16);
+      off = static_cast<unsigned>(row0 * ld * kElt + piece * 16);
     } else {
       base = reinterpret_cast<const char*>(p);
-#pragma unroll
-      for (int i = 0; i < kAlt; ++i) {
-        const int col = map((lane % P) ^ expert_swz<T, KIND, RIGHT, W>(row0 + i * R * WAVES));
-        off[i] = col >= 0 ? static_cast<unsigned>((row0 * ld + col) * kElt) : static_cast<unsigned>(kExpertOob);
-      }
+      const int col = map((lane % P) ^ expert_swz<T, KIND, RIGHT, W>(row0));
+      off = col >= 0 ? static_cast<unsigned>((row0 * ld + col) * kElt) : static_cast<unsigned>(kExpertOob);
     }
   }
   // Passes over n stages.
@@ -139,9 +136,9 @@ struct ExpertOperand {
   // offset past the resource stays past it (below 2^32) with the rows' strides added.
   struct Stage {
     __amdgpu_buffer_rsrc_t r;
-    unsigned o[kAlt], stride;
+    unsigned o, stride;
     __device__ __forceinline__ void issue(T* lds, int wave, int i) const {
-      expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, static_cast<int>(o[i % kAlt] + i * stride));
+      expert_dma(r, reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024, static_cast<int>(o + i * stride));
     }
   };
   __device__ __forceinline__ Stage next(int left) {
@@ -149,11 +146,8 @@ struct ExpertOperand {
     s.r = expert_rsrc(base,
                       __builtin_amdgcn_readfirstlane(KIND == kRows ? max(rows, 0) : max(0, min(left, kBk)) * pitch));
     s.stride = static_cast<unsigned>(R * WAVES) * static_cast<unsigned>(pitch);
-#pragma unroll
-    for (int i = 0; i < kAlt; ++i) {
-      s.o[i] = expert_opaque(off[i]);
-      if constexpr (KIND == kRows) s.o[i] = kc < left ? s.o[i] : static_cast<unsigned>(kExpertOob);
-    }
+    s.o = expert_opaque(off);
+    if constexpr (KIND == kRows) s.o = kc < left ? s.o : static_cast<unsigned>(kExpertOob);
     base += KIND == kRows ? kExpertRow : kBk * pitch;
     if constexpr (KIND == kRows) rows -= kExpertRow;
     return s;
@@ -301,28 +295,25 @@ struct ExpertTiles {
     return int4{lo, r % mt, r / mt, 0};
   }
 
-  // Tile `i` of those without work.
-  __device__ __forceinline__ bool clear(const ExpertGemmArgs& a, int i, ExpertTile& t) const {
-    return !a.quarters && i < a.tiles - nv && find(a, i, true, t);
-  }
-
-  __device__ __forceinline__ bool find(const ExpertGemmArgs& a, int want, bool empty, ExpertTile& t) const {
+  // Tile `want` of those without work.
+  __device__ __forceinline__ bool clear(const ExpertGemmArgs& a, int want, ExpertTile& t) const {
+    if (a.quarters || want >= a.tiles - nv) return false;
     const int lane = lane_id();
     for (int e0 = 0; e0 < a.E; e0 += kWave) {
       const int i = min(e0 + lane, a.E - 1);
-      // tiles along M up to and with expert i
-      const int upto = empty ? (i + 1) * a.tm - before[i] : before[i];
+      // such tiles along M up to and with expert i
+      const int upto = (i + 1) * a.tm - before[i];
       const uint64_t past = __ballot(e0 + lane < a.E && upto * a.tn > want);
       if (past) {
         const int e = e0 + __builtin_ctzll(past);
         const int last = __builtin_amdgcn_readfirstlane(before[e]);
         const int first = e > 0 ? __builtin_amdgcn_readfirstlane(before[e - 1]) : 0;
-        const int mt = empty ? a.tm - (last - first) : last - first;
-        const int r = want - (empty ? e * a.tm - first : first) * a.tn;
+        const int mt = a.tm - (last - first);
+        const int r = want - (e * a.tm - first) * a.tn;
         const int bn = r / mt;
         t.e = __builtin_amdgcn_readfirstlane(e);
         t.bn = __builtin_amdgcn_readfirstlane(bn);
-        t.bm = __builtin_amdgcn_readfirstlane(r - bn * mt + (empty ? a.tm - mt : 0));
+        t.bm = __builtin_amdgcn_readfirstlane(r - bn * mt + a.tm - mt);
         return true;
       }
     }
