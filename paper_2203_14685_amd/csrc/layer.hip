@@ -247,12 +247,19 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a, 
           if constexpr (kSplit) f *= u;
           T* out = reinterpret_cast<T*>(a.hidden) + static_cast<int64_t>(list[li]) * N + n0 + c;
           if constexpr (ELT == 2) {
-            const uint32_t hi = f32_to_bf16_bits(f);
-            const float rest = f - __uint_as_float(hi << 16);
+            // Both of f's sign and neither zero unless f is, so that times an infinite weight they
+            // add up to an infinity: the first is cut, not rounded, and a second one below the
+            // normal numbers becomes the least of them.  The 8 bits of the second follow the
+            // 8 of the first: off by 2^-16 of f at most.
+            uint32_t hi = __float_as_uint(f) >> 16, lo;
+            if ((hi & 0x7f80u) == 0x7f80u) {
+              hi = lo = f32_to_bf16_bits(f);  // an infinity or a NaN
+            } else {
+              lo = f32_to_bf16_bits(f - __uint_as_float(hi << 16));
+              if ((lo & 0x7f80u) == 0) lo = f == 0.f ? 0u : (hi & 0x8000u) | 0x0080u;
+            }
             out->bits = static_cast<uint16_t>(hi);
-            // nothing is left of an infinity or a NaN
-            out[static_cast<int64_t>(choices) * a.h].bits =
-                (hi & 0x7f80u) == 0x7f80u ? uint16_t(0) : static_cast<uint16_t>(f32_to_bf16_bits(rest));
+            out[static_cast<int64_t>(choices) * a.h].bits = static_cast<uint16_t>(lo);
           }
           else *out = f;
         } else {

@@ -59,3 +59,37 @@ def test_split_sums(S, d, E, k, h, parts, dtype):
         torch.cuda.synchronize()
         ref = ox.token_layer(xv, ids, wv, w1v, b1v, w2v, b2v, ACTS[act], gated, ROUND[dtype])
         check(y, ref, f"y {act} gated={gated} {case}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,E,k,h", [(1, 8, 2, 136), (40, 4, 2, 264), (3, 8, 1, 8200)])
+def test_infinite_second_weight(S, E, k, h, dtype):
+    """w2[e, j, c] = inf with hidden[j] > 0 makes y[:, c] of the rows that chose e infinite, of their
+    weight's sign, whichever way hidden rounds, and changes no other value."""
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    announce(f"token_layer infinite w2 {dtype} S={S} E={E} k={k} h={h}")
+    rng = np.random.default_rng(S)
+    d = 64
+    x = normal(rng, (S, d), dtype)[0].to(DEV)
+    (w1, _), (b1, _), (w2, _), (b2, _) = weights(rng, E, d, h, False, dtype)
+    ids = torch.from_numpy(np.stack([rng.permutation(E)[:k] for _ in range(S)]).astype(np.int32)).to(DEV)
+    w = normal(rng, (S, k), "f32")[0].to(DEV)
+    kw = dict(b1=b1, b2=b2, act=hm.MOE_ACT_RELU, ids=ids, weights=w)
+    b1[:] = b1.abs() + 12.0  # every hidden value positive: a row of x times a column of w1 is some 1 +- 1
+    w1.clamp_(-0.5, 0.5)
+    base = hm.token_layer(x, w1, w2, **kw)["y"]
+    e = int(ids[0, 0])
+    hit = (ids == e)
+    for j in range(0, h, max(1, h // 24)):  # hidden values of many roundings
+        v = w2.clone()
+        v[e, j, 5] = float("inf")
+        y = hm.token_layer(x, w1, v, **kw)["y"]
+        torch.cuda.synchronize()
+        sign = (w.sign() * hit).sum(dim=1)
+        rows = hit.any(dim=1)
+        assert (y[rows, 5].float() == sign[rows] * float("inf")).all(), (j, y[rows, 5])
+        same = torch.ones_like(y, dtype=torch.bool)
+        same[rows, 5] = False
+        assert torch.equal(y[same], base[same]), j
