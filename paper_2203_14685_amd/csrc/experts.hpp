@@ -160,8 +160,10 @@ struct ExpertOperand {
 };
 
 // ---------------------------------------------------------------- activations
-// sigmoid by the hardware exponential and reciprocal: both within about one
-// unit of the last place of fp32 for the arguments that matter.
+// sigmoid by the hardware exponential and reciprocal.  The exponential's argument is rounded
+// after its factor log2(e), so its relative error grows as |x| 2^-24 (some units of the last
+// place at |x| = 10, where 1 + it has long lost them for x > 0 and the result is below 5e-5 for
+// x < 0); the reciprocal is within one unit.
 __device__ __forceinline__ float expert_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + __expf(-x)); }
 
 constexpr float kGeluA = 0.7978845608028654f;  // sqrt(2 / pi)

@@ -25,11 +25,16 @@
 // Rows past the expert's count and pieces past K are zeros from outside the buffer
 // resource; nothing behind the count is read.
 //
-// Large products are bound by the chip's power: 64 x 2048 rows x 2048 x 2048, the gated
-// first product 1.86 ms and the second 0.91, 1.0 PFLOP/s of rows in use at 1.6 GHz, the matrix
-// units busy 54 % of the time; blocks of four waves with half of the LDS reads 1.95 and 0.95 ms
-// (1.8 GHz, 44 %).  The weight gradients also by what their transpose reads, loads and stores
-// take (64 x 460 rows x 2048 x 8192: 1.12 ms, without the stores 0.80, without the loads 0.75).
+// Large products: 64 experts of 2560 rows in use x 2048 x 2048, the gated first product 2.40
+// ms and the second 1.14, 1.15 and 1.20 PFLOP/s, the matrix units busy 56 and 60 % of the time at
+// 1.94 and 1.90 GHz.  The clock falls as the units get busier, so power takes part of what a
+// better fed loop would gain (a library product of 8192^3: 70 % at 1.90 GHz, 1.36 PFLOP/s; of zeros
+// 71 % at 2.42), but a seventh to a fifth is this loop's own: its reads, barriers and epilogues.  Rows
+// 16 KB apart feed it worse (one expert of 8192^3: 1.02 ms, 44 % at 2.33 GHz).  Blocks of four
+// waves with half of the LDS reads were slower (gated, uneven rows: 1.86 and 0.91 -> 1.95 and
+// 0.95 ms).  The weight gradients are bound by what their transpose reads, loads and stores take
+// (64 x 460 rows x 2048 x 8192: 1.12 ms, without the stores 0.80, without the loads 0.75; the units
+// busy 32 % at 2.3 GHz).
 #pragma once
 
 #include "experts.hpp"

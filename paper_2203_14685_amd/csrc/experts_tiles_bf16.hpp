@@ -20,8 +20,9 @@ struct Tile {
 constexpr int kMaxRounds = 16;
 
 // Tiles of 256 x 256 once they fill the CUs (dw of 64 x 512 x 2048 x 8192: 1.12 ms, 128 x 128
-// 1.47; 8 x 1024 x 1024 x 1024, where they do not: forward 52 us, 128 x 128 47) and an expert fills
-// more than half of one's rows (forward of 64 x 128 x 1024 x 4096 289 us, 128 x 128 264), of 128 x
+// 1.47; 8 x 1024 x 1024 x 1024, where they do not: forward 52 us, 128 x 128 47) and an expert's slots
+// are more than half of one's rows (the rows in use are known on the device alone: 154 of 313
+// take 256 x 256 too; forward of 64 x 128 x 1024 x 4096 289 us, 128 x 128 264), of 128 x
 // 128 once those fill the CUs, and else, or where an expert has few rows, of 64 x 64, whose four stages
 // keep memory busy from few blocks (forward of 8 x 128 x 1024 x 4096 44 us, 128 x 128 61; of
 // 32 x 128 x 1024 x 1024, where 128 x 128 fill the CUs, 45 and 35; dpre of 36 x 2 x 64, K =

@@ -8,8 +8,9 @@
 // registers, and add their sums in LDS at the end.  The second matrix's K is also
 // split over blocks where that is needed to occupy the chip; the last kernel adds
 // those parts in order.  No atomics: results repeat bit for bit.  Bound by the weights' bytes:
-// 64 experts of 2048 x 2048, gated, 32 tokens of two choices: 115 and 61 us, 5.8 TB/s; one
-// token, two experts of 2048 x 8192: 14 us each, 4.7 TB/s.
+// 64 experts of 2048 x 2048, gated, 32 tokens of two choices: 115 and 59 us, 5.8 TB/s; one
+// token, two experts of 2048 x 8192: 15 us each, 4.5 TB/s, with other experts each pass, whose
+// weights no cache holds (14 to 15 with the same ones, 134 MB that the Infinity Cache may hold).
 #include <algorithm>
 
 #include "experts.hpp"
@@ -434,8 +435,8 @@ hipError_t run_layer(const LayerArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Blocks along the second matrix's K: enough that two per CU run, with at least
-// four steps for each wave.
+// Blocks along the second matrix's K: enough that two per CU run, with at least four steps
+// for each wave (two where eight waves share a strip).
 int layer_splits(const LayerArgs& a) {
   const int elt = a.dtype == 1 ? 2 : 4;
   const bool nar = narrow(a, false);
