@@ -251,7 +251,7 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a, 
             // Both of f's sign and neither zero unless f is, so that times an infinite weight they
             // add up to an infinity: the first is cut, not rounded, and a second one below the
             // normal numbers becomes the least of them.  The 8 bits of the second follow the
-            // 8 of the first: off by 2^-16 of f at most.
+            // 8 of the first: off by 2^-16 of f at most (by 2^-126 where that is more).
             uint32_t hi = __float_as_uint(f) >> 16, lo;
             if ((hi & 0x7f80u) == 0x7f80u) {
               hi = lo = f32_to_bf16_bits(f);  // an infinity or a NaN
