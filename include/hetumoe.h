@@ -11,7 +11,12 @@
  * of step 4                                      -> moe_experts_bwd,
  * and of step 1                                  -> moe_gate_bwd;
  * the clipping of all gradients by their norm    -> moe_grad_norm, moe_grad_clip;
- * and the whole layer for a few tokens           -> moe_token_layer.
+ * the whole layer for a few tokens               -> moe_token_layer;
+ * and around the layer: the rows that it starts from -> moe_embed, moe_embed_bwd,
+ * dropout on rows and inside the experts         -> moe_dropout, moe_experts_dropout,
+ *                                                   moe_experts_dropout_bwd,
+ * the experts and the layer in 8-bit integers    -> moe_quantize, moe_quantize_weights,
+ *                                                   moe_experts_int8, moe_token_layer_int8.
  * Steps 3 and 5 (AllToAll) are outside this library.
  *
  * Conventions shared by every call
@@ -593,6 +598,151 @@ MOE_API moe_status moe_grad_norm(const moe_grad_tensor* tensors, int32_t count, 
  */
 MOE_API moe_status moe_grad_clip(const moe_grad_tensor* tensors, int32_t count, const double* sumsq,
                                  float max_norm, float* norm, hipStream_t stream);
+
+/* Parameters of moe_embed and moe_embed_bwd (host memory). */
+typedef struct {
+  int32_t T;          /* tokens */
+  int32_t V;          /* rows of the table */
+  int32_t d;          /* row length */
+  int32_t dtype;      /* moe_dtype of the table, the rows and their gradients */
+  float scale;        /* finite; 1 for plain rows */
+  int32_t accumulate; /* moe_embed_bwd: 1: dtable += the gradient; 0: dtable = it.  moe_embed: 0 */
+} moe_embed_params;
+
+/*
+ * moe_embed -- the rows that a layer starts from:
+ *   y[t,:] = scale * table[ids[t],:], rounded once; a zero row where ids[t] is outside
+ *            [0, V) (padding).
+ * ids [T] int32 (the token ids that a HASH gate routes by), table [V,d], y [T,d] output.
+ */
+MOE_API moe_status moe_embed(const moe_embed_params* p, const int32_t* ids, const void* table, void* y,
+                             hipStream_t stream);
+
+/* Bytes of device workspace moe_embed_bwd needs for `p`. */
+MOE_API moe_status moe_embed_bwd_workspace_size(const moe_embed_params* p, size_t* bytes);
+
+/*
+ * moe_embed_bwd -- gradient of moe_embed:
+ *   dtable[v,:] = [dtable[v,:] if accumulate] + scale * sum over t with ids[t] == v of dy[t,:]
+ * Sums are fp32 in a fixed order that depends on ids alone (tokens are sorted by id; no
+ * floating-point atomics): bitwise reproducible.  Rounded once.  Rows that no token names
+ * become zero, with accumulate they are neither read nor written.
+ *
+ * Inputs   dy [T,d], ids [T] int32 (ids outside [0, V) add to nothing).
+ * Outputs  dtable [V,d] (read first when accumulate).
+ * Range    T up to 2^30.
+ * Workspace device memory of at least moe_embed_bwd_workspace_size() bytes, 16-byte
+ *          aligned; contents on entry are ignored.
+ */
+MOE_API moe_status moe_embed_bwd(const moe_embed_params* p, const void* dy, const int32_t* ids, void* dtable,
+                                 void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* Which elements are dropped (host memory).  Element i of a buffer (row-major, i from
+ * 0) has the 16-bit word r_i: half i % 2 (the lower first) of word i / 2 % 4 of block i / 8 of the
+ * counter-based generator Philox4x32-10 (Salmon et al., SC 2011) with key (seed mod 2^32,
+ * seed / 2^32) and counter (block mod 2^32, block / 2^32, n mod 2^32, n / 2^32), n = call
+ * (+ *step) mod 2^64.  It is kept iff r_i >= t, t = p 2^16 rounded to the nearest integer (ties to
+ * even), and then scaled by 2^16 / (2^16 - t): p counts in steps of 2^-16 and the mean is kept
+ * exactly.  No mask is stored: the same parameters give the same mask, in the backward
+ * pass too. */
+typedef struct {
+  uint64_t seed;
+  uint64_t call;        /* numbers the masks of a seed: another one for every layer and step */
+  const uint64_t* step; /* [1] in DEVICE memory (8-byte aligned), added to call, or NULL: lets a captured
+                           graph draw other masks on every replay.  Let the calls of one step lie
+                           further apart than the steps count (for instance layer * 2^40) */
+  float p;              /* share that is dropped, in [0, 1]; 1 drops all, 0 none */
+  int32_t pad;
+} moe_dropout_mask;
+
+/*
+ * moe_dropout -- y_i = [residual_i] + (kept_i ? x_i * 2^16 / (2^16 - t) : 0), i = 0 .. n - 1,
+ * in fp32, rounded once.  A dropped x_i counts as 0 whatever it holds.  The gradient of x
+ * is the same call on dy without residual (the residual's is dy).
+ *
+ * Inputs   x [n], residual [n] or NULL.   Outputs  y [n]; may be x or residual.
+ * Range    n >= 0, any; every buffer 16-byte aligned.
+ */
+MOE_API moe_status moe_dropout(const moe_dropout_mask* mask, int64_t n, int32_t dtype, const void* x,
+                               const void* residual, void* y, hipStream_t stream);
+
+/*
+ * moe_experts_dropout -- moe_experts with dropout of the hidden rows (the expert dropout of
+ * Switch layers): hidden = drop(act(pre)) or drop(act(pre[:h]) * pre[h:]), before its rounding,
+ * with the mask of elements of [E,C,h], behind counts[e] too; all else as moe_experts.
+ * moe_experts_dropout_bwd -- its gradient, moe_experts_bwd with dhidden = drop(dye w2[e]^T) for
+ * the same mask; `hidden` is what the forward pass wrote.
+ */
+MOE_API moe_status moe_experts_dropout(const moe_experts_params* p, const moe_dropout_mask* mask,
+                                       const void* xe, const void* w1, const float* b1, const void* w2,
+                                       const float* b2, const int32_t* counts, void* pre, void* hidden,
+                                       void* ye, hipStream_t stream);
+MOE_API moe_status moe_experts_dropout_bwd(const moe_experts_params* p, const moe_dropout_mask* mask,
+                                           const void* dye, const void* xe, const void* w1, const void* w2,
+                                           const int32_t* counts, const void* pre, const void* hidden,
+                                           void* dxe, void* dw1, float* db1, void* dw2, float* db2,
+                                           void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * moe_quantize -- rows as 8-bit integers and one scale each: with a = max_j |x[r,j]|,
+ *   scale[r] = a / 127 (one fp32 division),  q[r,j] = the integer next to 127 x[r,j] / a (exact
+ *   quotient, ties to even), in [-127, 127];
+ * a row of zeros has scale 0 and zeros; one that holds an infinity or a NaN has scale NaN
+ * and zeros.
+ *
+ * Inputs   x [rows, n] (dtype), n a multiple of 16.   Outputs  q [rows, n] int8, scale [rows].
+ * x and q 16-byte aligned.
+ */
+MOE_API moe_status moe_quantize(int64_t rows, int32_t n, int32_t dtype, const void* x, int8_t* q, float* scale,
+                                hipStream_t stream);
+
+/*
+ * moe_quantize_weights -- expert weights w [E,K,N] (w1 or w2 of moe_experts) as integers in the
+ * layout that moe_experts_int8 reads, q [E,N,K], one scale per column, [E,N], by the rule of
+ * moe_quantize.  K and N multiples of 16; done once, when weights are loaded.
+ */
+MOE_API moe_status moe_quantize_weights(int32_t E, int32_t K, int32_t N, int32_t dtype, const void* w, int8_t* q,
+                                        float* scale, hipStream_t stream);
+
+/* Bytes of device workspace moe_experts_int8 needs for `p` (integer rows, hidden). */
+MOE_API moe_status moe_experts_int8_workspace_size(const moe_experts_params* p, size_t* bytes);
+
+/*
+ * moe_experts_int8 -- the expert networks in 8-bit integers, for inference.  For the first
+ * counts[e] rows, with (q, s) the integers and scale of a row as moe_quantize gives them:
+ *   pre    = (q(xe) . q1[e]) s(xe) s1[e] + b1[e]
+ *   hidden = act(pre), or act(pre[:h]) * pre[h:] when gated, rounded to dtype
+ *   ye     = (q(hidden) . q2[e]) s(hidden) s2[e] + b2[e]
+ * Integer sums are exact, the scales fp32; ye is rounded once.  Rows behind counts[e]
+ * are not read and are zero in ye.
+ *
+ * Inputs   xe [E,C,d] (dtype); q1 [E,h1,d], s1 [E,h1], q2 [E,d,h], s2 [E,d] as
+ *          moe_quantize_weights writes them; b1, b2, counts as moe_experts.
+ * Outputs  ye [E,C,d] (dtype).
+ * Range    d and h multiples of 16, at most 2^17 (sums of 32 bits); the matrices 16-byte
+ *          aligned.  E * C = 0 does nothing.
+ * Workspace device memory of at least moe_experts_int8_workspace_size() bytes, 16-byte
+ *          aligned; contents on entry are ignored.
+ */
+MOE_API moe_status moe_experts_int8(const moe_experts_params* p, const void* xe, const int8_t* q1,
+                                    const float* s1, const float* b1, const int8_t* q2, const float* s2,
+                                    const float* b2, const int32_t* counts, void* ye, void* workspace,
+                                    size_t workspace_bytes, hipStream_t stream);
+
+/* Bytes of device workspace moe_token_layer_int8 needs for `p`. */
+MOE_API moe_status moe_token_layer_int8_workspace_size(const moe_token_layer_params* p, size_t* bytes);
+
+/*
+ * moe_token_layer_int8 -- moe_token_layer with the expert networks of moe_experts_int8 (rows
+ * and hidden quantized token by token as there); the gate is moe_token_layer's, on x and wg
+ * in dtype.  Arguments, range (and that of moe_experts_int8) and workspace as there.
+ */
+MOE_API moe_status moe_token_layer_int8(const moe_token_layer_params* p, const void* x, const void* wg,
+                                        const float* bias, const int32_t* token_ids, const float* noise,
+                                        const int32_t* hash_table, const int8_t* q1, const float* s1,
+                                        const float* b1, const int8_t* q2, const float* s2, const float* b2,
+                                        int32_t* ids, float* weights, void* y, void* workspace,
+                                        size_t workspace_bytes, hipStream_t stream);
 
 /* Static description of a status code. */
 MOE_API const char* moe_status_string(moe_status s);

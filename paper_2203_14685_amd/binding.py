@@ -33,7 +33,9 @@ EXPORTED = (
     "moe_hash_balanced_table", "moe_base_gate_workspace_size", "moe_base_gate",
     "moe_base_gate_async", "moe_experts", "moe_experts_bwd_workspace_size", "moe_experts_bwd",
     "moe_token_layer_workspace_size", "moe_token_layer", "moe_grad_norm_workspace_size", "moe_grad_norm",
-    "moe_grad_clip", "moe_status_string", "moe_last_error", "moe_abi_version",
+    "moe_grad_clip", "moe_embed", "moe_embed_bwd_workspace_size", "moe_embed_bwd", "moe_dropout", "moe_experts_dropout",
+    "moe_experts_dropout_bwd", "moe_quantize", "moe_quantize_weights", "moe_experts_int8_workspace_size",
+    "moe_experts_int8", "moe_token_layer_int8_workspace_size", "moe_token_layer_int8", "moe_status_string", "moe_last_error", "moe_abi_version",
 )
 
 
@@ -101,6 +103,20 @@ class GradTensor(ctypes.Structure):
     ]
 
 
+class EmbedParams(ctypes.Structure):
+    _fields_ = [
+        ("T", ctypes.c_int32), ("V", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32),
+        ("scale", ctypes.c_float), ("accumulate", ctypes.c_int32),
+    ]
+
+
+class DropoutMask(ctypes.Structure):
+    _fields_ = [
+        ("seed", ctypes.c_uint64), ("call", ctypes.c_uint64), ("step", ctypes.c_void_p), ("p", ctypes.c_float),
+        ("pad", ctypes.c_int32),
+    ]
+
+
 # moe_base_status, which moe_base_gate_async writes to device memory: 24 bytes,
 # read back as int32 [6] (phases, rounds, eps as two words, status, pad)
 BASE_STATUS_BYTES = 24
@@ -148,6 +164,25 @@ def load():
     lib.moe_grad_norm_workspace_size.argtypes = [ctypes.POINTER(GradTensor), ctypes.c_int32, szp]
     lib.moe_grad_norm.argtypes = [ctypes.POINTER(GradTensor), ctypes.c_int32, vp, f32p, vp, sz, vp]
     lib.moe_grad_clip.argtypes = [ctypes.POINTER(GradTensor), ctypes.c_int32, vp, ctypes.c_float, f32p, vp]
+    drop, i32, f32, i64 = ctypes.POINTER(DropoutMask), ctypes.c_int32, ctypes.c_float, ctypes.c_int64
+    lib.moe_embed.argtypes = [ctypes.POINTER(EmbedParams), i32p, vp, vp, vp]
+    lib.moe_embed_bwd_workspace_size.argtypes = [ctypes.POINTER(EmbedParams), szp]
+    lib.moe_embed_bwd.argtypes = [ctypes.POINTER(EmbedParams), vp, i32p, vp, vp, sz, vp]
+    lib.moe_dropout.argtypes = [drop, i64, i32, vp, vp, vp, vp]
+    lib.moe_experts_dropout.argtypes = [lib.moe_experts.argtypes[0], drop, *lib.moe_experts.argtypes[1:]]
+    lib.moe_experts_dropout_bwd.argtypes = [lib.moe_experts_bwd.argtypes[0], drop, *lib.moe_experts_bwd.argtypes[1:]]
+    lib.moe_quantize.argtypes = [i64, i32, i32, vp, vp, f32p, vp]
+    lib.moe_quantize_weights.argtypes = [i32, i32, i32, i32, vp, vp, f32p, vp]
+    lib.moe_experts_int8_workspace_size.argtypes = [ctypes.POINTER(ExpertsParams), szp]
+    lib.moe_experts_int8.argtypes = [ctypes.POINTER(ExpertsParams), vp, vp, f32p, f32p, vp, f32p, f32p, i32p, vp, vp, sz,
+                                     vp]
+    lib.moe_token_layer_int8_workspace_size.argtypes = [ctypes.POINTER(TokenLayerParams), szp]
+    lib.moe_token_layer_int8.argtypes = [ctypes.POINTER(TokenLayerParams), vp, vp, f32p, i32p, f32p, i32p, vp, f32p, f32p,
+                                         vp, f32p, f32p, i32p, f32p, vp, vp, sz, vp]
+    for name in ("moe_embed", "moe_embed_bwd_workspace_size", "moe_embed_bwd", "moe_dropout", "moe_experts_dropout",
+                 "moe_experts_dropout_bwd", "moe_quantize", "moe_quantize_weights", "moe_experts_int8_workspace_size",
+                 "moe_experts_int8", "moe_token_layer_int8_workspace_size", "moe_token_layer_int8"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("moe_experts", "moe_experts_bwd_workspace_size", "moe_experts_bwd", "moe_token_layer_workspace_size",
                  "moe_token_layer", "moe_grad_norm_workspace_size", "moe_grad_norm", "moe_grad_clip"):
         getattr(lib, name).restype = ctypes.c_int
@@ -580,18 +615,32 @@ def _allocates_on_stream(fn):
     return run
 
 
+def _masked(call, mask, params, *args):
+    return call(params, mask, *args)
+
+
 def _bytes(workspace):
     return 0 if workspace is None else workspace.numel() * workspace.element_size()
 
 
-def moe_experts(params, xe, w1, b1, w2, b2, counts, pre, hidden, ye, stream=None):
+def _experts_pointers(params, xe, w1, b1, w2, b2, counts, pre, hidden, ye):
     dt, f32 = _dt(params.dtype), torch.float32
     rows, n1, n2, npre, nhid, h1 = _expert_sizes(params)
     E = params.E
-    _check(load().moe_experts(
-        ctypes.byref(params), _ptr(xe, dt, "xe", rows), _ptr(w1, dt, "w1", n1), _ptr(b1, f32, "b1", E * h1),
-        _ptr(w2, dt, "w2", n2), _ptr(b2, f32, "b2", E * params.d), _ptr(counts, torch.int32, "counts", E),
-        _ptr(pre, dt, "pre", npre), _ptr(hidden, dt, "hidden", nhid), _ptr(ye, dt, "ye", rows), _stream(stream)))
+    return (_ptr(xe, dt, "xe", rows), _ptr(w1, dt, "w1", n1), _ptr(b1, f32, "b1", E * h1), _ptr(w2, dt, "w2", n2),
+            _ptr(b2, f32, "b2", E * params.d), _ptr(counts, torch.int32, "counts", E), _ptr(pre, dt, "pre", npre),
+            _ptr(hidden, dt, "hidden", nhid), _ptr(ye, dt, "ye", rows))
+
+
+def moe_experts(params, xe, w1, b1, w2, b2, counts, pre, hidden, ye, stream=None):
+    _check(load().moe_experts(ctypes.byref(params),
+                              *_experts_pointers(params, xe, w1, b1, w2, b2, counts, pre, hidden, ye), _stream(stream)))
+
+
+def moe_experts_dropout(params, mask, xe, w1, b1, w2, b2, counts, pre, hidden, ye, stream=None):
+    _check(load().moe_experts_dropout(ctypes.byref(params), ctypes.byref(mask),
+                                      *_experts_pointers(params, xe, w1, b1, w2, b2, counts, pre, hidden, ye),
+                                      _stream(stream)))
 
 
 def moe_experts_bwd_workspace_size(params):
@@ -600,16 +649,29 @@ def moe_experts_bwd_workspace_size(params):
     return n.value
 
 
-def moe_experts_bwd(params, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace, stream=None):
+def _experts_bwd_pointers(params, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace):
     dt, f32 = _dt(params.dtype), torch.float32
     rows, n1, n2, npre, nhid, h1 = _expert_sizes(params)
     E = params.E
+    return (_ptr(dye, dt, "dye", rows), _ptr(xe, dt, "xe", rows), _ptr(w1, dt, "w1", n1), _ptr(w2, dt, "w2", n2),
+            _ptr(counts, torch.int32, "counts", E), _ptr(pre, dt, "pre", npre), _ptr(hidden, dt, "hidden", nhid),
+            _ptr(dxe, dt, "dxe", rows), _ptr(dw1, dt, "dw1", n1), _ptr(db1, f32, "db1", E * h1), _ptr(dw2, dt, "dw2", n2),
+            _ptr(db2, f32, "db2", E * params.d), _ptr(workspace, None, "workspace"), _bytes(workspace))
+
+
+def moe_experts_bwd(params, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace, stream=None):
     _check(load().moe_experts_bwd(
-        ctypes.byref(params), _ptr(dye, dt, "dye", rows), _ptr(xe, dt, "xe", rows), _ptr(w1, dt, "w1", n1),
-        _ptr(w2, dt, "w2", n2), _ptr(counts, torch.int32, "counts", E), _ptr(pre, dt, "pre", npre),
-        _ptr(hidden, dt, "hidden", nhid), _ptr(dxe, dt, "dxe", rows), _ptr(dw1, dt, "dw1", n1),
-        _ptr(db1, f32, "db1", E * h1), _ptr(dw2, dt, "dw2", n2), _ptr(db2, f32, "db2", E * params.d),
-        _ptr(workspace, None, "workspace"), _bytes(workspace), _stream(stream)))
+        ctypes.byref(params),
+        *_experts_bwd_pointers(params, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace),
+        _stream(stream)))
+
+
+def moe_experts_dropout_bwd(params, mask, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace,
+                            stream=None):
+    _check(load().moe_experts_dropout_bwd(
+        ctypes.byref(params), ctypes.byref(mask),
+        *_experts_bwd_pointers(params, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace),
+        _stream(stream)))
 
 
 def _weight_shapes(w1, w2, d, gated):
@@ -622,9 +684,11 @@ def _weight_shapes(w1, w2, d, gated):
 
 
 @_allocates_on_stream
-def experts(xe, w1, w2, *, b1=None, b2=None, counts=None, act=MOE_ACT_RELU, gated=False, want_pre=False, stream=None):
-    """Allocate the outputs and run moe_experts; returns a dict with ye, hidden
-    and pre (None unless want_pre; experts_bwd needs it)."""
+def experts(xe, w1, w2, *, b1=None, b2=None, counts=None, act=MOE_ACT_RELU, gated=False, want_pre=False, dropout=None,
+            stream=None):
+    """Allocate the outputs and run moe_experts, with `dropout` (a dropout_mask)
+    moe_experts_dropout; returns a dict with ye, hidden and pre (None unless
+    want_pre; experts_bwd needs it)."""
     E, C, d = xe.shape
     if _weight_shapes(w1, w2, d, gated)[0] != E:
         raise ValueError(f"xe has {E} experts, the weights {w2.shape[0]}")
@@ -635,16 +699,18 @@ def experts(xe, w1, w2, *, b1=None, b2=None, counts=None, act=MOE_ACT_RELU, gate
         "hidden": torch.empty((E, C, h), **new),
         "pre": torch.empty((E, C, w1.shape[2]), **new) if want_pre else None,
     }
-    moe_experts(experts_params(E, C, d, h, act, gated, _dtype_code(xe)), xe, w1, b1, w2, b2, counts, out["pre"],
-                out["hidden"], out["ye"], stream)
+    call = moe_experts if dropout is None else functools.partial(_masked, moe_experts_dropout, dropout)
+    call(experts_params(E, C, d, h, act, gated, _dtype_code(xe)), xe, w1, b1, w2, b2, counts, out["pre"], out["hidden"],
+         out["ye"], stream)
     return out
 
 
 @_allocates_on_stream
 def experts_bwd(dye, xe, w1, w2, pre, hidden, *, counts=None, act=MOE_ACT_RELU, gated=False, want_dxe=True,
-                want_dw=True, want_db=True, stream=None):
-    """Allocating wrapper of moe_experts_bwd; returns a dict with dxe, dw1, db1,
-    dw2 and db2 (None where not wanted)."""
+                want_dw=True, want_db=True, dropout=None, stream=None):
+    """Allocating wrapper of moe_experts_bwd, with the forward pass's `dropout` of
+    moe_experts_dropout_bwd; returns a dict with dxe, dw1, db1, dw2 and db2 (None where
+    not wanted)."""
     E, C, d = dye.shape
     if _weight_shapes(w1, w2, d, gated)[0] != E:
         raise ValueError(f"dye has {E} experts, the weights {w2.shape[0]}")
@@ -659,8 +725,9 @@ def experts_bwd(dye, xe, w1, w2, pre, hidden, *, counts=None, act=MOE_ACT_RELU, 
         "db2": torch.empty((E, d), **f32) if want_db else None,
     }
     ws = torch.empty((moe_experts_bwd_workspace_size(params),), dtype=torch.uint8, device=dye.device)
-    moe_experts_bwd(params, dye, xe, w1, w2, counts, pre, hidden, out["dxe"], out["dw1"], out["db1"], out["dw2"],
-                    out["db2"], ws, stream)
+    call = moe_experts_bwd if dropout is None else functools.partial(_masked, moe_experts_dropout_bwd, dropout)
+    call(params, dye, xe, w1, w2, counts, pre, hidden, out["dxe"], out["dw1"], out["db1"], out["dw2"], out["db2"], ws,
+         stream)
     return out
 
 
@@ -700,8 +767,19 @@ def token_layer(x, w1, w2, *, b1=None, b2=None, act=MOE_ACT_RELU, gated=False, k
     """The whole layer on x [S, d], S <= MOE_TOKEN_LAYER_MAX: allocate the outputs
     and run moe_token_layer.  The gate's arguments are those of `gate`; or pass
     another gate's ids and weights [S, k].  Returns a dict with y, ids and weights."""
+    E, h = _weight_shapes(w1, w2, int(x.shape[1]), gated)
+    params, ids, weights = _token_layer_choices(x, E, h, act, gated, kind, k, normalize, groups, hash_seed, hash_table,
+                                                temperature, ids, weights)
+    y = torch.empty_like(x)
+    ws = torch.empty((moe_token_layer_workspace_size(params),), dtype=torch.uint8, device=x.device)
+    moe_token_layer(params, x, wg, bias, token_ids, noise, hash_table, w1, b1, w2, b2, ids, weights, y, ws, stream)
+    return {"y": y, "ids": ids, "weights": weights}
+
+
+def _token_layer_choices(x, E, h, act, gated, kind, k, normalize, groups, hash_seed, hash_table, temperature, ids,
+                         weights):
+    """Parameters of a layer on x and its ids and weights, the caller's or empty ones."""
     S, d = x.shape
-    E, h = _weight_shapes(w1, w2, d, gated)
     routed = ids is not None or weights is not None
     if routed:
         if ids is None or weights is None or tuple(ids.shape) != tuple(weights.shape) or ids.dim() != 2 or ids.shape[0] != S:
@@ -714,10 +792,7 @@ def token_layer(x, w1, w2, *, b1=None, b2=None, act=MOE_ACT_RELU, gated=False, k
     vocab = 0 if hash_table is None else int(hash_table.shape[0])
     params = token_layer_params(S, d, E, k, h, kind, act, gated, _dtype_code(x), normalize, routed, groups, hash_seed,
                                 temperature, vocab)
-    y = torch.empty_like(x)
-    ws = torch.empty((moe_token_layer_workspace_size(params),), dtype=torch.uint8, device=x.device)
-    moe_token_layer(params, x, wg, bias, token_ids, noise, hash_table, w1, b1, w2, b2, ids, weights, y, ws, stream)
-    return {"y": y, "ids": ids, "weights": weights}
+    return params, ids, weights
 
 
 # ---------------------------------------------------------------- gradient norm and clipping
@@ -786,3 +861,199 @@ def clip_grads(grads, max_norm, out=None, sumsq=None, *, stream=None):
     else:
         moe_grad_clip(arr, sumsq, max_norm, norm, stream)
     return norm
+
+
+# ---------------------------------------------------------------- dropout
+
+def dropout_mask(p, seed, call=0, step=None):
+    """Which elements are dropped: the share p, a seed, and the mask's number among the
+    seed's (another one for every layer and step).  `step`: an int64 or uint64 device tensor [1]
+    that is added to `call`, so that a captured graph draws other masks on every replay; it
+    is kept alive by the mask."""
+    if step is not None and (step.dtype not in (torch.int64, torch.uint64) or step.numel() != 1):
+        raise TypeError("step must be one int64 or uint64")
+    m = DropoutMask(seed % 2 ** 64, call % 2 ** 64, _ptr(step, None, "step", 1), p, 0)
+    m.step_tensor = step
+    return m
+
+
+def moe_dropout(mask, n, dtype, x, residual, y, stream=None):
+    dt = _dt(dtype)
+    _check(load().moe_dropout(ctypes.byref(mask), n, dtype, _ptr(x, dt, "x", n), _ptr(residual, dt, "residual", n),
+                              _ptr(y, dt, "y", n), _stream(stream)))
+
+
+@_allocates_on_stream
+def dropout(x, mask, residual=None, out=None, *, stream=None):
+    """[residual +] x with the mask's elements dropped and the others scaled; `out` may be x
+    or residual.  The gradient of x is dropout(dy, mask)."""
+    y = torch.empty_like(x) if out is None else out
+    if y.shape != x.shape or (residual is not None and residual.shape != x.shape):
+        raise ValueError("x, residual and out must have one shape")
+    moe_dropout(mask, x.numel(), _dtype_code(x), x, residual, y, stream)
+    return y
+
+
+# ---------------------------------------------------------------- embedding rows
+
+def embed_params(T, V, d, dtype=MOE_F32, scale=1.0, accumulate=False):
+    return EmbedParams(T, V, d, dtype, scale, int(bool(accumulate)))
+
+
+def moe_embed(params, ids, table, y, stream=None):
+    dt, p = _dt(params.dtype), params
+    _check(load().moe_embed(ctypes.byref(p), _ptr(ids, torch.int32, "ids", p.T), _ptr(table, dt, "table", p.V * p.d),
+                            _ptr(y, dt, "y", p.T * p.d), _stream(stream)))
+
+
+def moe_embed_bwd_workspace_size(params):
+    n = ctypes.c_size_t(0)
+    _check(load().moe_embed_bwd_workspace_size(ctypes.byref(params), ctypes.byref(n)))
+    return n.value
+
+
+def moe_embed_bwd(params, dy, ids, dtable, workspace, stream=None):
+    dt, p = _dt(params.dtype), params
+    _check(load().moe_embed_bwd(ctypes.byref(p), _ptr(dy, dt, "dy", p.T * p.d), _ptr(ids, torch.int32, "ids", p.T),
+                                _ptr(dtable, dt, "dtable", p.V * p.d), _ptr(workspace, None, "workspace"),
+                                _bytes(workspace), _stream(stream)))
+
+
+@_allocates_on_stream
+def embed(ids, table, scale=1.0, *, stream=None):
+    """scale * table[ids] for int32 ids of any shape; zero rows where an id is outside the
+    table (padding)."""
+    V, d = table.shape
+    y = torch.empty((*ids.shape, d), dtype=table.dtype, device=table.device)
+    moe_embed(embed_params(ids.numel(), V, d, _dtype_code(table), scale), ids, table, y, stream)
+    return y
+
+
+@_allocates_on_stream
+def embed_bwd(dy, ids, V, scale=1.0, dtable=None, accumulate=False, *, stream=None):
+    """Gradient of embed for a table of V rows, into `dtable` if it is given, on top of what
+    it holds with `accumulate`."""
+    d = int(dy.shape[-1])
+    if tuple(dy.shape[:-1]) != tuple(ids.shape):
+        raise ValueError(f"dy {tuple(dy.shape)} and ids {tuple(ids.shape)} do not go together")
+    if accumulate and dtable is None:
+        raise ValueError("accumulate needs a dtable to add to")
+    if dtable is None:
+        dtable = torch.empty((V, d), dtype=dy.dtype, device=dy.device)
+    elif tuple(dtable.shape) != (V, d):
+        raise ValueError(f"dtable {tuple(dtable.shape)}, ({V}, {d}) expected")
+    params = embed_params(ids.numel(), V, d, _dtype_code(dy), scale, accumulate)
+    ws = torch.empty((moe_embed_bwd_workspace_size(params),), dtype=torch.uint8, device=dy.device)
+    moe_embed_bwd(params, dy, ids, dtable, ws, stream)
+    return dtable
+
+
+# ---------------------------------------------------------------- 8-bit integers
+
+def moe_quantize(rows, n, dtype, x, q, scale, stream=None):
+    _check(load().moe_quantize(rows, n, dtype, _ptr(x, _dt(dtype), "x", rows * n), _ptr(q, torch.int8, "q", rows * n),
+                               _ptr(scale, torch.float32, "scale", rows), _stream(stream)))
+
+
+def moe_quantize_weights(E, K, N, dtype, w, q, scale, stream=None):
+    _check(load().moe_quantize_weights(E, K, N, dtype, _ptr(w, _dt(dtype), "w", E * K * N),
+                                       _ptr(q, torch.int8, "q", E * K * N), _ptr(scale, torch.float32, "scale", E * N),
+                                       _stream(stream)))
+
+
+@_allocates_on_stream
+def quantize(x, *, stream=None):
+    """Rows (the last dimension) as 8-bit integers and one scale each: (q int8, scale float32)."""
+    n = int(x.shape[-1])
+    q = torch.empty(x.shape, dtype=torch.int8, device=x.device)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    moe_quantize(x.numel() // n if n else 0, n, _dtype_code(x), x, q, scale, stream)
+    return q, scale
+
+
+@_allocates_on_stream
+def quantize_weights(w, *, stream=None):
+    """Expert weights [E, K, N] as 8-bit integers [E, N, K], the layout that experts_int8 and
+    token_layer_int8 read, and one scale per column: (q, scale [E, N])."""
+    E, K, N = w.shape
+    q = torch.empty((E, N, K), dtype=torch.int8, device=w.device)
+    scale = torch.empty((E, N), dtype=torch.float32, device=w.device)
+    moe_quantize_weights(E, K, N, _dtype_code(w), w, q, scale, stream)
+    return q, scale
+
+
+def moe_experts_int8_workspace_size(params):
+    n = ctypes.c_size_t(0)
+    _check(load().moe_experts_int8_workspace_size(ctypes.byref(params), ctypes.byref(n)))
+    return n.value
+
+
+def moe_experts_int8(params, xe, q1, s1, b1, q2, s2, b2, counts, ye, workspace, stream=None):
+    dt, f32, i8 = _dt(params.dtype), torch.float32, torch.int8
+    rows, n1, n2, _, _, h1 = _expert_sizes(params)
+    E, d = params.E, params.d
+    _check(load().moe_experts_int8(
+        ctypes.byref(params), _ptr(xe, dt, "xe", rows), _ptr(q1, i8, "q1", n1), _ptr(s1, f32, "s1", E * h1),
+        _ptr(b1, f32, "b1", E * h1), _ptr(q2, i8, "q2", n2), _ptr(s2, f32, "s2", E * d), _ptr(b2, f32, "b2", E * d),
+        _ptr(counts, torch.int32, "counts", E), _ptr(ye, dt, "ye", rows), _ptr(workspace, None, "workspace"),
+        _bytes(workspace), _stream(stream)))
+
+
+def _int8_shapes(q1, q2, d, gated):
+    """E and h of quantized weights [E, h1, d] and [E, d, h]."""
+    E, h = int(q2.shape[0]), int(q2.shape[2])
+    if tuple(q2.shape) != (E, d, h) or tuple(q1.shape) != (E, 2 * h if gated else h, d):
+        raise ValueError(f"q1 {tuple(q1.shape)} and q2 {tuple(q2.shape)} are no quantized weights of width {d}"
+                         f"{', gated' if gated else ''}: [E, {'2 h' if gated else 'h'}, d] and [E, d, h] expected")
+    return E, h
+
+
+@_allocates_on_stream
+def experts_int8(xe, q1, s1, q2, s2, *, b1=None, b2=None, counts=None, act=MOE_ACT_RELU, gated=False, stream=None):
+    """The expert networks in 8-bit integers on xe [E, C, d], weights and scales from
+    quantize_weights: allocate ye and run moe_experts_int8."""
+    E, C, d = xe.shape
+    if _int8_shapes(q1, q2, d, gated)[0] != E:
+        raise ValueError(f"xe has {E} experts, the weights {q2.shape[0]}")
+    params = experts_params(E, C, d, int(q2.shape[2]), act, gated, _dtype_code(xe))
+    ye = torch.empty_like(xe)
+    ws = torch.empty((moe_experts_int8_workspace_size(params),), dtype=torch.uint8, device=xe.device)
+    moe_experts_int8(params, xe, q1, s1, b1, q2, s2, b2, counts, ye, ws, stream)
+    return ye
+
+
+def moe_token_layer_int8_workspace_size(params):
+    n = ctypes.c_size_t(0)
+    _check(load().moe_token_layer_int8_workspace_size(ctypes.byref(params), ctypes.byref(n)))
+    return n.value
+
+
+def moe_token_layer_int8(params, x, wg, bias, token_ids, noise, hash_table, q1, s1, b1, q2, s2, b2, ids, weights, y,
+                         workspace, stream=None):
+    g = params.gate
+    dt, f32, i32, i8 = _dt(g.dtype), torch.float32, torch.int32, torch.int8
+    S, d, E, k, h = g.S, g.d, g.E, g.k, params.h
+    h1 = 2 * h if params.gated else h
+    _check(load().moe_token_layer_int8(
+        ctypes.byref(params), _ptr(x, dt, "x", S * d), _ptr(wg, dt, "wg", d * E), _ptr(bias, f32, "bias", E),
+        _ptr(token_ids, i32, "token_ids", S), _ptr(noise, f32, "noise", S * E),
+        _ptr(hash_table, i32, "hash_table", g.hash_vocab), _ptr(q1, i8, "q1", E * d * h1), _ptr(s1, f32, "s1", E * h1),
+        _ptr(b1, f32, "b1", E * h1), _ptr(q2, i8, "q2", E * h * d), _ptr(s2, f32, "s2", E * d), _ptr(b2, f32, "b2", E * d),
+        _ptr(ids, i32, "ids", S * k), _ptr(weights, f32, "weights", S * k), _ptr(y, dt, "y", S * d),
+        _ptr(workspace, None, "workspace"), _bytes(workspace), _stream(stream)))
+
+
+@_allocates_on_stream
+def token_layer_int8(x, q1, s1, q2, s2, *, b1=None, b2=None, act=MOE_ACT_RELU, gated=False, kind=MOE_GATE_TOPK, k=None,
+                     wg=None, bias=None, normalize=0, groups=0, token_ids=None, hash_seed=0, hash_table=None, noise=None,
+                     temperature=0.0, ids=None, weights=None, stream=None):
+    """token_layer with weights and scales from quantize_weights."""
+    S, d = x.shape
+    E, h = _int8_shapes(q1, q2, d, gated)
+    params, ids, weights = _token_layer_choices(x, E, h, act, gated, kind, k, normalize, groups, hash_seed, hash_table,
+                                                temperature, ids, weights)
+    y = torch.empty_like(x)
+    ws = torch.empty((moe_token_layer_int8_workspace_size(params),), dtype=torch.uint8, device=x.device)
+    moe_token_layer_int8(params, x, wg, bias, token_ids, noise, hash_table, q1, s1, b1, q2, s2, b2, ids, weights, y, ws,
+                         stream)
+    return {"y": y, "ids": ids, "weights": weights}

@@ -18,7 +18,8 @@ LIB = os.path.join(PKG, "libhetumoe.so")
 SOURCES = ["base.hip", "gate_bwd.hip", "gate_bwd_tile.hip", "route_valu_f32.hip", "route_valu_bf16.hip", "route_mfma_rs.hip",
            "route_tile_bf16_small.hip", "route_tile_bf16_large.hip", "route_tile_f32.hip", "select_rows.hip",
            "gate.hip", "slots.hip", "layout.hip", "experts_act_bf16.hip", "experts_act_f32.hip", "experts_actgrad_bf16.hip",
-           "experts_actgrad_f32.hip", "experts_store_bf16.hip", "experts_store_f32.hip", "experts.hip", "layer.hip", "grads.hip",
+           "experts_actgrad_f32.hip", "experts_store_bf16.hip", "experts_store_f32.hip", "experts_drop_bf16.hip", "experts_drop_f32.hip", "experts.hip", "layer.hip", "grads.hip",
+           "dropout.hip", "embed.hip", "int8.hip", "experts_int8.hip", "layer_int8.hip",
            "capi.hip"]
 
 # -packed-fp32-ops: no v_pk_{add,mul,fma}_f32 in generated code.

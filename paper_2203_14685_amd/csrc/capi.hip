@@ -912,6 +912,229 @@ TokenLayerPlan plan_token_layer(const moe_token_layer_params* p) {
   return w;
 }
 
+// What moe_token_layer and its form in 8-bit integers are given.
+moe_status check_token_layer_buffers(const char* who, const moe_token_layer_params* p, const void* x, const void* wg,
+                                     const float* bias, const int32_t* token_ids, const float* noise,
+                                     const int32_t* hash_table, const void* w1, const float* b1, const void* w2,
+                                     const float* b2, const int32_t* ids, const float* weights, const void* y) {
+  const moe_gate_params& g = p->gate;
+  const int64_t S = g.S, E = g.E;
+  CHECK(need(x, S, 16, who, "x"));
+  CHECK(need(w1, S, 16, who, "w1"));
+  CHECK(need(w2, S, 16, who, "w2"));
+  CHECK(need(b1, 0, 4, who, "b1"));
+  CHECK(need(b2, 0, 4, who, "b2"));
+  CHECK(need(ids, S, 4, who, "ids"));
+  CHECK(need(weights, S, 4, who, "weights"));
+  CHECK(need(y, S, 16, who, "y"));
+  const bool hash = !p->routed && g.kind == MOE_GATE_HASH, learned = !p->routed && !hash;
+  if (learned) CHECK(need(wg, static_cast<int64_t>(g.d) * E, elt_size(g.dtype), who, "wg"));
+  else if (wg || bias || noise) return fail(MOE_ERR_INVALID_ARG, "%s: wg, bias and noise are for a learned gate", who);
+  CHECK(need(bias, 0, 4, who, "bias"));
+  if (noise && g.temperature == 0.f) return fail(MOE_ERR_INVALID_ARG, "%s: noise needs a temperature > 0", who);
+  CHECK(need(noise, 0, 4, who, "noise"));
+  if (hash) {
+    CHECK(need(token_ids, S, 4, who, "token_ids"));
+    if (g.hash_vocab > 0) CHECK(need(hash_table, g.hash_vocab, 4, who, "hash_table"));
+    else if (hash_table) return fail(MOE_ERR_INVALID_ARG, "%s: hash_table needs hash_vocab > 0", who);
+  } else if (token_ids || hash_table) {
+    return fail(MOE_ERR_INVALID_ARG, "%s: token_ids and hash_table are only for HASH", who);
+  }
+  return MOE_OK;
+}
+
+// The layer's gate: ids and weights, unless they are inputs.
+moe_status token_layer_gate(const char* who, const moe_token_layer_params* p, const void* x, const void* wg,
+                            const float* bias, const int32_t* token_ids, const float* noise, const int32_t* hash_table,
+                            int32_t* ids, float* weights, void* ws, size_t ws_bytes, hipStream_t stream) {
+  if (p->routed) return MOE_OK;
+  const moe_gate_params& g = p->gate;
+  const bool hash = g.kind == MOE_GATE_HASH;
+  LayerGateArgs q{};
+  q.S = g.S; q.d = g.d; q.E = g.E; q.k = g.k; q.kind = g.kind; q.normalize = g.normalize; q.groups = g.groups;
+  q.dtype = g.dtype; q.temperature = g.temperature;
+  q.z = layer_gate_splits(g.d); q.part = static_cast<float*>(ws);
+  q.x = x; q.wg = wg; q.bias = bias; q.noise = noise; q.ids = ids; q.weights = weights;
+  if (!hash && layer_gate_fits(q)) {
+    const hipError_t err = launch_layer_gate(q, stream);
+    return err == hipSuccess ? MOE_OK : hip_fail(err, who);
+  }
+  return gate_select(&g, hash ? nullptr : x, wg, bias, token_ids, noise, hash_table, nullptr, ids, weights, ws, ws_bytes, stream);
+}
+
+// ---------------------------------------------------------------- 8-bit integers
+constexpr int32_t kMaxInt8 = 1 << 17;  // products of 127 x 127: their sums stay below 2^31
+
+moe_status check_int8_widths(const char* who, int32_t d, int32_t h) {
+  if (d % 16 != 0 || h % 16 != 0) return fail(MOE_ERR_UNSUPPORTED, "%s: d = %d and h = %d must be multiples of 16", who, d, h);
+  if (d > kMaxInt8 || h > kMaxInt8) return fail(MOE_ERR_UNSUPPORTED, "%s: d = %d or h = %d beyond %d", who, d, h, kMaxInt8);
+  return MOE_OK;
+}
+
+// Workspace of moe_experts_int8: the integer rows (of xe, then of hidden), their scales, hidden.
+struct ExpertsInt8Plan {
+  size_t off_scale, off_hidden, total;
+};
+ExpertsInt8Plan plan_experts_int8(const moe_experts_params* p) {
+  const size_t rows = static_cast<size_t>(p->E) * static_cast<size_t>(p->capacity);
+  ExpertsInt8Plan w{};
+  w.off_scale = align256(rows * static_cast<size_t>(std::max(p->d, p->h)));
+  w.off_hidden = w.off_scale + align256(rows * 4);
+  w.total = w.off_hidden + align256(rows * static_cast<size_t>(p->h) * elt_size(p->dtype));
+  return w;
+}
+
+struct TokenLayerInt8Plan {
+  LayerArgs a;
+  size_t gate, off_hidden, off_part, off_qx, off_qh, off_sx, off_sh, total;
+};
+TokenLayerInt8Plan plan_token_layer_int8(const moe_token_layer_params* p) {
+  const TokenLayerPlan t = plan_token_layer(p);
+  const size_t S = static_cast<size_t>(p->gate.S), choices = S * static_cast<size_t>(p->gate.k);
+  TokenLayerInt8Plan w{};
+  w.a = t.a;
+  w.a.z2 = layer_int8_splits(w.a);
+  w.gate = t.gate;
+  w.off_hidden = t.off_hidden;
+  w.off_part = w.off_hidden + align256(choices * static_cast<size_t>(p->h) * elt_size(p->gate.dtype));
+  w.off_qx = w.off_part + align256(static_cast<size_t>(w.a.z2) * choices * static_cast<size_t>(p->gate.d) * 4);
+  w.off_qh = w.off_qx + align256(S * static_cast<size_t>(p->gate.d));
+  w.off_sx = w.off_qh + align256(choices * static_cast<size_t>(p->h));
+  w.off_sh = w.off_sx + align256(S * 4);
+  w.total = w.off_sh + align256(choices * 4);
+  return w;
+}
+
+// ---------------------------------------------------------------- dropout
+moe_status check_mask(const moe_dropout_mask* m, const char* who) {
+  if (!m) return fail(MOE_ERR_INVALID_ARG, "%s: mask is NULL", who);
+  if (!(m->p >= 0.f && m->p <= 1.f)) return fail(MOE_ERR_INVALID_ARG, "%s: p must lie in [0, 1]", who);
+  if (!aligned(m->step, 8)) return fail(MOE_ERR_INVALID_ARG, "%s: step is not 8-byte aligned", who);
+  return MOE_OK;
+}
+
+DropArgs drop_args(const moe_dropout_mask* m) {
+  DropArgs d{};
+  d.k0 = static_cast<uint32_t>(m->seed);
+  d.k1 = static_cast<uint32_t>(m->seed >> 32);
+  d.t = static_cast<uint32_t>(std::nearbyint(static_cast<double>(m->p) * 65536.0));
+  d.scale = d.t < 65536u ? static_cast<float>(65536.0 / (65536.0 - d.t)) : 0.f;
+  d.call = m->call;
+  d.step = m->step;
+  return d;
+}
+
+void set_drop(const moe_dropout_mask* m, ExpertArgs& a) {
+  a.drop = drop_args(m);
+  a.drops = a.drop.t > 0;  // nothing dropped: the plain products
+}
+
+// moe_experts, with dropout of hidden where `mask` is not null.
+moe_status run_experts(const char* who, const moe_experts_params* p, const moe_dropout_mask* mask, const void* xe,
+                       const void* w1, const float* b1, const void* w2, const float* b2, const int32_t* counts,
+                       void* pre, void* hidden, void* ye, hipStream_t stream) {
+  CHECK(check_experts(p, who));
+  const int64_t rows = static_cast<int64_t>(p->E) * p->capacity;
+  if (rows > 0) {
+    CHECK(need(w1, 1, 16, who, "w1"));
+    CHECK(need(w2, 1, 16, who, "w2"));
+  }
+  CHECK(need(xe, rows, 16, who, "xe"));
+  CHECK(need(hidden, rows, 16, who, "hidden"));
+  CHECK(need(ye, rows, 16, who, "ye"));
+  CHECK(need(pre, 0, 16, who, "pre"));
+  CHECK(need(b1, 0, 4, who, "b1"));
+  CHECK(need(b2, 0, 4, who, "b2"));
+  CHECK(need(counts, 0, 4, who, "counts"));
+  if (rows == 0) return ok();
+  ExpertArgs a = expert_args(p);
+  a.counts = counts; a.xe = xe; a.w1 = w1; a.w2 = w2; a.b1 = b1; a.b2 = b2; a.pre = pre; a.hidden = hidden; a.ye = ye;
+  if (mask) set_drop(mask, a);
+  const hipError_t err = launch_experts(a, stream);
+  if (err != hipSuccess) return hip_fail(err, who);
+  return ok();
+}
+
+moe_status run_experts_bwd(const char* who, const moe_experts_params* p, const moe_dropout_mask* mask, const void* dye,
+                           const void* xe, const void* w1, const void* w2, const int32_t* counts, const void* pre,
+                           const void* hidden, void* dxe, void* dw1, float* db1, void* dw2, float* db2,
+                           void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  CHECK(check_experts(p, who));
+  const int64_t rows = static_cast<int64_t>(p->E) * p->capacity;
+  const bool back = dxe || dw1 || db1;  // through the activation
+  CHECK(need(dye, rows, 16, who, "dye"));
+  CHECK(need(xe, dw1 ? rows : 0, 16, who, "xe"));
+  CHECK(need(w1, dxe ? rows : 0, 16, who, "w1"));
+  CHECK(need(w2, back ? rows : 0, 16, who, "w2"));
+  CHECK(need(pre, back ? rows : 0, 16, who, "pre"));
+  CHECK(need(hidden, dw2 ? rows : 0, 16, who, "hidden"));
+  CHECK(need(counts, 0, 4, who, "counts"));
+  CHECK(need(dxe, 0, 16, who, "dxe"));
+  CHECK(need(dw1, 0, 16, who, "dw1"));
+  CHECK(need(dw2, 0, 16, who, "dw2"));
+  CHECK(need(db1, 0, 4, who, "db1"));
+  CHECK(need(db2, 0, 4, who, "db2"));
+  const ExpertsBwdPlan w = plan_experts_bwd(p);
+  CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
+  char* ws = static_cast<char*>(workspace);
+  ExpertArgs a = expert_args(p);
+  a.counts = counts; a.dye = dye; a.xe = xe; a.w1 = w1; a.w2 = w2;
+  a.pre = const_cast<void*>(pre); a.hidden = const_cast<void*>(hidden);
+  a.dpre = ws + w.off_dpre;
+  a.colsum = reinterpret_cast<float*>(ws + w.off_col);
+  a.rowsum = reinterpret_cast<float*>(ws + w.off_row);
+  a.dxe = dxe; a.dw1 = dw1; a.db1 = db1; a.dw2 = dw2; a.db2 = db2;
+  if (mask) set_drop(mask, a);
+  const hipError_t err = launch_experts_bwd(a, stream);
+  if (err != hipSuccess) return hip_fail(err, who);
+  return ok();
+}
+
+// ---------------------------------------------------------------- embedding
+moe_status check_embed(const moe_embed_params* p, const char* who, bool bwd) {
+  if (!p) return fail(MOE_ERR_INVALID_ARG, "%s: params is NULL", who);
+  if (p->dtype != MOE_F32 && p->dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: dtype %d unknown", who, p->dtype);
+  if (p->T < 0 || p->V < 1 || p->d < 1)
+    return fail(MOE_ERR_INVALID_ARG, "%s: need T >= 0, V >= 1, d >= 1 (got T=%d V=%d d=%d)", who, p->T, p->V, p->d);
+  if (!std::isfinite(p->scale)) return fail(MOE_ERR_INVALID_ARG, "%s: scale must be finite", who);
+  if (p->accumulate != 0 && (p->accumulate != 1 || !bwd))
+    return fail(MOE_ERR_INVALID_ARG, "%s: accumulate must be 0%s", who, bwd ? " or 1" : "");
+  if (p->d * static_cast<int64_t>(elt_size(p->dtype)) % 16 != 0)
+    return fail(MOE_ERR_UNSUPPORTED, "%s: rows of d = %d elements are no multiple of 16 bytes", who, p->d);
+  if (p->d > kMaxWidth) return fail(MOE_ERR_UNSUPPORTED, "%s: d = %d beyond %d", who, p->d, kMaxWidth);
+  if (bwd && p->T > (1 << 30)) return fail(MOE_ERR_UNSUPPORTED, "%s: more than 2^30 tokens", who);
+  return MOE_OK;
+}
+
+EmbedArgs embed_args(const moe_embed_params* p) {
+  EmbedArgs a{};
+  a.T = p->T; a.V = p->V; a.d = p->d; a.dtype = p->dtype; a.accumulate = p->accumulate; a.scale = p->scale;
+  a.chunk = embed_chunk_length(p->T, p->d, p->dtype);
+  return a;
+}
+
+// Workspace of moe_embed_bwd: the sorted ids and their tokens, twice where passes over digits sort
+// them, those passes' counts, and the parts of the sums that cross chunks.
+struct EmbedBwdPlan {
+  size_t off_order, off_keys2, off_order2, off_counts, off_totals, off_crossers, off_crossing, off_part, total;
+};
+EmbedBwdPlan plan_embed_bwd(const moe_embed_params* p) {
+  const EmbedArgs a = embed_args(p);
+  const size_t list = align256(static_cast<size_t>(p->T) * 4), chunks = static_cast<size_t>(embed_chunks(a));
+  const bool passes = p->T > kEmbedRankMax;
+  EmbedBwdPlan w{};
+  w.off_order = list;
+  w.off_keys2 = 2 * list;
+  w.off_order2 = w.off_keys2 + (passes ? list : 0);
+  w.off_counts = w.off_order2 + (passes ? list : 0);
+  w.off_totals = w.off_counts + (passes ? align256(static_cast<size_t>(kEmbedDigits) * embed_sort_tiles(p->T) * 4) : 0);
+  w.off_crossers = w.off_totals + (passes ? align256(kEmbedDigits * 4) : 0);
+  w.off_crossing = w.off_crossers + align256(chunks * 4);
+  w.off_part = w.off_crossing + align256(4);
+  w.total = w.off_part + align256(chunks * 2 * static_cast<size_t>(p->d) * 4);
+  return w;
+}
+
 // ---------------------------------------------------------------- gradient norm
 static_assert(kLayerMaxTokens == MOE_TOKEN_LAYER_MAX, "tokens of the layer");
 
@@ -1011,26 +1234,15 @@ extern "C" {
 
 moe_status moe_experts(const moe_experts_params* p, const void* xe, const void* w1, const float* b1, const void* w2,
                        const float* b2, const int32_t* counts, void* pre, void* hidden, void* ye, hipStream_t stream) {
-  static const char* who = "moe_experts";
-  CHECK(check_experts(p, who));
-  const int64_t rows = static_cast<int64_t>(p->E) * p->capacity;
-  if (rows > 0) {
-    CHECK(need(w1, 1, 16, who, "w1"));
-    CHECK(need(w2, 1, 16, who, "w2"));
-  }
-  CHECK(need(xe, rows, 16, who, "xe"));
-  CHECK(need(hidden, rows, 16, who, "hidden"));
-  CHECK(need(ye, rows, 16, who, "ye"));
-  CHECK(need(pre, 0, 16, who, "pre"));
-  CHECK(need(b1, 0, 4, who, "b1"));
-  CHECK(need(b2, 0, 4, who, "b2"));
-  CHECK(need(counts, 0, 4, who, "counts"));
-  if (rows == 0) return ok();
-  ExpertArgs a = expert_args(p);
-  a.counts = counts; a.xe = xe; a.w1 = w1; a.w2 = w2; a.b1 = b1; a.b2 = b2; a.pre = pre; a.hidden = hidden; a.ye = ye;
-  const hipError_t err = launch_experts(a, stream);
-  if (err != hipSuccess) return hip_fail(err, "moe_experts: kernel launch");
-  return ok();
+  return run_experts("moe_experts", p, nullptr, xe, w1, b1, w2, b2, counts, pre, hidden, ye, stream);
+}
+
+moe_status moe_experts_dropout(const moe_experts_params* p, const moe_dropout_mask* mask, const void* xe, const void* w1,
+                               const float* b1, const void* w2, const float* b2, const int32_t* counts, void* pre,
+                               void* hidden, void* ye, hipStream_t stream) {
+  static const char* who = "moe_experts_dropout";
+  CHECK(check_mask(mask, who));
+  return run_experts(who, p, mask, xe, w1, b1, w2, b2, counts, pre, hidden, ye, stream);
 }
 
 moe_status moe_experts_bwd_workspace_size(const moe_experts_params* p, size_t* bytes) {
@@ -1045,35 +1257,18 @@ moe_status moe_experts_bwd(const moe_experts_params* p, const void* dye, const v
                            const int32_t* counts, const void* pre, const void* hidden, void* dxe, void* dw1,
                            float* db1, void* dw2, float* db2, void* workspace, size_t workspace_bytes,
                            hipStream_t stream) {
-  static const char* who = "moe_experts_bwd";
-  CHECK(check_experts(p, who));
-  const int64_t rows = static_cast<int64_t>(p->E) * p->capacity;
-  const bool back = dxe || dw1 || db1;  // through the activation
-  CHECK(need(dye, rows, 16, who, "dye"));
-  CHECK(need(xe, dw1 ? rows : 0, 16, who, "xe"));
-  CHECK(need(w1, dxe ? rows : 0, 16, who, "w1"));
-  CHECK(need(w2, back ? rows : 0, 16, who, "w2"));
-  CHECK(need(pre, back ? rows : 0, 16, who, "pre"));
-  CHECK(need(hidden, dw2 ? rows : 0, 16, who, "hidden"));
-  CHECK(need(counts, 0, 4, who, "counts"));
-  CHECK(need(dxe, 0, 16, who, "dxe"));
-  CHECK(need(dw1, 0, 16, who, "dw1"));
-  CHECK(need(dw2, 0, 16, who, "dw2"));
-  CHECK(need(db1, 0, 4, who, "db1"));
-  CHECK(need(db2, 0, 4, who, "db2"));
-  const ExpertsBwdPlan w = plan_experts_bwd(p);
-  CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
-  char* ws = static_cast<char*>(workspace);
-  ExpertArgs a = expert_args(p);
-  a.counts = counts; a.dye = dye; a.xe = xe; a.w1 = w1; a.w2 = w2;
-  a.pre = const_cast<void*>(pre); a.hidden = const_cast<void*>(hidden);
-  a.dpre = ws + w.off_dpre;
-  a.colsum = reinterpret_cast<float*>(ws + w.off_col);
-  a.rowsum = reinterpret_cast<float*>(ws + w.off_row);
-  a.dxe = dxe; a.dw1 = dw1; a.db1 = db1; a.dw2 = dw2; a.db2 = db2;
-  const hipError_t err = launch_experts_bwd(a, stream);
-  if (err != hipSuccess) return hip_fail(err, "moe_experts_bwd: kernel launch");
-  return ok();
+  return run_experts_bwd("moe_experts_bwd", p, nullptr, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2,
+                         workspace, workspace_bytes, stream);
+}
+
+moe_status moe_experts_dropout_bwd(const moe_experts_params* p, const moe_dropout_mask* mask, const void* dye,
+                                   const void* xe, const void* w1, const void* w2, const int32_t* counts,
+                                   const void* pre, const void* hidden, void* dxe, void* dw1, float* db1, void* dw2,
+                                   float* db2, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  static const char* who = "moe_experts_dropout_bwd";
+  CHECK(check_mask(mask, who));
+  return run_experts_bwd(who, p, mask, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace,
+                         workspace_bytes, stream);
 }
 
 moe_status moe_token_layer_workspace_size(const moe_token_layer_params* p, size_t* bytes) {
@@ -1090,46 +1285,12 @@ moe_status moe_token_layer(const moe_token_layer_params* p, const void* x, const
                            void* workspace, size_t workspace_bytes, hipStream_t stream) {
   static const char* who = "moe_token_layer";
   CHECK(check_token_layer(p, who));
-  const moe_gate_params& g = p->gate;
-  const int64_t S = g.S, E = g.E;
-  CHECK(need(x, S, 16, who, "x"));
-  CHECK(need(w1, S, 16, who, "w1"));
-  CHECK(need(w2, S, 16, who, "w2"));
-  CHECK(need(b1, 0, 4, who, "b1"));
-  CHECK(need(b2, 0, 4, who, "b2"));
-  CHECK(need(ids, S, 4, who, "ids"));
-  CHECK(need(weights, S, 4, who, "weights"));
-  CHECK(need(y, S, 16, who, "y"));
-  const bool hash = !p->routed && g.kind == MOE_GATE_HASH, learned = !p->routed && !hash;
-  if (learned) CHECK(need(wg, static_cast<int64_t>(g.d) * E, elt_size(g.dtype), who, "wg"));
-  else if (wg || bias || noise) return fail(MOE_ERR_INVALID_ARG, "%s: wg, bias and noise are for a learned gate", who);
-  CHECK(need(bias, 0, 4, who, "bias"));
-  if (noise && g.temperature == 0.f) return fail(MOE_ERR_INVALID_ARG, "%s: noise needs a temperature > 0", who);
-  CHECK(need(noise, 0, 4, who, "noise"));
-  if (hash) {
-    CHECK(need(token_ids, S, 4, who, "token_ids"));
-    if (g.hash_vocab > 0) CHECK(need(hash_table, g.hash_vocab, 4, who, "hash_table"));
-    else if (hash_table) return fail(MOE_ERR_INVALID_ARG, "%s: hash_table needs hash_vocab > 0", who);
-  } else if (token_ids || hash_table) {
-    return fail(MOE_ERR_INVALID_ARG, "%s: token_ids and hash_table are only for HASH", who);
-  }
+  CHECK(check_token_layer_buffers(who, p, x, wg, bias, token_ids, noise, hash_table, w1, b1, w2, b2, ids, weights, y));
   TokenLayerPlan w = plan_token_layer(p);
   CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
-  if (S == 0) return ok();
+  if (p->gate.S == 0) return ok();
   char* ws = static_cast<char*>(workspace);
-  if (!p->routed) {
-    LayerGateArgs q{};
-    q.S = g.S; q.d = g.d; q.E = g.E; q.k = g.k; q.kind = g.kind; q.normalize = g.normalize; q.groups = g.groups;
-    q.dtype = g.dtype; q.temperature = g.temperature;
-    q.z = layer_gate_splits(g.d); q.part = reinterpret_cast<float*>(ws);
-    q.x = x; q.wg = wg; q.bias = bias; q.noise = noise; q.ids = ids; q.weights = weights;
-    if (learned && layer_gate_fits(q)) {
-      const hipError_t err = launch_layer_gate(q, stream);
-      if (err != hipSuccess) return hip_fail(err, "moe_token_layer: gate kernel launch");
-    } else {
-      CHECK(gate_select(&g, hash ? nullptr : x, wg, bias, token_ids, noise, hash_table, nullptr, ids, weights, ws, w.gate, stream));
-    }
-  }
+  CHECK(token_layer_gate(who, p, x, wg, bias, token_ids, noise, hash_table, ids, weights, ws, w.gate, stream));
   LayerArgs& a = w.a;
   a.x = x; a.w1 = w1; a.w2 = w2; a.b1 = b1; a.b2 = b2; a.ids = ids; a.weights = weights; a.y = y;
   a.hidden = ws + w.off_hidden;
@@ -1184,6 +1345,178 @@ moe_status moe_grad_clip(const moe_grad_tensor* tensors, int32_t count, const do
   });
   if (err == hipSuccess && first && norm) err = launch_grad_scale(GradList{}, false, sumsq, max_norm, norm, stream);
   if (err != hipSuccess) return hip_fail(err, "moe_grad_clip: kernel launch");
+  return ok();
+}
+
+moe_status moe_dropout(const moe_dropout_mask* mask, int64_t n, int32_t dtype, const void* x, const void* residual,
+                       void* y, hipStream_t stream) {
+  static const char* who = "moe_dropout";
+  CHECK(check_mask(mask, who));
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: dtype %d unknown", who, dtype);
+  if (n < 0) return fail(MOE_ERR_INVALID_ARG, "%s: n < 0", who);
+  if (n > (int64_t(1) << 44)) return fail(MOE_ERR_UNSUPPORTED, "%s: more than 2^44 elements", who);
+  CHECK(need(x, n, 16, who, "x"));
+  CHECK(need(residual, 0, 16, who, "residual"));
+  CHECK(need(y, n, 16, who, "y"));
+  if (n == 0) return ok();
+  const hipError_t err = launch_dropout(drop_args(mask), n, dtype, x, residual, y, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_dropout: kernel launch");
+  return ok();
+}
+
+moe_status moe_embed(const moe_embed_params* p, const int32_t* ids, const void* table, void* y, hipStream_t stream) {
+  static const char* who = "moe_embed";
+  CHECK(check_embed(p, who, false));
+  CHECK(need(ids, p->T, 4, who, "ids"));
+  CHECK(need(table, p->T, 16, who, "table"));
+  CHECK(need(y, p->T, 16, who, "y"));
+  if (p->T == 0) return ok();
+  EmbedArgs a = embed_args(p);
+  a.ids = ids; a.table = table; a.y = y;
+  const hipError_t err = launch_embed(a, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_embed: kernel launch");
+  return ok();
+}
+
+moe_status moe_embed_bwd_workspace_size(const moe_embed_params* p, size_t* bytes) {
+  if (!bytes) return fail(MOE_ERR_INVALID_ARG, "bytes is NULL");
+  CHECK(check_embed(p, "moe_embed_bwd_workspace_size", true));
+  *bytes = plan_embed_bwd(p).total;
+  return ok();
+}
+
+moe_status moe_embed_bwd(const moe_embed_params* p, const void* dy, const int32_t* ids, void* dtable, void* workspace,
+                         size_t workspace_bytes, hipStream_t stream) {
+  static const char* who = "moe_embed_bwd";
+  CHECK(check_embed(p, who, true));
+  CHECK(need(dy, p->T, 16, who, "dy"));
+  CHECK(need(ids, p->T, 4, who, "ids"));
+  CHECK(need(dtable, 1, 16, who, "dtable"));
+  const EmbedBwdPlan w = plan_embed_bwd(p);
+  CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
+  char* ws = static_cast<char*>(workspace);
+  auto ints = [&](size_t off) { return reinterpret_cast<int32_t*>(ws + off); };
+  EmbedArgs a = embed_args(p);
+  a.ids = ids; a.dy = dy; a.dtable = dtable;
+  a.keys = ints(0); a.order = ints(w.off_order);
+  a.crossers = ints(w.off_crossers); a.crossing = ints(w.off_crossing);
+  a.part = reinterpret_cast<float*>(ws + w.off_part);
+  const hipError_t err = launch_embed_bwd(a, ints(w.off_keys2), ints(w.off_order2), ints(w.off_counts),
+                                          ints(w.off_totals), stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_embed_bwd: kernel launch");
+  return ok();
+}
+
+moe_status moe_quantize(int64_t rows, int32_t n, int32_t dtype, const void* x, int8_t* q, float* scale,
+                        hipStream_t stream) {
+  static const char* who = "moe_quantize";
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: dtype %d unknown", who, dtype);
+  if (rows < 0 || n < 1) return fail(MOE_ERR_INVALID_ARG, "%s: need rows >= 0 and n >= 1, got %lld and %d", who, static_cast<long long>(rows), n);
+  if (n % 16 != 0) return fail(MOE_ERR_UNSUPPORTED, "%s: rows of n = %d elements, a multiple of 16 is required", who, n);
+  if (rows > (int64_t(1) << 36)) return fail(MOE_ERR_UNSUPPORTED, "%s: more than 2^36 rows", who);
+  CHECK(need(x, rows, 16, who, "x"));
+  CHECK(need(q, rows, 16, who, "q"));
+  CHECK(need(scale, rows, 4, who, "scale"));
+  if (rows == 0) return ok();
+  QuantArgs a{};
+  a.rows = rows; a.n = n; a.dtype = dtype; a.x = x; a.q = q; a.scale = scale;
+  const hipError_t err = launch_quantize(a, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_quantize: kernel launch");
+  return ok();
+}
+
+moe_status moe_quantize_weights(int32_t E, int32_t K, int32_t N, int32_t dtype, const void* w, int8_t* q, float* scale,
+                                hipStream_t stream) {
+  static const char* who = "moe_quantize_weights";
+  if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: dtype %d unknown", who, dtype);
+  if (E < 1 || E > 1024) return fail(MOE_ERR_INVALID_ARG, "%s: E = %d outside [1, 1024]", who, E);
+  if (K < 1 || N < 1) return fail(MOE_ERR_INVALID_ARG, "%s: need K >= 1 and N >= 1, got %d and %d", who, K, N);
+  if (K % 16 != 0 || N % 16 != 0) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d and N = %d must be multiples of 16", who, K, N);
+  if (K > kMaxInt8 || N > 2 * kMaxInt8) return fail(MOE_ERR_UNSUPPORTED, "%s: K = %d beyond %d or N = %d beyond %d", who, K, kMaxInt8, N, 2 * kMaxInt8);
+  CHECK(need(w, 1, 16, who, "w"));
+  CHECK(need(q, 1, 16, who, "q"));
+  CHECK(need(scale, 1, 4, who, "scale"));
+  const hipError_t err = launch_quantize_weights(E, K, N, dtype, w, q, scale, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_quantize_weights: kernel launch");
+  return ok();
+}
+
+moe_status moe_experts_int8_workspace_size(const moe_experts_params* p, size_t* bytes) {
+  static const char* who = "moe_experts_int8_workspace_size";
+  if (!bytes) return fail(MOE_ERR_INVALID_ARG, "bytes is NULL");
+  CHECK(check_experts(p, who));
+  CHECK(check_int8_widths(who, p->d, p->h));
+  *bytes = plan_experts_int8(p).total;
+  return ok();
+}
+
+moe_status moe_experts_int8(const moe_experts_params* p, const void* xe, const int8_t* q1, const float* s1,
+                            const float* b1, const int8_t* q2, const float* s2, const float* b2, const int32_t* counts,
+                            void* ye, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  static const char* who = "moe_experts_int8";
+  CHECK(check_experts(p, who));
+  CHECK(check_int8_widths(who, p->d, p->h));
+  const int64_t rows = static_cast<int64_t>(p->E) * p->capacity;
+  CHECK(need(xe, rows, 16, who, "xe"));
+  CHECK(need(q1, rows, 16, who, "q1"));
+  CHECK(need(s1, rows, 4, who, "s1"));
+  CHECK(need(b1, 0, 4, who, "b1"));
+  CHECK(need(q2, rows, 16, who, "q2"));
+  CHECK(need(s2, rows, 4, who, "s2"));
+  CHECK(need(b2, 0, 4, who, "b2"));
+  CHECK(need(counts, 0, 4, who, "counts"));
+  CHECK(need(ye, rows, 16, who, "ye"));
+  const ExpertsInt8Plan w = plan_experts_int8(p);
+  CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
+  if (rows == 0) return ok();
+  char* ws = static_cast<char*>(workspace);
+  ExpertInt8Args a{};
+  a.E = p->E; a.C = p->capacity; a.d = p->d; a.h = p->h; a.act = p->act; a.gated = p->gated; a.dtype = p->dtype;
+  a.counts = counts; a.xe = xe; a.q1 = q1; a.q2 = q2; a.s1 = s1; a.s2 = s2; a.b1 = b1; a.b2 = b2; a.ye = ye;
+  a.q = reinterpret_cast<int8_t*>(ws);
+  a.scale = reinterpret_cast<float*>(ws + w.off_scale);
+  a.hidden = ws + w.off_hidden;
+  const hipError_t err = launch_experts_int8(a, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_experts_int8: kernel launch");
+  return ok();
+}
+
+moe_status moe_token_layer_int8_workspace_size(const moe_token_layer_params* p, size_t* bytes) {
+  static const char* who = "moe_token_layer_int8_workspace_size";
+  if (!bytes) return fail(MOE_ERR_INVALID_ARG, "bytes is NULL");
+  CHECK(check_token_layer(p, who));
+  CHECK(check_int8_widths(who, p->gate.d, p->h));
+  *bytes = plan_token_layer_int8(p).total;
+  return ok();
+}
+
+moe_status moe_token_layer_int8(const moe_token_layer_params* p, const void* x, const void* wg, const float* bias,
+                                const int32_t* token_ids, const float* noise, const int32_t* hash_table,
+                                const int8_t* q1, const float* s1, const float* b1, const int8_t* q2, const float* s2,
+                                const float* b2, int32_t* ids, float* weights, void* y, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream) {
+  static const char* who = "moe_token_layer_int8";
+  CHECK(check_token_layer(p, who));
+  CHECK(check_int8_widths(who, p->gate.d, p->h));
+  CHECK(check_token_layer_buffers(who, p, x, wg, bias, token_ids, noise, hash_table, q1, b1, q2, b2, ids, weights, y));
+  CHECK(need(s1, p->gate.S, 4, who, "s1"));
+  CHECK(need(s2, p->gate.S, 4, who, "s2"));
+  TokenLayerInt8Plan w = plan_token_layer_int8(p);
+  CHECK(check_workspace(who, workspace, workspace_bytes, w.total));
+  if (p->gate.S == 0) return ok();
+  char* ws = static_cast<char*>(workspace);
+  CHECK(token_layer_gate(who, p, x, wg, bias, token_ids, noise, hash_table, ids, weights, ws, w.gate, stream));
+  LayerInt8Args b{};
+  b.a = w.a;
+  LayerArgs& a = b.a;
+  a.x = x; a.w1 = q1; a.w2 = q2; a.b1 = b1; a.b2 = b2; a.ids = ids; a.weights = weights; a.y = y;
+  a.hidden = ws + w.off_hidden;
+  a.part = reinterpret_cast<float*>(ws + w.off_part);
+  b.s1 = s1; b.s2 = s2;
+  b.qx = reinterpret_cast<int8_t*>(ws + w.off_qx); b.qh = reinterpret_cast<int8_t*>(ws + w.off_qh);
+  b.sx = reinterpret_cast<float*>(ws + w.off_sx); b.sh = reinterpret_cast<float*>(ws + w.off_sh);
+  const hipError_t err = launch_layer_int8(b, stream);
+  if (err != hipSuccess) return hip_fail(err, "moe_token_layer_int8: kernel launch");
   return ok();
 }
 

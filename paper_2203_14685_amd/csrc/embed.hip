@@ -1,0 +1,504 @@
+// The embedding rows that a layer starts from, and their table's gradient.
+//
+// Forward: a gather of rows, bound by the rows written.  Backward: the tokens are sorted by id
+// (stable, so that every sum runs over its tokens in their order), then the rows' gradients are
+// added in runs of equal ids: the sorted tokens are cut into chunks of equal length, however
+// the ids are spread, one group of lanes per chunk and strip of columns.  A run inside one chunk is
+// written at once; the parts of a run that crosses chunks go to the workspace and are added
+// by a last launch.  Rows of the table that no token names are cleared beside it, which is
+// most of what there is to write.
+#include <algorithm>
+
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace hetumoe {
+
+namespace {
+
+// ---------------------------------------------------------------- forward
+// A block's threads as groups of `tpr` (a power of two) along a row, R rows per group at a time.
+template <class T, int R>
+__global__ __launch_bounds__(kBlock) void embed_kernel(const int32_t* ids, const T* table, T* y, int T_, int V, int d,
+                                                       float scale, int tpr) {
+  constexpr int PE = Chunk<T>::kElems;
+  const int group = threadIdx.x / tpr, lane = threadIdx.x % tpr;
+  const int64_t row0 = (long_block() * (kBlock / tpr) + group) * R;
+  if (row0 >= T_) return;
+  int id[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) id[r] = row0 + r < T_ ? ids[row0 + r] : -1;
+  for (int c = lane * PE; c < d; c += tpr * PE) {
+    u32x4 v[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const bool in = id[r] >= 0 && id[r] < V;
+      v[r] = in ? *reinterpret_cast<const u32x4*>(table + static_cast<int64_t>(id[r]) * d + c) : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row0 + r >= T_) continue;
+      const bool in = id[r] >= 0 && id[r] < V;
+      float f[PE];
+      Chunk<T>::unpack(v[r], f);
+#pragma unroll
+      for (int q = 0; q < PE; ++q) f[q] = in ? f[q] * scale : 0.f;  // zeros of padding whatever the scale's sign
+      *reinterpret_cast<u32x4*>(y + (row0 + r) * d + c) = Chunk<T>::pack(f);
+    }
+  }
+}
+
+template <class T>
+hipError_t run_embed(const EmbedArgs& a, hipStream_t st) {
+  const int pieces = a.d / Chunk<T>::kElems;
+  int tpr = 1;
+  while (tpr < pieces && tpr < kBlock) tpr *= 2;
+  const int groups = kBlock / tpr;
+  const T* table = static_cast<const T*>(a.table);
+  T* y = static_cast<T*>(a.y);
+  const auto blocks = [&](int r) {
+    return long_grid((a.T + static_cast<int64_t>(groups) * r - 1) / (static_cast<int64_t>(groups) * r));
+  };
+  // four rows at once where blocks are many, so that four loads are in flight
+  if (a.T >= groups * 4 * 512) embed_kernel<T, 4><<<blocks(4), kBlock, 0, st>>>(a.ids, table, y, a.T, a.V, a.d, a.scale, tpr);
+  else embed_kernel<T, 1><<<blocks(1), kBlock, 0, st>>>(a.ids, table, y, a.T, a.V, a.d, a.scale, tpr);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------- sorting the tokens
+// Keys: the id, V for padding (behind all others).
+__device__ __forceinline__ int embed_key(const int32_t* ids, int64_t t, int V) {
+  const int id = ids[t];
+  return id >= 0 && id < V ? id : V;
+}
+
+// Few tokens: token t's place is the number of keys below its own, and of equal ones before
+// it.  A block places 64 tokens, its waves count in a share of all keys each.  (T^2 comparisons;
+// one launch where the passes below take seven.)
+constexpr int kRankWaves = 16;
+constexpr int kRankKeys = 1024;  // keys in LDS at a time
+__global__ __launch_bounds__(kRankWaves* kWave) void embed_rank_kernel(EmbedArgs a) {
+  __shared__ int keys[kRankKeys];
+  __shared__ int part[kRankWaves][kWave];
+  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  const int t = blockIdx.x * kWave + lane;
+  const int mine = t < a.T ? embed_key(a.ids, t, a.V) : 0x7fffffff;
+  int below = 0;
+  for (int base = 0; base < a.T; base += kRankKeys) {
+    __syncthreads();
+    for (int i = threadIdx.x; i < kRankKeys; i += kRankWaves * kWave)
+      keys[i] = base + i < a.T ? embed_key(a.ids, base + i, a.V) : 0x7fffffff;  // behind all
+    __syncthreads();
+    const int n = kRankKeys / kRankWaves, from = wave * n;
+    for (int i = 0; i < n; i += 4) {
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int k = keys[from + i + q], u = base + from + i + q;
+        below += k < mine || (k == mine && u < t) ? 1 : 0;
+      }
+    }
+  }
+  part[wave][lane] = below;
+  __syncthreads();
+  if (wave == 0 && t < a.T) {
+    int at = 0;
+#pragma unroll
+    for (int w = 0; w < kRankWaves; ++w) at += part[w][lane];
+    a.keys[at] = mine;
+    a.order[at] = t;
+  }
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.crossing = 0;
+}
+
+// More tokens: passes over digits of the key, lowest first, each stable.  A tile of keys
+// belongs to one block, its waves hold consecutive parts of it.
+constexpr int kDigits = kEmbedDigits;
+static_assert(kDigits == kBlock, "a thread per digit");
+constexpr int kSortItems = 4;                       // keys per thread
+constexpr int kSortTile = kBlock * kSortItems;
+
+__device__ __forceinline__ int sort_key(const EmbedSortPass& s, int64_t i) {
+  return s.first ? embed_key(s.ids, i, s.V) : s.keys_in[i];
+}
+
+__global__ __launch_bounds__(kBlock) void sort_count_kernel(EmbedSortPass s) {
+  __shared__ int count[kDigits];
+  count[threadIdx.x] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < kSortItems; ++q) {
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * kSortTile + q * kBlock + threadIdx.x;
+    if (i < s.T) atomicAdd(&count[(sort_key(s, i) >> s.shift) & (kDigits - 1)], 1);
+  }
+  __syncthreads();
+  s.counts[static_cast<int64_t>(threadIdx.x) * s.tiles + blockIdx.x] = count[threadIdx.x];
+  if (blockIdx.x == 0 && threadIdx.x == 0) *s.crossing = 0;
+}
+
+// Block `digit`: its counts of the tiles become the sums of those before; their total.
+__global__ __launch_bounds__(kBlock) void sort_scan_kernel(EmbedSortPass s) {
+  __shared__ int wave_sum[kWavesPerBlock];
+  int32_t* c = s.counts + static_cast<int64_t>(blockIdx.x) * s.tiles;
+  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  int carry = 0;
+  for (int base = 0; base < s.tiles; base += kBlock) {
+    const int i = base + threadIdx.x;
+    const int v = i < s.tiles ? c[i] : 0;
+    int sum = v;
+#pragma unroll
+    for (int k = 1; k < kWave; k <<= 1) {
+      const int up = __shfl_up(sum, k);
+      sum += lane >= k ? up : 0;
+    }
+    if (lane == kWave - 1) wave_sum[wave] = sum;
+    __syncthreads();
+    int before = carry;
+#pragma unroll
+    for (int w = 0; w < kWavesPerBlock; ++w) {
+      before += w < wave ? wave_sum[w] : 0;
+      carry += wave_sum[w];
+    }
+    if (i < s.tiles) c[i] = before + sum - v;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) s.totals[blockIdx.x] = carry;
+}
+
+__global__ __launch_bounds__(kBlock) void sort_place_kernel(EmbedSortPass s) {
+  __shared__ int at[kWavesPerBlock][kDigits];  // keys of a wave's part by digit, then their first place
+  __shared__ int wave_sum[kWavesPerBlock];
+  const int lane = lane_id(), wave = threadIdx.x / kWave, tid = threadIdx.x;
+#pragma unroll
+  for (int w = 0; w < kWavesPerBlock; ++w) at[w][tid] = 0;
+  __syncthreads();
+  const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile + wave * (kWave * kSortItems);
+  int key[kSortItems], token[kSortItems], rank[kSortItems];
+#pragma unroll
+  for (int q = 0; q < kSortItems; ++q) {
+    const int64_t i = base + q * kWave + lane;
+    key[q] = i < s.T ? sort_key(s, i) : 0;
+    token[q] = i < s.T && !s.first ? s.order_in[i] : static_cast<int>(i);
+  }
+#pragma unroll
+  for (int q = 0; q < kSortItems; ++q) {
+    const bool in = base + q * kWave + lane < s.T;
+    const int digit = (key[q] >> s.shift) & (kDigits - 1);
+    uint64_t same = __ballot(in);
+#pragma unroll
+    for (int b = 0; b < 8; ++b) {
+      const uint64_t set = __ballot(digit >> b & 1);
+      same &= (digit >> b & 1) ? set : ~set;
+    }
+    const int before = at[wave][digit];
+    rank[q] = before + popc_below(same);
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    if (in && popc_below(same) == 0) at[wave][digit] = before + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  }
+  // keys of smaller digits, by a sum over the digits' totals
+  const int total = s.totals[tid];
+  int sum = total;
+#pragma unroll
+  for (int k = 1; k < kWave; k <<= 1) {
+    const int up = __shfl_up(sum, k);
+    sum += lane >= k ? up : 0;
+  }
+  if (lane == kWave - 1) wave_sum[wave] = sum;
+  __syncthreads();
+  int first = sum - total;
+#pragma unroll
+  for (int w = 0; w < kWavesPerBlock; ++w) first += w < wave ? wave_sum[w] : 0;
+  first += s.counts[static_cast<int64_t>(tid) * s.tiles + blockIdx.x];
+#pragma unroll
+  for (int w = 0; w < kWavesPerBlock; ++w) {
+    const int n = at[w][tid];
+    at[w][tid] = first;
+    first += n;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int q = 0; q < kSortItems; ++q) {
+    if (base + q * kWave + lane >= s.T) continue;
+    const int to = at[wave][(key[q] >> s.shift) & (kDigits - 1)] + rank[q];
+    s.keys_out[to] = key[q];
+    s.order_out[to] = token[q];
+  }
+}
+
+// ---------------------------------------------------------------- sums of runs
+// Writes scale * sum (+ what is there) to a piece of the table's gradient.
+template <class T>
+__device__ __forceinline__ void embed_write(const EmbedArgs& a, int key, int c, const float* sum) {
+  constexpr int PE = Chunk<T>::kElems;
+  u32x4* p = reinterpret_cast<u32x4*>(static_cast<T*>(a.dtable) + static_cast<int64_t>(key) * a.d + c);
+  float f[PE];
+  if (a.accumulate) {
+    Chunk<T>::unpack(*p, f);
+#pragma unroll
+    for (int q = 0; q < PE; ++q) f[q] += a.scale * sum[q];
+  } else {
+#pragma unroll
+    for (int q = 0; q < PE; ++q) f[q] = a.scale * sum[q];
+  }
+  *p = Chunk<T>::pack(f);
+}
+
+// Which part of a run that crosses chunks a partial sum is: kHead goes on from the chunk
+// before, kTail starts in its chunk and goes on in the next.
+constexpr int kHead = 0, kTail = 1;
+template <class T>
+__device__ __forceinline__ float* embed_part(const EmbedArgs& a, int64_t chunk, int which, int c) {
+  return a.part + (chunk * 2 + which) * a.d + c;
+}
+
+// L lanes per chunk and strip of L pieces; chunks of a.chunk sorted tokens.
+template <class T, int L>
+__device__ __forceinline__ void embed_chunk(const EmbedArgs& a, int64_t unit) {
+  constexpr int PE = Chunk<T>::kElems, U = 8;
+  const int strips = (a.d + L * PE - 1) / (L * PE);
+  const int64_t chunk = unit / strips;
+  const int strip = static_cast<int>(unit - chunk * strips);
+  const int64_t lo = chunk * a.chunk, hi = min(static_cast<int64_t>(a.T), lo + a.chunk);
+  if (lo >= a.T) return;
+  const int c = (strip * L + lane_id() % L) * PE;
+  const bool in = c < a.d;
+  const T* dy = static_cast<const T*>(a.dy) + (in ? c : 0);
+  const int last_key = a.keys[hi - 1];
+  const bool from_left = lo > 0 && a.keys[lo - 1] == a.keys[lo];
+  const bool to_right = hi < a.T && a.keys[hi] == last_key;
+  float sum[PE];
+#pragma unroll
+  for (int q = 0; q < PE; ++q) sum[q] = 0.f;
+  int cur = a.keys[lo];
+  bool head = from_left;
+  auto flush = [&](bool right) {
+    if (!in || cur >= a.V) return;
+    if (head || right) {
+      float* p = embed_part<T>(a, chunk, head ? kHead : kTail, c);
+#pragma unroll
+      for (int q = 0; q < PE; q += 4) *reinterpret_cast<u32x4*>(p + q) = Chunk<float>::pack(sum + q);
+    } else {
+      embed_write<T>(a, cur, c, sum);
+    }
+  };
+  for (int64_t i = lo; i < hi; i += U) {
+    int key[U];
+    u32x4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t at = min(i + u, hi - 1);
+      key[u] = a.keys[at];
+      // padding rows are not read; past the chunk's end the last one again, not added
+      v[u] = in && key[u] < a.V ? *reinterpret_cast<const u32x4*>(dy + static_cast<int64_t>(a.order[at]) * a.d)
+                                : u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (i + u >= hi) continue;
+      if (key[u] != cur) {
+        flush(false);
+        cur = key[u];
+        head = false;
+#pragma unroll
+        for (int q = 0; q < PE; ++q) sum[q] = 0.f;
+      }
+      float f[PE];
+      Chunk<T>::unpack(v[u], f);
+#pragma unroll
+      for (int q = 0; q < PE; ++q) sum[q] += f[q];
+    }
+  }
+  flush(to_right);
+  // one entry for each run that starts here and crosses into the next chunk
+  if (to_right && !head && cur < a.V && strip == 0 && lane_id() % L == 0) {
+    a.crossers[atomicAdd(a.crossing, 1)] = static_cast<int32_t>(chunk);
+  }
+}
+
+// Clears the rows among kClearRows, from v0 on, that no token names: a wave.
+constexpr int kClearRows = 16;
+template <class T>
+__device__ __forceinline__ void embed_clear(const EmbedArgs& a, int64_t v0) {
+  constexpr int PE = Chunk<T>::kElems;
+  const int lane = lane_id();
+  // lanes 0 .. kClearRows - 1: the first sorted token whose key is not below the row
+  const int64_t v = v0 + min(lane, kClearRows - 1);
+  int64_t lo = 0, hi = a.T;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (a.keys[mid] < v) lo = mid + 1;
+    else hi = mid;
+  }
+  const bool empty = lane < kClearRows && v < a.V && (lo >= a.T || a.keys[lo] != v);
+  uint64_t mask = __ballot(empty);
+  while (mask) {
+    const int r = __builtin_ctzll(mask);
+    mask &= mask - 1;
+    T* p = static_cast<T*>(a.dtable) + (v0 + r) * a.d;
+    for (int c = lane * PE; c < a.d; c += kWave * PE) *reinterpret_cast<u32x4*>(p + c) = u32x4{0, 0, 0, 0};
+  }
+}
+
+template <class T, int L>
+__global__ __launch_bounds__(kBlock) void embed_sums_kernel(EmbedArgs a, int64_t sum_blocks) {
+  const int64_t block = long_block();
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  if (block < sum_blocks) {
+    embed_chunk<T, L>(a, L == kWave ? block * kWavesPerBlock + wave : block * (kBlock / L) + threadIdx.x / L);
+  } else {
+    const int64_t v0 = ((block - sum_blocks) * kWavesPerBlock + wave) * kClearRows;
+    if (v0 < a.V) embed_clear<T>(a, v0);
+  }
+}
+
+// The runs that cross chunks: the parts are added by the block's waves, every kJoinWaves-th
+// each, then over the waves, in an order that the ids alone decide.
+constexpr int kJoinWaves = 4;
+template <class T>
+__global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedArgs a) {
+  constexpr int PE = Chunk<T>::kElems;
+  __shared__ float red[kJoinWaves][kWave * PE + 4];
+  const int lane = lane_id(), wave = threadIdx.x / kWave;
+  const int strips = (a.d + kWave * PE - 1) / (kWave * PE);
+  const int64_t items = static_cast<int64_t>(*a.crossing) * strips;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int64_t chunk = a.crossers[item / strips];
+    const int c = (static_cast<int>(item % strips) * kWave + lane) * PE;
+    const int key = a.keys[(chunk + 1) * a.chunk];  // that of the run, which goes on there
+    // the run's end
+    int64_t lo = (chunk + 1) * a.chunk, hi = a.T;
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) / 2;
+      if (a.keys[mid] <= key) lo = mid + 1;
+      else hi = mid;
+    }
+    const int64_t parts = (lo - 1) / a.chunk - chunk + 1;
+    float sum[PE];
+#pragma unroll
+    for (int q = 0; q < PE; ++q) sum[q] = 0.f;
+    if (c < a.d) {
+      constexpr int U = 4;
+      for (int64_t p = wave; p < parts; p += kJoinWaves * U) {
+        u32x4 v[U][PE / 4];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int64_t at = min(p + u * kJoinWaves, parts - 1);
+          const float* src = embed_part<T>(a, chunk + at, at == 0 ? kTail : kHead, c);
+#pragma unroll
+          for (int q = 0; q < PE / 4; ++q) v[u][q] = reinterpret_cast<const u32x4*>(src)[q];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (p + u * kJoinWaves >= parts) continue;
+#pragma unroll
+          for (int q = 0; q < PE; ++q) sum[q] += __uint_as_float(v[u][q / 4][q % 4]);
+        }
+      }
+    }
+    __syncthreads();  // the sums of the item before are read
+#pragma unroll
+    for (int q = 0; q < PE; ++q) red[wave][lane * PE + q] = sum[q];
+    __syncthreads();
+    if (wave == 0 && c < a.d) {
+#pragma unroll
+      for (int q = 0; q < PE; ++q) {
+        sum[q] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kJoinWaves; ++w) sum[q] += red[w][lane * PE + q];
+      }
+      embed_write<T>(a, key, c, sum);
+    }
+  }
+}
+
+// Passes over the digits of keys up to V.
+int sort_passes(int V) {
+  int bits = 1;
+  while (bits < 31 && (V >> bits) != 0) ++bits;
+  return (bits + 7) / 8;
+}
+
+// Lanes per chunk: those that a row's pieces fill.
+int chunk_lanes(const EmbedArgs& a) {
+  const int pieces = a.d / (a.dtype == 1 ? 8 : 4);
+  return pieces <= 8 ? 8 : pieces <= 16 ? 16 : pieces <= 32 ? 32 : 64;
+}
+
+template <class T, int L>
+hipError_t run_sums(const EmbedArgs& a, hipStream_t st) {
+  const int64_t strips = (a.d + L * Chunk<T>::kElems - 1) / (L * Chunk<T>::kElems);
+  const int64_t units = static_cast<int64_t>(embed_chunks(a)) * strips;
+  const int64_t sums = (units + kBlock / L - 1) / (kBlock / L);
+  const int64_t rows = kWavesPerBlock * kClearRows;
+  const int64_t clears = a.accumulate ? 0 : (a.V + rows - 1) / rows;
+  if (sums + clears == 0) return hipSuccess;
+  embed_sums_kernel<T, L><<<long_grid(sums + clears), kBlock, 0, st>>>(a, sums);
+  return hipGetLastError();
+}
+
+template <class T>
+hipError_t run_bwd(const EmbedArgs& a, hipStream_t st) {
+  hipError_t err = hipSuccess;
+  switch (chunk_lanes(a)) {
+    case 8: err = run_sums<T, 8>(a, st); break;
+    case 16: err = run_sums<T, 16>(a, st); break;
+    case 32: err = run_sums<T, 32>(a, st); break;
+    default: err = run_sums<T, 64>(a, st); break;
+  }
+  if (err != hipSuccess || embed_chunks(a) < 2) return err;
+  const int64_t strips = (a.d + kWave * Chunk<T>::kElems - 1) / (kWave * Chunk<T>::kElems);
+  const int64_t most = std::min<int64_t>(embed_chunks(a) * strips, 2048);
+  embed_join_kernel<T><<<dim3(static_cast<unsigned>(most)), kJoinWaves * kWave, 0, st>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// Sorted tokens per chunk: so that about 16384 waves' worth of chunks and strips run, 8 at least.
+int embed_chunk_length(int T, int d, int dtype) {
+  const int64_t row = static_cast<int64_t>(d) * (dtype == 1 ? 2 : 4);
+  const int64_t want = T * std::max<int64_t>(row, 128) / 1024 / 16384;
+  int n = 8;
+  while (n < 1024 && n < want) n *= 2;
+  return n;
+}
+
+int embed_chunks(const EmbedArgs& a) { return (a.T + a.chunk - 1) / a.chunk; }
+int embed_sort_tiles(int T) { return (T + kSortTile - 1) / kSortTile; }
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
+  return a.dtype == 1 ? run_embed<bf16_t>(a, st) : run_embed<float>(a, st);
+}
+
+// a.keys and a.order: where the sorted tokens are to be; spare_keys and spare_order: as much again.
+hipError_t launch_embed_bwd(const EmbedArgs& a, int32_t* spare_keys, int32_t* spare_order, int32_t* counts,
+                            int32_t* totals, hipStream_t st) {
+  hipError_t err = hipSuccess;
+  if (a.T > 0 && a.T <= kEmbedRankMax) {
+    embed_rank_kernel<<<dim3((a.T + kWave - 1) / kWave), kRankWaves * kWave, 0, st>>>(a);
+    err = hipGetLastError();
+  } else if (a.T > 0) {
+    EmbedSortPass s{};
+    s.ids = a.ids; s.T = a.T; s.V = a.V; s.tiles = embed_sort_tiles(a.T);
+    s.counts = counts; s.totals = totals; s.crossing = a.crossing;
+    const int passes = sort_passes(a.V);
+    for (int p = 0; p < passes && err == hipSuccess; ++p) {
+      const bool to_end = (passes - 1 - p) % 2 == 0;  // the last pass ends in a.keys
+      s.first = p == 0;
+      s.shift = 8 * p;
+      s.keys_in = to_end ? spare_keys : a.keys;
+      s.order_in = to_end ? spare_order : a.order;
+      s.keys_out = to_end ? a.keys : spare_keys;
+      s.order_out = to_end ? a.order : spare_order;
+      sort_count_kernel<<<dim3(s.tiles), kBlock, 0, st>>>(s);
+      sort_scan_kernel<<<dim3(kDigits), kBlock, 0, st>>>(s);
+      sort_place_kernel<<<dim3(s.tiles), kBlock, 0, st>>>(s);
+      err = hipGetLastError();
+    }
+  }
+  if (err != hipSuccess) return err;
+  return a.dtype == 1 ? run_bwd<bf16_t>(a, st) : run_bwd<float>(a, st);
+}
+
+}  // namespace hetumoe

@@ -101,7 +101,8 @@ hipError_t launch_experts(const ExpertArgs& x, hipStream_t st) {
   a.bias = x.b1;
   a.out = x.hidden; a.ldo = x.h; a.sO = static_cast<int64_t>(x.C) * x.h;
   a.pre = x.pre;
-  hipError_t err = x.dtype == 1 ? expert_act_bf16(x, a, st) : expert_act_f32(x, a, st);
+  hipError_t err = x.drops ? (x.dtype == 1 ? expert_act_drop_bf16(x, a, st) : expert_act_drop_f32(x, a, st))
+                           : (x.dtype == 1 ? expert_act_bf16(x, a, st) : expert_act_f32(x, a, st));
   if (err != hipSuccess) return err;
   a = expert_base_args(x);
   a.M = x.C; a.N = x.d; a.K = x.h;
@@ -131,7 +132,8 @@ hipError_t launch_experts_bwd(const ExpertArgs& x, hipStream_t st) {
     a.pre = x.pre;
     a.out = x.dpre; a.ldo = h1; a.sO = rows_h1;
     a.colsum = x.db1 ? x.colsum : nullptr;
-    err = x.dtype == 1 ? expert_actgrad_bf16(x, a, st) : expert_actgrad_f32(x, a, st);
+    err = x.drops ? (x.dtype == 1 ? expert_actgrad_drop_bf16(x, a, st) : expert_actgrad_drop_f32(x, a, st))
+                  : (x.dtype == 1 ? expert_actgrad_bf16(x, a, st) : expert_actgrad_f32(x, a, st));
     if (err != hipSuccess) return err;
   }
   if (rows && x.dxe) {

@@ -13,6 +13,7 @@
 
 #include "common.hpp"
 #include "kernels.hpp"
+#include "philox.hpp"
 
 namespace hetumoe {
 
@@ -29,6 +30,17 @@ constexpr int kExpertOob = 0x7ffffff0;  // offset past every buffer resource: lo
 constexpr int kEpiStore = 0;    // + bias, rounded once
 constexpr int kEpiAct = 1;      // + bias: pre (optional); hidden
 constexpr int kEpiActGrad = 2;  // dhidden: times the activation's gradient -> dpre; column sums of it
+constexpr int kEpiActDrop = 3, kEpiActGradDrop = 4;  // kEpiAct and kEpiActGrad with dropout of hidden
+// Products of 8-bit integers (bf16 units of two), times row and column scales, + bias: rounded
+// once to bf16 or stored in fp32; with the activation (never `pre`).
+constexpr int kEpiInt8 = 5, kEpiInt8Act = 6, kEpiInt8F32 = 7, kEpiInt8ActF32 = 8;
+constexpr bool expert_int8(int epi) { return epi >= kEpiInt8; }
+constexpr bool expert_int8_f32(int epi) { return epi >= kEpiInt8F32; }
+constexpr bool expert_acts(int epi) {
+  return epi == kEpiAct || epi == kEpiActDrop || epi == kEpiInt8Act || epi == kEpiInt8ActF32;
+}
+constexpr bool expert_act_grads(int epi) { return epi == kEpiActGrad || epi == kEpiActGradDrop; }
+constexpr bool expert_drops(int epi) { return epi == kEpiActDrop || epi == kEpiActGradDrop; }
 
 // gfx950's LDS transpose read (ds_read_b64_tr_b16): within each group of 16
 // lanes, lane i receives element i % 4 of the four-element pieces addressed by
@@ -150,6 +162,59 @@ struct ExpertOperand {
     if constexpr (KIND == kRows) s.o = kc < left ? s.o : static_cast<unsigned>(kExpertOob);
     base += KIND == kRows ? kExpertRow : kBk * pitch;
     if constexpr (KIND == kRows) rows -= kExpertRow;
+    return s;
+  }
+  __device__ __forceinline__ void load(T* lds, int wave, int left) {
+    const Stage s = next(left);
+#pragma unroll
+    for (int i = 0; i < N; ++i) s.issue(lds, wave, i);
+  }
+};
+
+// The right operand of a gated forward product whose weights' rows run along K: of each 64 rows
+// of the tile 32 are the gate's, 32 the other factor's, `apart` rows behind them.
+template <class T, int W, int WAVES>
+struct ExpertSplitOperand {
+  static constexpr int kElt = static_cast<int>(sizeof(T));
+  static constexpr int N = W * kExpertRow / 1024 / WAVES, P = kExpertRow / 16, R = 64 / P;
+  static_assert(N * WAVES * 1024 == W * kExpertRow && R * WAVES >= 16, "whole loads, one order of the pieces");
+  const char *gate, *other;
+  int rows, pitch, kc;
+  unsigned off;  // of the lane's first piece in 32 rows
+
+  __device__ __forceinline__ void init(const T* p, int ld, int first, int valid, int apart, int wave) {
+    const int lane = expert_opaque(lane_id());
+    pitch = ld * kElt;
+    gate = reinterpret_cast<const char*>(p + static_cast<int64_t>(first) * ld);
+    other = gate + static_cast<int64_t>(apart) * pitch;
+    rows = max(0, valid) * pitch;
+    const int piece = (lane % P) ^ expert_swz<T, kRows, true, W>(wave * R + lane / P);
+    kc = piece * kExpertPe<T>;
+    off = static_cast<unsigned>(lane / P * pitch + piece * 16);
+  }
+  struct Stage {
+    __amdgpu_buffer_rsrc_t g, u;
+    unsigned o;
+    int pitch;
+    __device__ __forceinline__ void issue(T* lds, int wave, int i) const {
+      const int row = (i * WAVES + wave) * R;  // of the tile, the same for all lanes
+      const unsigned at = o + static_cast<unsigned>((row / 64 * 32 + row % 32) * pitch);
+      char* dst = reinterpret_cast<char*>(lds) + (i * WAVES + wave) * 1024;
+      if (row / 32 % 2 == 0) expert_dma(g, dst, static_cast<int>(at));
+      else expert_dma(u, dst, static_cast<int>(at));
+    }
+  };
+  __device__ __forceinline__ Stage next(int left) {
+    Stage s;
+    const int bytes = __builtin_amdgcn_readfirstlane(max(rows, 0));
+    s.g = expert_rsrc(gate, bytes);
+    s.u = expert_rsrc(other, bytes);
+    s.o = expert_opaque(off);
+    s.o = kc < left ? s.o : static_cast<unsigned>(kExpertOob);
+    s.pitch = pitch;
+    gate += kExpertRow;
+    other += kExpertRow;
+    rows -= kExpertRow;
     return s;
   }
   __device__ __forceinline__ void load(T* lds, int wave, int left) {

@@ -37,6 +37,8 @@
 // busy 32 % at 2.3 GHz).
 #pragma once
 
+#include <type_traits>
+
 #include "experts.hpp"
 
 namespace hetumoe {
@@ -76,9 +78,10 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   constexpr int WAVES = WM * WN;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16, NP = NT / 2;
   static_assert(NT == 4, "64 columns per wave");
+  constexpr bool kInt8 = expert_int8(EPI);
   // columns of the output per block and wave: with GATED in the forward product half of
   // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
-  constexpr bool kSplit = EPI == kEpiAct && GATED;
+  constexpr bool kSplit = expert_acts(EPI) && GATED;
   constexpr int BNO = kSplit ? BN / 2 : BN;
   constexpr bool kDeep = BM * BN <= 64 * 128 || WM == 4;        // four stages: few blocks
   constexpr bool kRing = !kDeep && KA == kCols && KB == kCols;  // four stages of half the length
@@ -105,7 +108,8 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   list_tiles();
 
   ExpertOperand<bf16_t, KA, false, BM, WAVES, BK> oa;
-  ExpertOperand<bf16_t, KB, true, BN, WAVES, BK> ob;
+  constexpr bool kSplitRows = kSplit && KB == kRows;
+  std::conditional_t<kSplitRows, ExpertSplitOperand<bf16_t, BN, WAVES>, ExpertOperand<bf16_t, KB, true, BN, WAVES, BK>> ob;
   int left = 0;  // K elements of the loads' tile from the next stage on
   // Points the loads at tile t (none: zeros).
   auto aim = [&](bool any, const ExpertTile& t) {
@@ -115,7 +119,9 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     const int K = a.k_is_rows ? n : any && m0 < n ? a.K : 0;
     oa.init(reinterpret_cast<const bf16_t*>(a.A) + t.e * a.sA, a.lda, m0, a.k_is_rows ? BM : min(BM, n - m0), wave,
             [&](int piece) { return m0 + piece * 8 < a.M ? m0 + piece * 8 : -1; });
-    ob.init(reinterpret_cast<const bf16_t*>(a.B) + t.e * a.sB, a.ldb, n0, min(BN, a.N - n0), wave, [&](int piece) {
+    if constexpr (kSplitRows)
+      ob.init(reinterpret_cast<const bf16_t*>(a.B) + t.e * a.sB, a.ldb, n0, min(BNO, a.N - n0), a.N, wave);
+    else ob.init(reinterpret_cast<const bf16_t*>(a.B) + t.e * a.sB, a.ldb, n0, min(BN, a.N - n0), wave, [&](int piece) {
       if constexpr (kSplit) {
         // pieces 0..3 of each wave's 8 are the gate's
         const int c = n0 + (piece / 8) * 32 + (piece % 4) * 8;
@@ -130,11 +136,14 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   ExpertFrag<KB, true, BN, NT> rb;
   ra.init(wm * MT * 16, g, m);
   rb.init(wn * NT * 16, g, m);
-  constexpr int kLoads = ExpertOperand<bf16_t, KA, false, BM, WAVES, BK>::N + ExpertOperand<bf16_t, KB, true, BN, WAVES, BK>::N;
+  constexpr int kLoads = decltype(oa)::N + decltype(ob)::N;
   // Stores that every tile's epilogue ends with at least, all issued whatever is masked.
-  constexpr int kStores = EPI == kEpiStore ? MT * NP : EPI == kEpiAct ? MT * (kSplit ? 1 : NP) : MT * NP * (GATED ? 2 : 1);
+  constexpr int kStores = EPI == kEpiStore ? MT * NP
+                          : kInt8          ? MT * (kSplit ? 1 : NP) * (expert_int8_f32(EPI) ? 2 : 1)
+                          : expert_acts(EPI) ? MT * (kSplit ? 1 : NP)
+                                             : MT * NP * (GATED ? 2 : 1);
   // and with pre written too
-  constexpr int kStoresPre = EPI == kEpiAct ? kStores + MT * NP : kStores;
+  constexpr int kStoresPre = expert_acts(EPI) && !kInt8 ? kStores + MT * NP : kStores;
   f32x4 acc[MT][NT];
   u32x4 fa[MT], fb[NT], fn[NT];
   auto load = [&](bf16_t* As, bf16_t* Bs) __attribute__((always_inline)) {
@@ -171,8 +180,13 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
 #pragma unroll
-      for (int j = 0; j < NT; ++j)
-        asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc[i][j]) : "v"(cur[j]), "v"(fa[i]));
+      for (int j = 0; j < NT; ++j) {
+        // sums of integers are held in the same registers, as their bits
+        if constexpr (kInt8)
+          asm volatile("s_nop 1\n\tv_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+v"(acc[i][j]) : "v"(cur[j]), "v"(fa[i]));
+        else
+          asm volatile("s_nop 1\n\tv_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+v"(acc[i][j]) : "v"(cur[j]), "v"(fa[i]));
+      }
       if constexpr (SYNC) {
         if (i == kFirst) {
           barrier(sync);
@@ -307,7 +321,69 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     __builtin_amdgcn_raw_buffer_store_b128(Chunk<bf16_t>::pack(v), r, static_cast<int>(off), 0, 0);
   };
   const int valid = min(BM, a.M - m0);  // rows of the output
-  if constexpr (EPI == kEpiStore) {
+  uint64_t call = 0;
+  if constexpr (expert_drops(EPI)) call = drop_call(a.drop);
+  // dropout's words of 8 columns from c on of row lrow + 16 i of hidden
+  auto words = [&](int i, int c) {
+    return philox<expert_act_grads(EPI) && GATED ? 1 : 10>(
+        a.drop, call, static_cast<uint64_t>((static_cast<int64_t>(e) * a.C + m0 + lrow + 16 * i) * a.N + c) >> 3);
+  };
+  if constexpr (kInt8) {
+    using Out = std::conditional_t<expert_int8_f32(EPI), float, bf16_t>;
+    constexpr int kElt = static_cast<int>(sizeof(Out));
+    constexpr bool kAct = expert_acts(EPI);
+    const int N1 = kSplit ? 2 * a.N : a.N;
+    const __amdgpu_buffer_rsrc_t out =
+        expert_rows<Out>(reinterpret_cast<const Out*>(a.out) + e * a.sO, m0, a.ldo, valid);
+    // scales of the rows in use; the others' are not written
+    const float* sa = a.sa + static_cast<int64_t>(e) * a.C + m0 + lrow;
+    float sr[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) sr[i] = m0 + lrow + 16 * i < rows ? sa[16 * i] : 0.f;
+#pragma unroll
+    for (int p = 0; p < (kSplit ? 1 : NP); ++p) {
+      const int c = col0 + 32 * p;
+      const int64_t at = static_cast<int64_t>(e) * N1 + c;
+      // of the 8 columns, and of the other factor's 8
+      float sc[kSplit ? 2 : 1][8], bias[kSplit ? 2 : 1][8];
+#pragma unroll
+      for (int s = 0; s < (kSplit ? 2 : 1); ++s)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          sc[s][q] = c < a.N ? a.sb[at + s * a.N + q] : 0.f;
+          bias[s][q] = a.bias && c < a.N ? a.bias[at + s * a.N + q] : 0.f;
+        }
+      auto finish = [&](auto which) {
+        constexpr int ACT = decltype(which)::v;
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          const bool used = m0 + lrow + 16 * i < rows;
+          // an exact sum, rounded once to 24 bits
+          auto scaled = [&](int pair, int s, int q) {
+            const float v = static_cast<float>(__float_as_int(value(i, pair, q))) * sr[i] * sc[s][q] + bias[s][q];
+            return used ? v : 0.f;
+          };
+          float f[8];
+#pragma unroll
+          for (int q = 0; q < 8; ++q) {
+            f[q] = scaled(p, 0, q);
+            if constexpr (kAct) f[q] = expert_act<ACT>(f[q]);
+            if constexpr (kSplit) f[q] *= scaled(1, 1, q);
+          }
+          const unsigned off = static_cast<unsigned>(c < a.N ? (lrow * a.ldo + c) * kElt : kExpertOob) + i * 16 * kElt * a.ldo;
+          if constexpr (kElt == 2) {
+            put(out, off, f);
+          } else {
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+              __builtin_amdgcn_raw_buffer_store_b128(Chunk<float>::pack(f + 4 * s), out, static_cast<int>(off + 16 * s), 0, 0);
+          }
+        }
+      };
+      if constexpr (kAct) expert_by_act(a.act, finish);
+      else finish(ExpertInt<0>());
+    }
+  } else if constexpr (EPI == kEpiStore) {
     const __amdgpu_buffer_rsrc_t out =
         expert_rows<bf16_t>(reinterpret_cast<const bf16_t*>(a.out) + e * a.sO, m0, a.ldo, valid);
     float bias[NP][8];
@@ -327,7 +403,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
         put(out, place(a.ldo, col0 + 32 * p, col0 + 32 * p < a.N) + i * 32 * a.ldo, v);
       }
     }
-  } else if constexpr (EPI == kEpiAct) {
+  } else if constexpr (expert_acts(EPI)) {
     const int N1 = GATED ? 2 * a.N : a.N;
     constexpr int NPO = kSplit ? 1 : NP;
     const __amdgpu_buffer_rsrc_t hid =
@@ -359,6 +435,11 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
               u[q] = used ? value(i, 1, q) + bias[1][q] : 0.f;
               f[q] *= u[q];
             }
+          }
+          if constexpr (expert_drops(EPI)) {
+            const u32x4 w = words(i, c);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) f[q] = dropped(a.drop, w, q, f[q]);
           }
           if (a.pre) {
             const unsigned at_pre = place(N1, c, c < a.N) + i * 32 * N1;
@@ -402,6 +483,8 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
           float v[8], u[8];
           Chunk<bf16_t>::unpack(pv[i], v);
           if constexpr (GATED) Chunk<bf16_t>::unpack(pu[i], u);
+          u32x4 w;
+          if constexpr (expert_drops(EPI)) w = words(i0 + i, c);
           // chosen per row: branches around all rows would hold all their loads at once
           expert_by_act(a.act, [&](auto which) {
             constexpr int ACT = decltype(which)::v;
@@ -409,7 +492,15 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
             for (int q = 0; q < 8; ++q) {
               float f, df;
               expert_act_grad<ACT>(v[q], f, df);
-              const float dh = used ? value(i0 + i, p, q) : 0.f;
+              float dh = used ? value(i0 + i, p, q) : 0.f;
+              if constexpr (expert_drops(EPI)) {
+                // a dropped element has no gradient, whatever pre holds
+                const bool kept = drop_keeps(a.drop, w, q);
+                dh = kept ? dh * a.drop.scale : 0.f;
+                df = kept ? df : 0.f;
+                f = kept ? f : 0.f;
+                if constexpr (GATED) u[q] = kept ? u[q] : 0.f;
+              }
               v[q] = GATED ? dh * u[q] * df : dh * df;
               if constexpr (GATED) u[q] = dh * f;
             }

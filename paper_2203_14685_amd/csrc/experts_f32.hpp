@@ -72,7 +72,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64, BM == 128 ? 2 : 4) void experts_ge
   constexpr int WAVES = WM * WN;
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16;
   static_assert(NT == 4 || NT == 2, "64 or 32 columns per wave");
-  constexpr bool kSplit = EPI == kEpiAct && GATED;  // half of a wave's columns are the gate's
+  constexpr bool kSplit = expert_acts(EPI) && GATED;  // half of a wave's columns are the gate's
   constexpr int BNO = kSplit ? BN / 2 : BN;
   __shared__ __align__(1024) float A0[KG * BM * kFBK], B0[KG * BN * kFBK], A1[KG * BM * kFBK], B1[KG * BN * kFBK];
   __shared__ int tile_before[kMaxExperts], tile_rows[kMaxExperts];
@@ -212,6 +212,14 @@ __global__ __launch_bounds__(WM* WN* KG * 64, BM == 128 ? 2 : 4) void experts_ge
   const int row0 = m0 + wm * MT * 16 + m;
   const int col0 = n0 + (kSplit ? 8 * NT : 16 * NT) * wn + 4 * g;
   auto value = [&](int i, int r, int q) { return sum[i][(4 * r + q) % NT][(4 * r + q) / NT]; };
+  uint64_t call = 0;
+  if constexpr (expert_drops(EPI)) call = drop_call(a.drop);
+  // dropout's words of columns c .. c + 3 of a row of hidden: one half of a block's
+  auto words = [&](int row, int c) {
+    const uint64_t i = static_cast<uint64_t>((static_cast<int64_t>(e) * a.C + row) * a.N + c);
+    const u32x4 w = philox(a.drop, call, i >> 3);
+    return i & 4 ? u32x4{w[2], w[3], 0u, 0u} : w;
+  };
   auto put = [](float* p, const float (&v)[4]) { *reinterpret_cast<f32x4*>(p) = f32x4{v[0], v[1], v[2], v[3]}; };
   if constexpr (EPI == kEpiStore) {
 #pragma unroll
@@ -231,7 +239,7 @@ __global__ __launch_bounds__(WM* WN* KG * 64, BM == 128 ? 2 : 4) void experts_ge
         put(reinterpret_cast<float*>(a.out) + e * a.sO + static_cast<int64_t>(row) * a.ldo + c, v);
       }
     }
-  } else if constexpr (EPI == kEpiAct) {
+  } else if constexpr (expert_acts(EPI)) {
     const int N1 = GATED ? 2 * a.N : a.N;
     constexpr int R = kSplit ? NT / 2 : NT;
     expert_by_act(a.act, [&](auto which) {
@@ -259,6 +267,11 @@ __global__ __launch_bounds__(WM* WN* KG * 64, BM == 128 ? 2 : 4) void experts_ge
               u[q] = row < rows ? value(i, r + NT / 2, q) + b1[q] : 0.f;
               f[q] *= u[q];
             }
+          }
+          if constexpr (expert_drops(EPI)) {
+            const u32x4 w = words(row, c);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) f[q] = dropped(a.drop, w, q, f[q]);
           }
           if (a.pre) {
             float* pre = reinterpret_cast<float*>(a.pre) + (static_cast<int64_t>(e) * a.C + row) * N1 + c;
@@ -288,11 +301,21 @@ __global__ __launch_bounds__(WM* WN* KG * 64, BM == 128 ? 2 : 4) void experts_ge
             const float* src = reinterpret_cast<const float*>(a.pre) + at;
             Chunk<float>::unpack(*reinterpret_cast<const u32x4*>(src), v);
             if constexpr (GATED) Chunk<float>::unpack(*reinterpret_cast<const u32x4*>(src + a.N), u);
+            u32x4 w;
+            if constexpr (expert_drops(EPI)) w = words(row, c);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
               float f, df;
               expert_act_grad<ACT>(v[q], f, df);
-              const float dh = value(i, r, q);
+              float dh = value(i, r, q);
+              if constexpr (expert_drops(EPI)) {
+                // a dropped element has no gradient, whatever pre holds
+                const bool kept = drop_keeps(a.drop, w, q);
+                dh = kept ? dh * a.drop.scale : 0.f;
+                df = kept ? df : 0.f;
+                f = kept ? f : 0.f;
+                u[q] = kept ? u[q] : 0.f;
+              }
               v[q] = GATED ? dh * u[q] * df : dh * df;
               u[q] = dh * f;
               s0[q] += v[q];

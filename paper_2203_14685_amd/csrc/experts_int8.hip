@@ -1,0 +1,57 @@
+// The expert networks in 8-bit integers: rows and hidden rows are quantized by launches of their own
+// (a row's scale is known when all of it is), the products are the bf16 ones' loop on
+// v_mfma_i32_16x16x64_i8.  A fragment's 16 bytes are 16 integers for 8 bf16, in the same places along K
+// in both operands, so tiles, LDS and loads are those of bf16 rows half as long; both
+// operands' rows run along K.
+#include "experts_tiles_bf16.hpp"
+
+namespace hetumoe {
+
+namespace {
+
+template <int EPI>
+hipError_t product(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st) {
+  constexpr bool kAct = expert_acts(EPI);
+  return by_tile(x, a.M, kAct && x.gated ? 2 * a.N : a.N, [&](auto tile) {
+    using TL = decltype(tile);
+    if constexpr (kAct) {
+      if (x.gated) return launch_tile_bf16<TL, kRows, kRows, EPI, true>(x, a, st);
+    }
+    return launch_tile_bf16<TL, kRows, kRows, EPI, false>(x, a, st);
+  });
+}
+
+}  // namespace
+
+hipError_t launch_experts_int8(const ExpertInt8Args& x, hipStream_t st) {
+  ExpertArgs shape{};
+  shape.E = x.E; shape.C = x.C; shape.d = x.d; shape.h = x.h; shape.act = x.act; shape.gated = x.gated;
+  shape.dtype = x.dtype; shape.counts = x.counts;
+  const int h1 = x.gated ? 2 * x.h : x.h;
+  const int64_t rows = static_cast<int64_t>(x.E) * x.C;
+  QuantArgs q{};
+  q.rows = rows; q.n = x.d; q.C = x.C; q.dtype = x.dtype; q.counts = x.counts;
+  q.x = x.xe; q.q = x.q; q.scale = x.scale;
+  hipError_t err = launch_quantize(q, st);
+  if (err != hipSuccess) return err;
+  // K, and elements from one row to the next, in units of two integers
+  ExpertGemmArgs a = expert_base_args(shape);
+  a.M = x.C; a.N = x.h; a.K = x.d / 2;
+  a.A = x.q; a.lda = x.d / 2; a.sA = static_cast<int64_t>(x.C) * (x.d / 2);
+  a.B = x.q1; a.ldb = x.d / 2; a.sB = static_cast<int64_t>(h1) * (x.d / 2);
+  a.sa = x.scale; a.sb = x.s1; a.bias = x.b1;
+  a.out = x.hidden; a.ldo = x.h; a.sO = static_cast<int64_t>(x.C) * x.h;
+  err = x.dtype == 1 ? product<kEpiInt8Act>(shape, a, st) : product<kEpiInt8ActF32>(shape, a, st);
+  if (err != hipSuccess) return err;
+  q.n = x.h; q.x = x.hidden;
+  if ((err = launch_quantize(q, st)) != hipSuccess) return err;
+  a = expert_base_args(shape);
+  a.M = x.C; a.N = x.d; a.K = x.h / 2;
+  a.A = x.q; a.lda = x.h / 2; a.sA = static_cast<int64_t>(x.C) * (x.h / 2);
+  a.B = x.q2; a.ldb = x.h / 2; a.sB = static_cast<int64_t>(x.d) * (x.h / 2);
+  a.sa = x.scale; a.sb = x.s2; a.bias = x.b2;
+  a.out = x.ye; a.ldo = x.d; a.sO = static_cast<int64_t>(x.C) * x.d;
+  return x.dtype == 1 ? product<kEpiInt8>(shape, a, st) : product<kEpiInt8F32>(shape, a, st);
+}
+
+}  // namespace hetumoe

@@ -12,6 +12,7 @@ inline ExpertGemmArgs expert_base_args(const ExpertArgs& x) {
   a.C = x.C;
   a.counts = x.counts;
   a.act = x.act;
+  a.drop = x.drop;
   return a;
 }
 
@@ -26,6 +27,11 @@ hipError_t expert_act_bf16(const ExpertArgs& x, const ExpertGemmArgs& a, hipStre
 hipError_t expert_act_f32(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st);
 hipError_t expert_actgrad_bf16(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st);
 hipError_t expert_actgrad_f32(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st);
+// with dropout of hidden
+hipError_t expert_act_drop_bf16(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st);
+hipError_t expert_act_drop_f32(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st);
+hipError_t expert_actgrad_drop_bf16(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st);
+hipError_t expert_actgrad_drop_f32(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st);
 // epilogue kEpiStore: kinds of the operands as (ka, kb) = (rows, cols), (rows, rows), (cols, cols)
 hipError_t expert_store_bf16(const ExpertArgs& x, const ExpertGemmArgs& a, int ka, int kb, hipStream_t st);
 hipError_t expert_store_f32(const ExpertArgs& x, const ExpertGemmArgs& a, int ka, int kb, hipStream_t st);

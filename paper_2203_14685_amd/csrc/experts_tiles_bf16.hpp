@@ -37,9 +37,9 @@ static hipError_t by_tile(const ExpertArgs& x, int M, int N, Fn fn) {
 
 template <class TL, int KA, int KB, int EPI, bool GATED>
 static hipError_t launch_tile_bf16(const ExpertArgs& x, ExpertGemmArgs a, hipStream_t st) {
-  expert_set_tiles(a, x.E, TL::bm, EPI == kEpiAct && GATED ? TL::bn / 2 : TL::bn);
+  expert_set_tiles(a, x.E, TL::bm, expert_acts(EPI) && GATED ? TL::bn / 2 : TL::bn);
   const int resident = TL::per_cu * device_cu_count();
-  constexpr bool kQuarters = TL::bm == 256 && EPI != kEpiActGrad;  // that one's column sums go by tile
+  constexpr bool kQuarters = TL::bm == 256 && !expert_act_grads(EPI);  // that one's column sums go by tile
   if (kQuarters && a.tiles <= kMaxRounds * resident) {
     // without counts that cut M the tiles are known here
     const int last = a.tiles % resident;

@@ -42,7 +42,7 @@ static hipError_t by_tile(const ExpertArgs& x, int M, int N, int K, Fn fn) {
 
 template <class TL, int KA, int KB, int EPI, bool GATED>
 static hipError_t launch_tile_f32(const ExpertArgs& x, ExpertGemmArgs a, hipStream_t st) {
-  expert_set_tiles(a, x.E, TL::bm, EPI == kEpiAct && GATED ? TL::bn / 2 : TL::bn);
+  expert_set_tiles(a, x.E, TL::bm, expert_acts(EPI) && GATED ? TL::bn / 2 : TL::bn);
   experts_gemm_f32_kernel<TL::bm, TL::bn, TL::wm, TL::wn, TL::kg, KA, KB, EPI, GATED>
       <<<dim3(expert_blocks(a.tiles, TL::per_cu * device_cu_count())), dim3(TL::wm * TL::wn * TL::kg * kWave), 0, st>>>(a);
   return hipGetLastError();

@@ -233,6 +233,15 @@ hipError_t run_base_auction(const BaseArgs& a, hipStream_t st, BaseStats* stats)
 // auction did not finish (its current one, else s mod E).
 hipError_t run_base_auction_async(const BaseArgs& a, int launch_rounds, BaseDevStatus* status, hipStream_t st);
 
+// Which elements dropout drops (philox.hpp).
+struct DropArgs {
+  uint32_t k0, k1;          // the seed
+  uint32_t t;               // kept: words >= t of 2^16
+  float scale;              // of kept elements
+  uint64_t call;
+  const uint64_t* step;     // device memory, added to call, or null
+};
+
 // Expert networks (step 4 of Algorithm 1): one batched product (experts.hpp).
 struct ExpertGemmArgs {
   int E, C;                 // experts, slots of each
@@ -251,6 +260,8 @@ struct ExpertGemmArgs {
   void* pre;                // kEpiAct: output or null; kEpiActGrad: input
   float* colsum;            // kEpiActGrad: [E, parts, N1] or null
   int act;
+  DropArgs drop;            // of the elements of hidden (kEpiActDrop, kEpiActGradDrop)
+  const float *sa, *sb;     // scales of 8-bit integers: rows [E, C], columns as bias
 };
 
 struct ExpertArgs {
@@ -265,12 +276,41 @@ struct ExpertArgs {
   float *db1, *db2;
   float* colsum;            // workspace [E, expert_parts, h1]
   float* rowsum;            // workspace [E, expert_row_parts, d]
+  int drops;                // dropout of hidden
+  DropArgs drop;
 };
 hipError_t launch_experts(const ExpertArgs& a, hipStream_t st);
 hipError_t launch_experts_bwd(const ExpertArgs& a, hipStream_t st);
 // Row ranges per expert whose sums of dpre, and of dye, go to the workspace.
 int expert_parts(const ExpertArgs& a);
 int expert_row_parts(const ExpertArgs& a);
+
+// 8-bit integers (int8.hip): rows (of experts: the first counts[e] of each C; counts null: all), and
+// weights [E, K, N] as [E, N, K].
+struct QuantArgs {
+  int64_t rows;
+  int n, C, dtype;
+  const int32_t* counts;
+  const void* x;
+  int8_t* q;
+  float* scale;
+};
+hipError_t launch_quantize(const QuantArgs& a, hipStream_t st);
+hipError_t launch_quantize_weights(int E, int K, int N, int dtype, const void* w, int8_t* q, float* scale, hipStream_t st);
+
+// The expert networks in 8-bit integers (experts_int8.hip).
+struct ExpertInt8Args {
+  int E, C, d, h, act, gated, dtype;
+  const int32_t* counts;
+  const void* xe;
+  const int8_t *q1, *q2;
+  const float *s1, *s2, *b1, *b2;
+  void* ye;
+  int8_t* q;                // workspace [E, C, max(d, h)]
+  float* scale;             // workspace [E, C]
+  void* hidden;             // workspace [E, C, h]
+};
+hipError_t launch_experts_int8(const ExpertInt8Args& a, hipStream_t st);
 
 // The layer for a few tokens (layer.hip), behind its gate.
 constexpr int kLayerMaxTokens = 256;
@@ -305,6 +345,60 @@ bool layer_gate_fits(const LayerGateArgs& a);
 hipError_t launch_layer_gate(const LayerGateArgs& a, hipStream_t st);
 int layer_splits(const LayerArgs& a);
 hipError_t launch_layer(const LayerArgs& a, hipStream_t st);
+
+// The same with weights and rows in 8-bit integers (layer_int8.hip); of `a`, part holds integers and
+// w1, w2 are [E, h1, d] and [E, d, h].
+struct LayerInt8Args {
+  LayerArgs a;
+  const float *s1, *s2;
+  int8_t *qx, *qh;          // workspace [S, d], [S * k, h]
+  float *sx, *sh;           // workspace [S], [S * k]
+};
+int layer_int8_splits(const LayerArgs& a);
+hipError_t launch_layer_int8(const LayerInt8Args& a, hipStream_t st);
+
+// Blocks of a long launch: a grid's dimension holds 2^32 threads, so they go along two; the last
+// row may be partly filled (blocks past the end do nothing).
+constexpr int64_t kGridRow = 1 << 20;
+inline dim3 long_grid(int64_t blocks) {
+  return blocks <= kGridRow ? dim3(static_cast<unsigned>(blocks))
+                            : dim3(static_cast<unsigned>(kGridRow), static_cast<unsigned>((blocks + kGridRow - 1) / kGridRow));
+}
+__device__ __forceinline__ int64_t long_block() {
+  return static_cast<int64_t>(blockIdx.y) * gridDim.x + blockIdx.x;
+}
+
+// Dropout (dropout.hip): y = [res] + drop(x).
+hipError_t launch_dropout(const DropArgs& m, int64_t n, int dtype, const void* x, const void* res, void* y,
+                          hipStream_t st);
+
+// Embedding rows and their table's gradient (embed.hip).
+constexpr int kEmbedRankMax = 8192;   // most tokens that are sorted by counting comparisons
+constexpr int kEmbedDigits = 256;     // of a sorting pass
+struct EmbedArgs {
+  int T, V, d, dtype, accumulate;
+  int chunk;                // sorted tokens whose runs are summed together
+  float scale;
+  const int32_t* ids;
+  const void *table, *dy;
+  void *y, *dtable;
+  int32_t *keys, *order;    // workspace [T]: sorted ids (V: padding) and their tokens
+  float* part;              // workspace [chunks, 2, d]
+  int32_t *crossers, *crossing;  // workspace [chunks], [1]: chunks where a run that crosses chunks begins
+};
+struct EmbedSortPass {
+  int T, V, tiles, shift, first;
+  const int32_t *ids, *keys_in, *order_in;
+  int32_t *keys_out, *order_out;
+  int32_t *counts, *totals; // [digits, tiles], [digits]
+  int32_t* crossing;
+};
+int embed_chunk_length(int T, int d, int dtype);
+int embed_chunks(const EmbedArgs& a);
+int embed_sort_tiles(int T);
+hipError_t launch_embed(const EmbedArgs& a, hipStream_t st);
+hipError_t launch_embed_bwd(const EmbedArgs& a, int32_t* spare_keys, int32_t* spare_order, int32_t* counts,
+                            int32_t* totals, hipStream_t st);
 
 // Gradients by chunks (grads.hip).  A list holds as many tensors as fit a launch's
 // arguments; longer ones take several launches.

@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "experts.hpp"
+#include "layer_choices.hpp"
 #include "select.hpp"
 
 namespace hetumoe {
@@ -150,50 +151,9 @@ __global__ __launch_bounds__(WAVES* kWave) void layer_strip_kernel(LayerArgs a, 
   const int tid = threadIdx.x, lane = lane_id(), m = lane % 16;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int choices = a.S * a.k;
-  int e = blockIdx.y;
-  int n = 0;
+  int e, n;
   const int* list;  // the choices of e, in order
-  if (choices <= kWave) {
-    // each wave for itself, without a barrier
-    const int mine = lane < choices ? a.ids[lane] : -1;
-    if (a.by_choice) {
-      e = __builtin_amdgcn_readlane(mine, blockIdx.y);
-      if (e < 0 || e >= a.E) return;
-    }
-    const uint64_t mask = __ballot(mine == e);
-    // the first choice of an expert takes all of its rows
-    if (a.by_choice && (mask & ((uint64_t(1) << blockIdx.y) - 1)) != 0) return;
-    n = __popcll(mask);
-    if (mine == e) lists[wave * kWave + popc_below(mask)] = lane;
-    list = lists + wave * kWave;
-    __builtin_amdgcn_wave_barrier();
-  } else {
-    if (a.by_choice) {
-      const int c = blockIdx.y;
-      e = a.ids[c];
-      if (e < 0 || e >= a.E) return;
-      bool earlier = false;
-      for (int i = lane; i < c; i += kWave) earlier |= a.ids[i] == e;
-      if (__ballot(earlier)) return;
-    }
-    for (int base = 0; base < choices; base += THREADS) {
-      const int c = base + tid;
-      const bool mine = c < choices && a.ids[c] == e;
-      const uint64_t mask = __ballot(mine);
-      if (lane == 0) wave_n[wave] = __popcll(mask);
-      __syncthreads();
-      int at = n;
-#pragma unroll
-      for (int w = 0; w < WAVES; ++w) {
-        const int wn = wave_n[w];
-        at += w < wave ? wn : 0;
-        n += wn;
-      }
-      if (mine) lists[at + popc_below(mask)] = c;
-      __syncthreads();
-    }
-    list = lists;
-  }
+  if (!layer_choices<WAVES>(a, lists, wave_n, e, n, list)) return;
   const int share = blockIdx.z % shares, z = blockIdx.z / shares, zs = gridDim.z / shares;
   if (n <= 16 * MAXT * share) return;
 

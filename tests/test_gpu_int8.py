@@ -1,0 +1,285 @@
+"""8-bit integers against the oracle: the integers themselves exactly, the expert networks and the
+layer for few tokens within bounds that allow a hidden value on a border to fall on either
+side; types, widths, capacities around the tiles, rows that are zero or not finite, graphs,
+streams, and both entry points giving the same values."""
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2203_14685_amd as hm
+from oracle import int8 as oi
+
+from _experts import ACTS, DEV, ROUND, TORCH, announce, check, f64, normal
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True, scope="module")
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    hm.load()
+    yield
+
+
+def _same_quantized(q, s, value):
+    want_q, want_s = oi.quantize(value)
+    assert np.array_equal(q.cpu().numpy().astype(np.float64), want_q)
+    assert np.array_equal(f64(s), want_s, equal_nan=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,n", [(1, 16), (300, 16), (37, 64), (5, 240), (64, 272), (9, 1008), (7, 1040), (33, 2048), (5, 4112),
+                                    (3, 8192), (2, 16400), (1, 40000)])
+def test_rows(rows, n, dtype):
+    announce(f"quantize {dtype} rows={rows} n={n}")
+    rng = np.random.default_rng(n)
+    x, _ = normal(rng, (rows, n), dtype)
+    if rows > 4:
+        x[0] = 0
+        x[1, 3] = float("inf")
+        x[2, n - 1] = float("nan")
+        x[3] = x[3] * 2.0 ** -120  # 127 / a would overflow
+        x[4, ::2] = x[4].abs().max() / 2  # halves of the largest value: borders
+    x[rows - 1] *= 2.0 ** 100
+    q, s = hm.quantize(x.to(DEV))
+    _same_quantized(q, s, x.double().numpy())
+
+
+def test_borders_everywhere():
+    """Rows whose values lie on or next to (2 k + 1) / 254 of the largest one, in fp32."""
+    rng = np.random.default_rng(0)
+    a = np.concatenate([2.0 ** rng.integers(-20, 20, 40), rng.random(40) * 1000]).astype(np.float32)
+    k = np.arange(-127, 127)
+    x = ((2 * k + 1) / 254.0 * a[:, None].astype(np.float64)).astype(np.float32)
+    x = np.concatenate([x, np.nextafter(x, np.float32(np.inf)), np.nextafter(x, np.float32(-np.inf)), a[:, None], a[:, None]], axis=1)
+    x = np.concatenate([x, np.zeros((len(a), -x.shape[1] % 16), dtype=np.float32)], axis=1)
+    x = np.clip(x, -a[:, None], a[:, None])
+    t = torch.from_numpy(x)
+    q, s = hm.quantize(t.to(DEV))
+    _same_quantized(q, s, t.double().numpy())
+
+
+def test_batched_rows_and_none():
+    x = torch.randn(3, 5, 32, device=DEV)
+    q, s = hm.quantize(x)
+    assert q.shape == (3, 5, 32) and s.shape == (3, 5)
+    _same_quantized(q.reshape(15, 32), s.reshape(15), x.reshape(15, 32).double().cpu().numpy())
+    q, s = hm.quantize(torch.empty(0, 32, device=DEV))
+    assert q.shape == (0, 32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("E,K,N", [(1, 16, 16), (3, 16, 80), (2, 80, 16), (5, 64, 64), (2, 272, 144), (3, 528, 1040), (1, 2064, 48)])
+def test_weights(E, K, N, dtype):
+    announce(f"quantize_weights {dtype} E={E} K={K} N={N}")
+    rng = np.random.default_rng(K + N)
+    w, _ = normal(rng, (E, K, N), dtype, K ** -0.5)
+    w[0, :, 0] = 0
+    w[E - 1, K // 2, N - 1] = float("inf")
+    w[E - 1, 0, N // 2] = float("nan")
+    q, s = hm.quantize_weights(w.to(DEV))
+    assert q.shape == (E, N, K)
+    _same_quantized(q, s, np.swapaxes(w.double().numpy(), 1, 2))
+
+
+# ---------------------------------------------------------------- the networks
+
+def _net(rng, E, d, h, gated, bias=True):
+    """Weights as the library's quantization lays them out, and their values for the oracle."""
+    h1 = 2 * h if gated else h
+    out = []
+    for shape, width in (((E, d, h1), d), ((E, h, d), h)):
+        w, wv = normal(rng, shape, "bf16", width ** -0.5)
+        qv, sv = oi.quantize_weights(wv)
+        q = torch.from_numpy(np.ascontiguousarray(qv, dtype=np.int8)).to(DEV)
+        s = torch.from_numpy(np.ascontiguousarray(sv, dtype=np.float32)).to(DEV)
+        b, bv = normal(rng, (E, shape[2]), "f32", 0.3) if bias else (None, None)
+        out += [(q, qv), (s, sv), (b if b is None else b.to(DEV), bv)]
+    return [t for t, _ in out], [v for _, v in out]
+
+
+def _counts(rng, E, C):
+    c = rng.integers(0, C + 1, E)
+    for e, v in zip(range(E), (0, min(1, C), C)):
+        c[e] = v
+    return c.astype(np.int32)
+
+
+SHAPES = [
+    # E, C, d, h: one row; tiles cut short along each side; around 64, 128 and 256 rows; K of
+    # one 16-byte piece, of odd pieces, of a stage and one more
+    (1, 1, 16, 16), (3, 1, 64, 128), (4, 5, 80, 208), (3, 64, 128, 64), (3, 65, 144, 272), (5, 129, 64, 16), (2, 257, 528, 32),
+    (3, 300, 16, 336), (60, 7, 48, 80), (3, 130, 272, 528),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("E,C,d,h", SHAPES)
+def test_experts(E, C, d, h, dtype):
+    for i, (act, gated) in enumerate([("relu", False), ("silu", True), ("gelu", False), ("gelu", True)]):
+        announce(f"experts_int8 {dtype} E={E} C={C} d={d} h={h} {act} gated={gated}")
+        rng = np.random.default_rng(C + i)
+        xe, xv = normal(rng, (E, C, d), dtype)
+        (q1, s1, b1, q2, s2, b2), vals = _net(rng, E, d, h, gated, bias=i != 2)
+        counts = _counts(rng, E, C)
+        for e in range(E):
+            xe[e, counts[e]:] = float("nan")  # not read
+        args = dict(b1=b1, b2=b2, counts=torch.from_numpy(counts).to(DEV), act=ACTS[act], gated=gated)
+        y = hm.experts_int8(xe.to(DEV), q1, s1, q2, s2, **args)
+        check(y, oi.experts(xv, *vals, counts, ACTS[act], gated, ROUND[dtype]), "ye")
+        assert torch.equal(y, hm.experts_int8(xe.to(DEV), q1, s1, q2, s2, **args))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gated", [False, True])
+def test_large_tiles(dtype, gated):
+    """Tiles of 256 x 256 with a last round in quarters, and of 128 x 128; all rows in use."""
+    for E, C, d, h in ((8, 520, 272, 2064), (5, 1300, 1040, 528), (16, 256, 512, 528)):
+        announce(f"experts_int8 large {dtype} E={E} C={C} d={d} h={h} gated={gated}")
+        rng = np.random.default_rng(C)
+        xe, xv = normal(rng, (E, C, d), dtype)
+        (q1, s1, b1, q2, s2, b2), vals = _net(rng, E, d, h, gated)
+        y = hm.experts_int8(xe.to(DEV), q1, s1, q2, s2, b1=b1, b2=b2, act=ACTS["silu"], gated=gated)
+        for e in (0, E - 1):
+            ref = oi.experts(xv[e:e + 1], *[v[e:e + 1] for v in vals], None, ACTS["silu"], gated, ROUND[dtype])
+            check(y[e:e + 1], ref, f"ye of expert {e}")
+
+
+def test_exact_sums():
+    """Sums up to 2^31: all integers 127, K = 2^17; and alternating signs that cancel."""
+    d, h = 1 << 17, 16
+    xe = torch.ones(1, 3, d, device=DEV)
+    xe[0, 1, 1::2] = -1
+    xe[0, 2, 1::2] = -1
+    xe[0, 2, 0] = -1
+    q1 = torch.full((1, h, d), 127, dtype=torch.int8, device=DEV)
+    s1, s2 = torch.full((1, h), 2.0 ** -31, device=DEV), torch.full((1, d), 1.0, device=DEV)
+    q2 = torch.zeros(1, d, h, dtype=torch.int8, device=DEV)
+    q2[0, 0, 0] = 1
+    announce("experts_int8 K=2^17")
+    y = f64(hm.experts_int8(xe, q1, s1, q2, s2))[0, :, 0]
+    # hidden = sum * (1 / 127 in fp32) * 2^-31, quantized to 127 with scale hidden / 127, times 1: hidden again
+    top = 127.0 * 127.0 * 2 ** 17 / 127.0 * 2.0 ** -31
+    assert abs(y[0] - top) <= 8 * 2.0 ** -24 * top
+    assert y[1] == 0 and y[2] == 0  # relu of -2 * 127 * 127
+
+
+def test_values_that_are_not_finite():
+    """A row that holds one gives NaN in its own outputs alone; a weight's column in its own."""
+    rng = np.random.default_rng(1)
+    E, C, d, h = 2, 5, 32, 48
+    (q1, s1, b1, q2, s2, b2), vals = _net(rng, E, d, h, False)
+    xe, xv = normal(rng, (E, C, d), "bf16")
+    xe[0, 2, 5] = float("inf")
+    y = f64(hm.experts_int8(xe.to(DEV), q1, s1, q2, s2, b1=b1, b2=b2, act=ACTS["silu"]))
+    assert np.isnan(y[0, 2]).all() and np.isfinite(np.delete(y[0], 2, 0)).all() and np.isfinite(y[1]).all()
+    s2[1, 7] = float("nan")
+    xe[0, 2, 5] = 0
+    y = f64(hm.experts_int8(xe.to(DEV), q1, s1, q2, s2, b1=b1, b2=b2, act=ACTS["silu"]))
+    assert np.isnan(y[1, :, 7]).all() and np.isfinite(np.delete(y[1], 7, 1)).all() and np.isfinite(y[0]).all()
+
+
+def test_a_row_of_zeros():
+    rng = np.random.default_rng(2)
+    (q1, s1, b1, q2, s2, b2), vals = _net(rng, 1, 32, 48, True)
+    y = hm.experts_int8(torch.zeros(1, 3, 32, dtype=torch.bfloat16, device=DEV), q1, s1, q2, s2, b1=b1, b2=b2, act=ACTS["gelu"],
+                        gated=True)
+    check(y, oi.experts(np.zeros((1, 3, 32)), *vals, None, ACTS["gelu"], True, ROUND["bf16"]), "ye")
+    y = hm.experts_int8(torch.zeros(1, 3, 32, dtype=torch.bfloat16, device=DEV), q1, s1, q2, s2, act=ACTS["relu"], gated=True)
+    assert not y.any()
+
+
+# ---------------------------------------------------------------- the layer for few tokens
+
+LAYERS = [
+    # S, d, E, k, h: one token; fewer choices than experts; more; few experts of many rows; all 256
+    (1, 16, 1, 1, 16), (1, 144, 8, 2, 208), (3, 64, 16, 2, 80), (32, 80, 6, 2, 272), (17, 528, 4, 1, 64), (70, 48, 3, 3, 96),
+    (256, 32, 2, 1, 48), (200, 64, 5, 4, 2064), (9, 1040, 12, 8, 32), (256, 16, 4, 2, 4112),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("S,d,E,k,h", LAYERS)
+def test_token_layer(S, d, E, k, h, dtype):
+    for i, (act, gated) in enumerate([("silu", True), ("relu", False), ("gelu", False)]):
+        announce(f"token_layer_int8 {dtype} S={S} d={d} E={E} k={k} h={h} {act} gated={gated}")
+        rng = np.random.default_rng(S + i)
+        x, xv = normal(rng, (S, d), dtype)
+        wg, _ = normal(rng, (d, E), dtype, d ** -0.5)
+        (q1, s1, b1, q2, s2, b2), vals = _net(rng, E, d, h, gated, bias=i != 1)
+        kw = dict(b1=b1, b2=b2, act=ACTS[act], gated=gated)
+        o = hm.token_layer_int8(x.to(DEV), q1, s1, q2, s2, k=k, wg=wg.to(DEV), normalize=1, **kw)
+        ids, weights = o["ids"].cpu().numpy(), f64(o["weights"])
+        check(o["y"], oi.token_layer(xv, ids, weights, *vals, ACTS[act], gated, ROUND[dtype]), "y")
+        # the gate is that of the layer without integers
+        w1, w2 = torch.zeros(E, d, 2 * h if gated else h, dtype=TORCH[dtype], device=DEV), torch.zeros(E, h, d, dtype=TORCH[dtype], device=DEV)
+        g = hm.token_layer(x.to(DEV), w1, w2, k=k, wg=wg.to(DEV), normalize=1, act=ACTS[act], gated=gated)
+        assert torch.equal(g["ids"], o["ids"]) and torch.equal(g["weights"], o["weights"])
+        # routed: another gate's choices, among them padding
+        ids = rng.integers(-1, E + 1, (S, k)).astype(np.int32)
+        r = hm.token_layer_int8(x.to(DEV), q1, s1, q2, s2, ids=torch.from_numpy(ids).to(DEV), weights=o["weights"], **kw)
+        check(r["y"], oi.token_layer(xv, ids, weights, *vals, ACTS[act], gated, ROUND[dtype]), "y, routed")
+
+
+def test_gates_of_the_layer():
+    rng = np.random.default_rng(5)
+    S, d, E, h = 20, 64, 8, 48
+    x, xv = normal(rng, (S, d), "bf16")
+    wg = normal(rng, (d, E), "bf16", 0.1)[0].to(DEV)
+    bias = normal(rng, (E,), "f32")[0].to(DEV)
+    tok = torch.from_numpy(rng.integers(0, 1000, S).astype(np.int32)).to(DEV)
+    table = torch.from_numpy(rng.integers(0, E, 1000).astype(np.int32)).to(DEV)
+    noise = normal(rng, (S, E), "f32")[0].to(DEV)
+    (q1, s1, b1, q2, s2, b2), vals = _net(rng, E, d, h, False)
+    w1, w2 = torch.zeros(E, d, h, dtype=torch.bfloat16, device=DEV), torch.zeros(E, h, d, dtype=torch.bfloat16, device=DEV)
+    for kw in (dict(kind=hm.MOE_GATE_KTOP1, k=4, wg=wg, bias=bias), dict(kind=hm.MOE_GATE_HTOPK, k=2, groups=2, wg=wg, bias=bias),
+               dict(kind=hm.MOE_GATE_HASH, k=1, token_ids=tok, hash_seed=3),
+               dict(kind=hm.MOE_GATE_HASH, k=1, token_ids=tok, hash_table=table),
+               dict(k=2, wg=wg, noise=noise, temperature=0.7)):
+        announce(f"token_layer_int8 gate {sorted(kw)}")
+        o = hm.token_layer_int8(x.to(DEV), q1, s1, q2, s2, b1=b1, b2=b2, act=ACTS["gelu"], **kw)
+        g = hm.token_layer(x.to(DEV), w1, w2, **kw)
+        assert torch.equal(g["ids"], o["ids"]) and torch.equal(g["weights"], o["weights"])
+        check(o["y"], oi.token_layer(xv, o["ids"].cpu().numpy(), f64(o["weights"]), *vals, ACTS["gelu"], False, ROUND["bf16"]), "y")
+
+
+def test_graphs_and_streams():
+    rng = np.random.default_rng(6)
+    S, d, E, k, h, C = 32, 128, 8, 2, 272, 40
+    (q1, s1, b1, q2, s2, b2), vals = _net(rng, E, d, h, True)
+    x = normal(rng, (S, d), "bf16")[0].to(DEV)
+    wg = normal(rng, (d, E), "bf16", 0.1)[0].to(DEV)
+    xe = normal(rng, (E, C, d), "bf16")[0].to(DEV)
+    kw = dict(b1=b1, b2=b2, act=ACTS["silu"], gated=True)
+
+    def step():
+        return (hm.token_layer_int8(x, q1, s1, q2, s2, k=k, wg=wg, **kw)["y"], hm.experts_int8(xe, q1, s1, q2, s2, **kw))
+
+    want = step()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    keep, keep_e = x.clone(), xe.clone()
+    for i in range(4):
+        x.copy_(keep if i % 2 == 0 else -keep)
+        xe.copy_(keep_e if i % 2 == 0 else keep_e.flip(1))
+        for t in got:
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want if i % 2 == 0 else step()):
+            assert torch.equal(a, b), i
+    x.copy_(keep)
+    torch.cuda.synchronize()
+    s1_, s2_ = torch.cuda.Stream(), torch.cuda.Stream()
+    a = hm.token_layer_int8(x, q1, s1, q2, s2, k=k, wg=wg, stream=s1_, **kw)["y"]
+    b = hm.token_layer_int8(x, q1, s1, q2, s2, k=k, wg=wg, stream=s2_, **kw)["y"]
+    torch.cuda.synchronize()
+    assert torch.equal(a, want[0]) and torch.equal(b, want[0])
