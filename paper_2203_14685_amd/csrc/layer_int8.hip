@@ -1,10 +1,10 @@
 // The layer for a few tokens with weights in 8-bit integers.
 //
 // As layer.hip: the weights' bytes are what there is to read, a block streams a strip of one
-// expert's matrix past all rows that chose it.  The matrix's rows are its columns of the
-// product and run along K, so a lane's 16 bytes are a matrix-core operand as they come from memory:
-// 16 rows of the matrix are one operand, 16 tokens the other.  A block's waves take ranges of K and
-// add their sums, which are exact, in LDS; K of the second product is also split over blocks.
+// expert's matrix past all rows that chose it.  The matrix's rows are the product's columns and run
+// along K, so 16 bytes of one are a lane's part of a matrix-core operand: 16 rows of the
+// matrix are one operand, 16 tokens the other.  A block's waves take ranges of K and add their
+// sums, which are exact, in LDS; K of the second product is also split over blocks.
 // Tokens and hidden rows are quantized by launches of their own: a row's scale needs all of it.
 #include <algorithm>
 
@@ -17,65 +17,101 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kInt8Waves = 8;
+constexpr int kInt8Waves = 4;
 constexpr int kInt8Tiles = 4;                  // of 16 rows of the matrix per block
 constexpr int kInt8Strip = 16 * kInt8Tiles;
-constexpr int kInt8Step = 64;                  // K of one matrix instruction
+constexpr int kInt8Step = 256;                 // K of one stage: bytes of a row that are read together
+constexpr int kInt8Stage = 16 * kInt8Step;     // bytes of a stage: 16 rows, four loads to LDS
+constexpr int kInt8Ring = 4;                   // stages of a wave
 
-// Sums of the strip with MT tiles of 16 tokens over steps lo .. hi - 1.
+// A wave's stages come straight to its own part of LDS, 16 rows x 256 bytes each, so that memory is
+// read in whole stretches (40 experts of 4096 rows of 2048 bytes: 6.9 TB/s non-temporal; with
+// 64 bytes of each of 16 rows at a time, as the operands would take them, 4.8): per 256 of K the token
+// tiles first, then the strip's tiles.  Four stages take turns; no wave waits for another.
+//
+// Piece c (16 bytes) of row r lies at place c ^ r, which leaves the operand reads without bank
+// conflicts; a load fills LDS in lane order, so the lane fetches the piece that belongs there.
+
+// The four operands of a stage (64 of K each): waits until no more than the three stages behind it
+// are on their way; when it returns the stage's place is free.
+__device__ __forceinline__ void int8_operands(unsigned at, i32x4 (&f)[4]) {
+  static_assert(kInt8Ring == 4, "12 loads of the three stages behind this one");
+  asm volatile(
+      "s_waitcnt vmcnt(12)\n\t"
+      "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+      : "v"(at), "v"(at ^ 64), "v"(at ^ 128), "v"(at ^ 192)
+      : "memory");
+}
+
+// Sums of the strip with MT tiles of 16 tokens over steps lo .. hi - 1 of K.
 template <int MT>
 struct Int8Sums {
-  static constexpr int U = 2;  // steps requested together
-  struct Regs {
-    u32x4 w[U][kInt8Tiles], x[U][MT];
-  };
+  static constexpr int kStages = MT + kInt8Tiles;  // per step
   i32x4 acc[MT][kInt8Tiles];
 
   // w0, w1: the matrix from the strip's first row on, for the first and the other half of its
-  // tiles; xrow: byte of the lane's token per tile, or -1.
+  // tiles; xrow[i][q]: byte of the row of tile i that the lane fetches in load q, or kExpertOob.
   __device__ __forceinline__ void run(__amdgpu_buffer_rsrc_t w0, __amdgpu_buffer_rsrc_t w1, int pitch,
-                                      __amdgpu_buffer_rsrc_t x, const int (&xrow)[MT], int K, int lo, int hi) {
-    const int g = lane_id() / 16, m = lane_id() % 16;
+                                      __amdgpu_buffer_rsrc_t x, const int (&xrow)[MT][4], int K, int lo, int hi,
+                                      char* ring) {
+    const int lane = lane_id(), g = lane / 16, m = lane % 16;
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < kInt8Tiles; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-    // pieces past K are those of the next row: their tokens' are zeros
-    auto load = [&](Regs& r, int st) __attribute__((always_inline)) {
+    // load q of a stage: rows 4 q + g
+    int wrow[4], piece[4];
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = (st + u) * kInt8Step + 16 * g;
-        const bool in = st + u < hi && k < K;
+    for (int q = 0; q < 4; ++q) {
+      piece[q] = (m ^ (4 * q + g)) * 16;
+      wrow[q] = (4 * q + g) * pitch + piece[q];
+    }
+    // stage s of step st, to place p; behind the last step: zeros, so that the count of loads stays
+    auto load = [&](int s, int st, int p) __attribute__((always_inline)) {
+      char* dst = ring + p * kInt8Stage;
+      const int k = st * kInt8Step, j = s - MT;
 #pragma unroll
-        for (int j = 0; j < kInt8Tiles; ++j) {
-          const int off = in ? (j % (kInt8Tiles / 2) * 16 + m) * pitch + k : kExpertOob;
-          r.w[u][j] = __builtin_amdgcn_raw_buffer_load_b128(j < kInt8Tiles / 2 ? w0 : w1, off, 0, 2);  // read once
+      for (int q = 0; q < 4; ++q) {
+        const bool in = st < hi && k + piece[q] < K;
+        if (s < MT) {
+          const int off = in && xrow[s < MT ? s : 0][q] != kExpertOob ? xrow[s < MT ? s : 0][q] + k + piece[q] : kExpertOob;
+          __builtin_amdgcn_raw_ptr_buffer_load_lds(x, (lds_void*)(dst + q * 1024), 16, off, 0, 0, 0);
+        } else {
+          // non-temporal: a strip is read once
+          const int off = in ? j % (kInt8Tiles / 2) * 16 * pitch + wrow[q] + k : kExpertOob;
+          if (j < kInt8Tiles / 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(w0, (lds_void*)(dst + q * 1024), 16, off, 0, 0, 2);
+          else __builtin_amdgcn_raw_ptr_buffer_load_lds(w1, (lds_void*)(dst + q * 1024), 16, off, 0, 0, 2);
         }
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-          r.x[u][i] = __builtin_amdgcn_raw_buffer_load_b128(x, in && xrow[i] >= 0 ? xrow[i] + k : kExpertOob, 0, 0);
       }
     };
-    auto multiply = [&](const Regs& r) __attribute__((always_inline)) {
+    const unsigned at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(ring))) +
+                        m * kInt8Step + (g ^ m) * 16;
 #pragma unroll
-      for (int u = 0; u < U; ++u)
+    for (int s = 0; s < kInt8Ring; ++s) load(s % kStages, lo + s / kStages, s);
+    i32x4 xf[MT][4];
+    int n = 0;  // stages taken: the next one lies at place n % 4
+    for (int st = lo; st < hi; ++st) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+      for (int s = 0; s < kStages; ++s) {
+        const int p = n++ % kInt8Ring;
+        if (s < MT) {
+          int8_operands(at + p * kInt8Stage, xf[s < MT ? s : 0]);
+        } else {
+          i32x4 wf[4];
+          int8_operands(at + p * kInt8Stage, wf);
 #pragma unroll
-          for (int j = 0; j < kInt8Tiles; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, r.w[u][j]),
-                                                              __builtin_bit_cast(i32x4, r.x[u][i]), acc[i][j], 0, 0, 0);
-    };
-    Regs ra, rb;
-    load(ra, lo);
-    int st = lo;
-    for (; st + U < hi; st += 2 * U) {
-      load(rb, st + U);
-      multiply(ra);
-      load(ra, st + 2 * U);
-      multiply(rb);
+          for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+              acc[i][s < MT ? 0 : s - MT] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[u], xf[i][u], acc[i][s < MT ? 0 : s - MT], 0, 0, 0);
+        }
+        load((s + kInt8Ring) % kStages, st + (s + kInt8Ring) / kStages, p);
+      }
     }
-    if (st < hi) multiply(ra);
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): nothing is on its way to the ring
+    asm volatile("" ::: "memory");
   }
 
   // Tile i to LDS: token m, the strip's rows next to each other.
@@ -90,15 +126,17 @@ struct Int8Sums {
 // One strip of an expert's matrix past its rows, MT tiles of them at a time, passes dealt to
 // `shares` blocks.  FIRST: hidden (T), else partial integer sums.
 template <class T, int MT, bool FIRST, bool GATED>
-__global__ __launch_bounds__(kInt8Waves* kWave) void layer_int8_kernel(LayerInt8Args b, int shares) {
+__global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerInt8Args b, int shares) {
   constexpr bool kSplit = FIRST && GATED;  // half of the strip's rows are the gate's
   constexpr int NBO = kSplit ? kInt8Strip / 2 : kInt8Strip;
   constexpr int kPitch = kInt8Strip + 4, kThreads = kInt8Waves * kWave;
-  __shared__ __align__(16) int red[kInt8Waves][16 * kPitch];
+  // the waves' rings; then, in the same places, a tile of sums of each
+  __shared__ __align__(1024) char ring[kInt8Waves][kInt8Ring * kInt8Stage];
+  static_assert(16 * kPitch * 4 <= kInt8Ring * kInt8Stage, "room for a tile");
   __shared__ int lists[kLayerMaxChoices];
   __shared__ int wave_n[kInt8Waves];
   const LayerArgs& a = b.a;
-  const int tid = threadIdx.x, m = lane_id() % 16;
+  const int tid = threadIdx.x, g = lane_id() / 16;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   int e, n;
   const int* list;
@@ -114,24 +152,27 @@ __global__ __launch_bounds__(kInt8Waves* kWave) void layer_int8_kernel(LayerInt8
   const int half = kSplit ? NBO : NBO / 2;
   const int64_t apart = static_cast<int64_t>(kSplit ? N : half) * K;
   const int v0 = min(half, N - n0), v1 = kSplit ? v0 : max(0, min(half, N - n0 - half));
-  const __amdgpu_buffer_rsrc_t w0 = expert_rsrc(w, v0 * K), w1 = expert_rsrc(w + apart, v1 * K);
+  const __amdgpu_buffer_rsrc_t w0 = expert_rsrc(w, __builtin_amdgcn_readfirstlane(v0 * K));
+  const __amdgpu_buffer_rsrc_t w1 = expert_rsrc(w + apart, __builtin_amdgcn_readfirstlane(v1 * K));
   const __amdgpu_buffer_rsrc_t x = expert_rsrc(FIRST ? b.qx : b.qh, (FIRST ? a.S : a.S * a.k) * K);
   const int steps = (K + kInt8Step - 1) / kInt8Step, parts = zs * kInt8Waves;
   const int per = (steps + parts - 1) / parts, lo = (z * kInt8Waves + wave) * per;
 
   for (int r0 = 16 * MT * share; r0 < n; r0 += 16 * MT * shares) {
-    int xrow[MT];
+    int xrow[MT][4];
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-      const int li = r0 + 16 * i + m;
-      xrow[i] = li < n ? (FIRST ? list[li] / a.k : list[li]) * K : -1;
-    }
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int li = r0 + 16 * i + 4 * q + g;
+        xrow[i][q] = li < n ? (FIRST ? list[li] / a.k : list[li]) * K : kExpertOob;
+      }
     Int8Sums<MT> sums;
-    sums.run(w0, w1, K, x, xrow, K, lo, min(steps, lo + per));
+    sums.run(w0, w1, K, x, xrow, K, lo, min(steps, lo + per), ring[wave]);
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       if (r0 + 16 * i >= n) break;
-      sums.put(red[wave], i);
+      sums.put(reinterpret_cast<int*>(ring[wave]), i);
       __syncthreads();
       for (int o = tid; o < 16 * NBO; o += kThreads) {
         const int row = o / NBO, c = o % NBO, li = r0 + 16 * i + row;
@@ -139,8 +180,9 @@ __global__ __launch_bounds__(kInt8Waves* kWave) void layer_int8_kernel(LayerInt8
         int v = 0, u = 0;
 #pragma unroll
         for (int q = 0; q < kInt8Waves; ++q) {
-          v += red[q][row * kPitch + c];
-          if constexpr (kSplit) u += red[q][row * kPitch + NBO + c];
+          const int* red = reinterpret_cast<const int*>(ring[q]) + row * kPitch + c;
+          v += red[0];
+          if constexpr (kSplit) u += red[NBO];
         }
         const int choice = list[li];
         if constexpr (FIRST) {
@@ -231,11 +273,10 @@ hipError_t run_layer(const LayerInt8Args& b, hipStream_t st) {
 
 }  // namespace
 
-// Blocks along the second matrix's K: enough that two per CU run, four steps for each wave
-// at least.
+// Blocks along the second matrix's K: enough that two per CU run, a step for each wave at least.
 int layer_int8_splits(const LayerArgs& a) {
   const int64_t blocks = static_cast<int64_t>(slots(a)) * ((a.d + kInt8Strip - 1) / kInt8Strip);
-  const int64_t most = a.h / (kInt8Step * 4 * kInt8Waves);
+  const int64_t most = a.h / (kInt8Step * kInt8Waves);
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({8, most, 512 / std::max<int64_t>(1, blocks)})));
 }
 
