@@ -5,8 +5,8 @@
 // added in runs of equal ids: the sorted tokens are cut into chunks of equal length, however
 // the ids are spread, one group of lanes per chunk and strip of columns.  A run inside one chunk is
 // written at once; the parts of a run that crosses chunks go to the workspace and are added
-// by a last launch.  Rows of the table that no token names are cleared beside it, which is
-// most of what there is to write.
+// by a last launch.  The table is cleared beside the sorting, whose few blocks wait for one
+// another most of the time; rows in use are written again later, which is less than to find the others.
 #include <algorithm>
 
 #include "common.hpp"
@@ -18,7 +18,8 @@ namespace {
 
 // ---------------------------------------------------------------- forward
 // A block's threads as groups of `tpr` (a power of two) along a row, R rows per group at a time.
-template <class T, int R>
+// NT: non-temporal stores.
+template <class T, int R, bool NT>
 __global__ __launch_bounds__(kBlock) void embed_kernel(const int32_t* ids, const T* table, T* y, int T_, int V, int d,
                                                        float scale, int tpr) {
   constexpr int PE = Chunk<T>::kElems;
@@ -43,7 +44,9 @@ __global__ __launch_bounds__(kBlock) void embed_kernel(const int32_t* ids, const
       Chunk<T>::unpack(v[r], f);
 #pragma unroll
       for (int q = 0; q < PE; ++q) f[q] = in ? f[q] * scale : 0.f;  // zeros of padding whatever the scale's sign
-      *reinterpret_cast<u32x4*>(y + (row0 + r) * d + c) = Chunk<T>::pack(f);
+      u32x4* to = reinterpret_cast<u32x4*>(y + (row0 + r) * d + c);
+      if constexpr (NT) __builtin_nontemporal_store(Chunk<T>::pack(f), to);
+      else *to = Chunk<T>::pack(f);
     }
   }
 }
@@ -59,9 +62,13 @@ hipError_t run_embed(const EmbedArgs& a, hipStream_t st) {
   const auto blocks = [&](int r) {
     return long_grid((a.T + static_cast<int64_t>(groups) * r - 1) / (static_cast<int64_t>(groups) * r));
   };
-  // four rows at once where blocks are many, so that four loads are in flight
-  if (a.T >= groups * 4 * 512) embed_kernel<T, 4><<<blocks(4), kBlock, 0, st>>>(a.ids, table, y, a.T, a.V, a.d, a.scale, tpr);
-  else embed_kernel<T, 1><<<blocks(1), kBlock, 0, st>>>(a.ids, table, y, a.T, a.V, a.d, a.scale, tpr);
+  // Rows that no cache holds until they are read (the Infinity Cache has 256 MB) are stored
+  // non-temporally, two per group at once (65536 rows of 4096 bf16: 122 us; one 163, four 127; with
+  // ordinary stores, four, 158).
+  if (static_cast<int64_t>(a.T) * a.d * sizeof(T) > (int64_t(256) << 20))
+    embed_kernel<T, 2, true><<<blocks(2), kBlock, 0, st>>>(a.ids, table, y, a.T, a.V, a.d, a.scale, tpr);
+  else
+    embed_kernel<T, 1, false><<<blocks(1), kBlock, 0, st>>>(a.ids, table, y, a.T, a.V, a.d, a.scale, tpr);
   return hipGetLastError();
 }
 
@@ -72,16 +79,36 @@ __device__ __forceinline__ int embed_key(const int32_t* ids, int64_t t, int V) {
   return id >= 0 && id < V ? id : V;
 }
 
+// Clears a share of the table's gradient: block `block` of those of a launch.
+constexpr int kClearPieces = 8;  // of 16 bytes per thread
+template <int THREADS>
+__device__ __forceinline__ void embed_clear(const EmbedClear& c, int64_t block) {
+  u32x4* p = static_cast<u32x4*>(c.to);
+  const int64_t first = c.first + block * (THREADS * kClearPieces) + threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < kClearPieces; ++i)
+    if (first + i * THREADS < c.end) p[first + i * THREADS] = u32x4{0, 0, 0, 0};
+}
+template <int THREADS>
+int64_t clear_blocks(const EmbedClear& c) {
+  return (c.end - c.first + THREADS * kClearPieces - 1) / (THREADS * kClearPieces);
+}
+
 // Few tokens: token t's place is the number of keys below its own, and of equal ones before
 // it.  A block places 64 tokens, its waves count in a share of all keys each.  (T^2 comparisons;
 // one launch where the passes below take seven.)
 constexpr int kRankWaves = 16;
 constexpr int kRankKeys = 1024;  // keys in LDS at a time
-__global__ __launch_bounds__(kRankWaves* kWave) void embed_rank_kernel(EmbedArgs a) {
+__global__ __launch_bounds__(kRankWaves* kWave) void embed_rank_kernel(EmbedArgs a, EmbedClear clear) {
   __shared__ int keys[kRankKeys];
   __shared__ int part[kRankWaves][kWave];
+  const int64_t block = long_block(), ranks = (a.T + kWave - 1) / kWave;
+  if (block >= ranks) {
+    embed_clear<kRankWaves * kWave>(clear, block - ranks);
+    return;
+  }
   const int lane = lane_id(), wave = threadIdx.x / kWave;
-  const int t = blockIdx.x * kWave + lane;
+  const int t = static_cast<int>(block) * kWave + lane;
   const int mine = t < a.T ? embed_key(a.ids, t, a.V) : 0x7fffffff;
   int below = 0;
   for (int base = 0; base < a.T; base += kRankKeys) {
@@ -107,7 +134,7 @@ __global__ __launch_bounds__(kRankWaves* kWave) void embed_rank_kernel(EmbedArgs
     a.keys[at] = mine;
     a.order[at] = t;
   }
-  if (blockIdx.x == 0 && threadIdx.x == 0) *a.crossing = 0;
+  if (block == 0 && threadIdx.x == 0) *a.crossing = 0;
 }
 
 // More tokens: passes over digits of the key, lowest first, each stable.  A tile of keys
@@ -121,24 +148,34 @@ __device__ __forceinline__ int sort_key(const EmbedSortPass& s, int64_t i) {
   return s.first ? embed_key(s.ids, i, s.V) : s.keys_in[i];
 }
 
-__global__ __launch_bounds__(kBlock) void sort_count_kernel(EmbedSortPass s) {
+__global__ __launch_bounds__(kBlock) void sort_count_kernel(EmbedSortPass s, EmbedClear clear) {
+  const int64_t block = long_block();
+  if (block >= s.tiles) {
+    embed_clear<kBlock>(clear, block - s.tiles);
+    return;
+  }
   __shared__ int count[kDigits];
   count[threadIdx.x] = 0;
   __syncthreads();
 #pragma unroll
   for (int q = 0; q < kSortItems; ++q) {
-    const int64_t i = static_cast<int64_t>(blockIdx.x) * kSortTile + q * kBlock + threadIdx.x;
+    const int64_t i = block * kSortTile + q * kBlock + threadIdx.x;
     if (i < s.T) atomicAdd(&count[(sort_key(s, i) >> s.shift) & (kDigits - 1)], 1);
   }
   __syncthreads();
-  s.counts[static_cast<int64_t>(threadIdx.x) * s.tiles + blockIdx.x] = count[threadIdx.x];
-  if (blockIdx.x == 0 && threadIdx.x == 0) *s.crossing = 0;
+  s.counts[static_cast<int64_t>(threadIdx.x) * s.tiles + block] = count[threadIdx.x];
+  if (block == 0 && threadIdx.x == 0) *s.crossing = 0;
 }
 
 // Block `digit`: its counts of the tiles become the sums of those before; their total.
-__global__ __launch_bounds__(kBlock) void sort_scan_kernel(EmbedSortPass s) {
+__global__ __launch_bounds__(kBlock) void sort_scan_kernel(EmbedSortPass s, EmbedClear clear) {
   __shared__ int wave_sum[kWavesPerBlock];
-  int32_t* c = s.counts + static_cast<int64_t>(blockIdx.x) * s.tiles;
+  const int64_t block = long_block();
+  if (block >= kDigits) {
+    embed_clear<kBlock>(clear, block - kDigits);
+    return;
+  }
+  int32_t* c = s.counts + block * s.tiles;
   const int lane = lane_id(), wave = threadIdx.x / kWave;
   int carry = 0;
   for (int base = 0; base < s.tiles; base += kBlock) {
@@ -161,17 +198,22 @@ __global__ __launch_bounds__(kBlock) void sort_scan_kernel(EmbedSortPass s) {
     if (i < s.tiles) c[i] = before + sum - v;
     __syncthreads();
   }
-  if (threadIdx.x == 0) s.totals[blockIdx.x] = carry;
+  if (threadIdx.x == 0) s.totals[block] = carry;
 }
 
-__global__ __launch_bounds__(kBlock) void sort_place_kernel(EmbedSortPass s) {
+__global__ __launch_bounds__(kBlock) void sort_place_kernel(EmbedSortPass s, EmbedClear clear) {
+  const int64_t block = long_block();
+  if (block >= s.tiles) {
+    embed_clear<kBlock>(clear, block - s.tiles);
+    return;
+  }
   __shared__ int at[kWavesPerBlock][kDigits];  // keys of a wave's part by digit, then their first place
   __shared__ int wave_sum[kWavesPerBlock];
   const int lane = lane_id(), wave = threadIdx.x / kWave, tid = threadIdx.x;
 #pragma unroll
   for (int w = 0; w < kWavesPerBlock; ++w) at[w][tid] = 0;
   __syncthreads();
-  const int64_t base = static_cast<int64_t>(blockIdx.x) * kSortTile + wave * (kWave * kSortItems);
+  const int64_t base = block * kSortTile + wave * (kWave * kSortItems);
   int key[kSortItems], token[kSortItems], rank[kSortItems];
 #pragma unroll
   for (int q = 0; q < kSortItems; ++q) {
@@ -210,7 +252,7 @@ __global__ __launch_bounds__(kBlock) void sort_place_kernel(EmbedSortPass s) {
   int first = sum - total;
 #pragma unroll
   for (int w = 0; w < kWavesPerBlock; ++w) first += w < wave ? wave_sum[w] : 0;
-  first += s.counts[static_cast<int64_t>(tid) * s.tiles + blockIdx.x];
+  first += s.counts[static_cast<int64_t>(tid) * s.tiles + block];
 #pragma unroll
   for (int w = 0; w < kWavesPerBlock; ++w) {
     const int n = at[w][tid];
@@ -256,7 +298,7 @@ __device__ __forceinline__ float* embed_part(const EmbedArgs& a, int64_t chunk, 
 // L lanes per chunk and strip of L pieces; chunks of a.chunk sorted tokens.
 template <class T, int L>
 __device__ __forceinline__ void embed_chunk(const EmbedArgs& a, int64_t unit) {
-  constexpr int PE = Chunk<T>::kElems, U = 8;
+  constexpr int PE = Chunk<T>::kElems, U = L < 16 ? 8 : 16;  // rows in flight
   const int strips = (a.d + L * PE - 1) / (L * PE);
   const int64_t chunk = unit / strips;
   const int strip = static_cast<int>(unit - chunk * strips);
@@ -283,31 +325,39 @@ __device__ __forceinline__ void embed_chunk(const EmbedArgs& a, int64_t unit) {
       embed_write<T>(a, cur, c, sum);
     }
   };
-  for (int64_t i = lo; i < hi; i += U) {
-    int key[U];
-    u32x4 v[U];
+  const int lane = lane_id();
+  for (int64_t base = lo; base < hi; base += L) {
+    // a key and a token per lane, then from lane to lane: loads of single ones would wait for each
+    // other (1024 rows of 256 fp32: 7.9 -> 4.4 us).  Rows are read once, non-temporally (65536 rows of
+    // 4096 bf16: 169 -> 125).
+    const int64_t mine = min(base + lane % L, hi - 1);
+    const int keys = a.keys[mine], tokens = a.order[mine];
+    auto of = [&](int held, int i) {
+      if constexpr (L == kWave) return __builtin_amdgcn_readlane(held, i);
+      else return __shfl(held, i, L);
+    };
+    const int count = static_cast<int>(min(static_cast<int64_t>(L), hi - base));
+    for (int i = 0; i < count; i += U) {
+      u32x4 v[U];
+      // past the chunk's end the last row again, not added; sums of padding rows go nowhere
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int64_t at = min(i + u, hi - 1);
-      key[u] = a.keys[at];
-      // padding rows are not read; past the chunk's end the last one again, not added
-      v[u] = in && key[u] < a.V ? *reinterpret_cast<const u32x4*>(dy + static_cast<int64_t>(a.order[at]) * a.d)
-                                : u32x4{0, 0, 0, 0};
-    }
+      for (int u = 0; u < U; ++u) v[u] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(dy + static_cast<int64_t>(of(tokens, i + u)) * a.d));
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      if (i + u >= hi) continue;
-      if (key[u] != cur) {
-        flush(false);
-        cur = key[u];
-        head = false;
+      for (int u = 0; u < U; ++u) {
+        const int key = of(keys, i + u);
+        if (i + u >= count) continue;
+        if (key != cur) {
+          flush(false);
+          cur = key;
+          head = false;
 #pragma unroll
-        for (int q = 0; q < PE; ++q) sum[q] = 0.f;
+          for (int q = 0; q < PE; ++q) sum[q] = 0.f;
+        }
+        float f[PE];
+        Chunk<T>::unpack(v[u], f);
+#pragma unroll
+        for (int q = 0; q < PE; ++q) sum[q] += f[q];
       }
-      float f[PE];
-      Chunk<T>::unpack(v[u], f);
-#pragma unroll
-      for (int q = 0; q < PE; ++q) sum[q] += f[q];
     }
   }
   flush(to_right);
@@ -317,45 +367,15 @@ __device__ __forceinline__ void embed_chunk(const EmbedArgs& a, int64_t unit) {
   }
 }
 
-// Clears the rows among kClearRows, from v0 on, that no token names: a wave.
-constexpr int kClearRows = 16;
-template <class T>
-__device__ __forceinline__ void embed_clear(const EmbedArgs& a, int64_t v0) {
-  constexpr int PE = Chunk<T>::kElems;
-  const int lane = lane_id();
-  // lanes 0 .. kClearRows - 1: the first sorted token whose key is not below the row
-  const int64_t v = v0 + min(lane, kClearRows - 1);
-  int64_t lo = 0, hi = a.T;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) / 2;
-    if (a.keys[mid] < v) lo = mid + 1;
-    else hi = mid;
-  }
-  const bool empty = lane < kClearRows && v < a.V && (lo >= a.T || a.keys[lo] != v);
-  uint64_t mask = __ballot(empty);
-  while (mask) {
-    const int r = __builtin_ctzll(mask);
-    mask &= mask - 1;
-    T* p = static_cast<T*>(a.dtable) + (v0 + r) * a.d;
-    for (int c = lane * PE; c < a.d; c += kWave * PE) *reinterpret_cast<u32x4*>(p + c) = u32x4{0, 0, 0, 0};
-  }
-}
-
 template <class T, int L>
-__global__ __launch_bounds__(kBlock) void embed_sums_kernel(EmbedArgs a, int64_t sum_blocks) {
-  const int64_t block = long_block();
+__global__ __launch_bounds__(kBlock) void embed_sums_kernel(EmbedArgs a) {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  if (block < sum_blocks) {
-    embed_chunk<T, L>(a, L == kWave ? block * kWavesPerBlock + wave : block * (kBlock / L) + threadIdx.x / L);
-  } else {
-    const int64_t v0 = ((block - sum_blocks) * kWavesPerBlock + wave) * kClearRows;
-    if (v0 < a.V) embed_clear<T>(a, v0);
-  }
+  embed_chunk<T, L>(a, L == kWave ? long_block() * kWavesPerBlock + wave : long_block() * (kBlock / L) + threadIdx.x / L);
 }
 
 // The runs that cross chunks: the parts are added by the block's waves, every kJoinWaves-th
 // each, then over the waves, in an order that the ids alone decide.
-constexpr int kJoinWaves = 4;
+constexpr int kJoinWaves = 8;
 template <class T>
 __global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedArgs a) {
   constexpr int PE = Chunk<T>::kElems;
@@ -367,14 +387,14 @@ __global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedArgs
     const int64_t chunk = a.crossers[item / strips];
     const int c = (static_cast<int>(item % strips) * kWave + lane) * PE;
     const int key = a.keys[(chunk + 1) * a.chunk];  // that of the run, which goes on there
-    // the run's end
-    int64_t lo = (chunk + 1) * a.chunk, hi = a.T;
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) / 2;
-      if (a.keys[mid] <= key) lo = mid + 1;
-      else hi = mid;
+    // one part per chunk that begins inside the run, and the first
+    int64_t parts = 1;
+    for (;;) {
+      const int64_t begin = (chunk + parts + lane) * a.chunk;
+      const uint64_t outside = __ballot(begin >= a.T || a.keys[min(begin, static_cast<int64_t>(a.T) - 1)] != key);
+      parts += outside ? __builtin_ctzll(outside) : kWave;
+      if (outside) break;
     }
-    const int64_t parts = (lo - 1) / a.chunk - chunk + 1;
     float sum[PE];
 #pragma unroll
     for (int q = 0; q < PE; ++q) sum[q] = 0.f;
@@ -430,16 +450,13 @@ template <class T, int L>
 hipError_t run_sums(const EmbedArgs& a, hipStream_t st) {
   const int64_t strips = (a.d + L * Chunk<T>::kElems - 1) / (L * Chunk<T>::kElems);
   const int64_t units = static_cast<int64_t>(embed_chunks(a)) * strips;
-  const int64_t sums = (units + kBlock / L - 1) / (kBlock / L);
-  const int64_t rows = kWavesPerBlock * kClearRows;
-  const int64_t clears = a.accumulate ? 0 : (a.V + rows - 1) / rows;
-  if (sums + clears == 0) return hipSuccess;
-  embed_sums_kernel<T, L><<<long_grid(sums + clears), kBlock, 0, st>>>(a, sums);
+  embed_sums_kernel<T, L><<<long_grid((units + kBlock / L - 1) / (kBlock / L)), kBlock, 0, st>>>(a);
   return hipGetLastError();
 }
 
 template <class T>
 hipError_t run_bwd(const EmbedArgs& a, hipStream_t st) {
+  if (a.T == 0) return hipSuccess;
   hipError_t err = hipSuccess;
   switch (chunk_lanes(a)) {
     case 8: err = run_sums<T, 8>(a, st); break;
@@ -456,10 +473,11 @@ hipError_t run_bwd(const EmbedArgs& a, hipStream_t st) {
 
 }  // namespace
 
-// Sorted tokens per chunk: so that about 16384 waves' worth of chunks and strips run, 8 at least.
+// Sorted tokens per chunk: so that about 4096 waves' worth of chunks and strips run, 8 at least.  (65536
+// tokens of 8 KB by Zipf's law: 16384 waves leave 19 us of parts to join, 4096 leave 8.)
 int embed_chunk_length(int T, int d, int dtype) {
   const int64_t row = static_cast<int64_t>(d) * (dtype == 1 ? 2 : 4);
-  const int64_t want = T * std::max<int64_t>(row, 128) / 1024 / 16384;
+  const int64_t want = T * std::max<int64_t>(row, 128) / 1024 / 4096;
   int n = 8;
   while (n < 1024 && n < want) n *= 2;
   return n;
@@ -475,14 +493,26 @@ hipError_t launch_embed(const EmbedArgs& a, hipStream_t st) {
 hipError_t launch_embed_bwd(const EmbedArgs& a, int32_t* spare_keys, int32_t* spare_order, int32_t* counts,
                             int32_t* totals, hipStream_t st) {
   hipError_t err = hipSuccess;
-  if (a.T > 0 && a.T <= kEmbedRankMax) {
-    embed_rank_kernel<<<dim3((a.T + kWave - 1) / kWave), kRankWaves * kWave, 0, st>>>(a);
+  EmbedClear clear{a.dtable, 0, 0};
+  const int64_t pieces = a.accumulate ? 0 : static_cast<int64_t>(a.V) * a.d * (a.dtype == 1 ? 2 : 4) / 16;
+  if (a.T <= kEmbedRankMax) {
+    clear.end = pieces;
+    constexpr int kThreads = kRankWaves * kWave;
+    const int64_t blocks = (a.T + kWave - 1) / kWave + clear_blocks<kThreads>(clear);
+    if (blocks > 0) embed_rank_kernel<<<long_grid(blocks), kThreads, 0, st>>>(a, clear);
     err = hipGetLastError();
-  } else if (a.T > 0) {
+  } else {
     EmbedSortPass s{};
     s.ids = a.ids; s.T = a.T; s.V = a.V; s.tiles = embed_sort_tiles(a.T);
     s.counts = counts; s.totals = totals; s.crossing = a.crossing;
     const int passes = sort_passes(a.V);
+    int launch = 0;
+    // the next launch's share of the table
+    auto share = [&](int64_t blocks) {
+      clear.first = clear.end;
+      clear.end = pieces * ++launch / (3 * passes);
+      return long_grid(blocks + clear_blocks<kBlock>(clear));
+    };
     for (int p = 0; p < passes && err == hipSuccess; ++p) {
       const bool to_end = (passes - 1 - p) % 2 == 0;  // the last pass ends in a.keys
       s.first = p == 0;
@@ -491,9 +521,12 @@ hipError_t launch_embed_bwd(const EmbedArgs& a, int32_t* spare_keys, int32_t* sp
       s.order_in = to_end ? spare_order : a.order;
       s.keys_out = to_end ? a.keys : spare_keys;
       s.order_out = to_end ? a.order : spare_order;
-      sort_count_kernel<<<dim3(s.tiles), kBlock, 0, st>>>(s);
-      sort_scan_kernel<<<dim3(kDigits), kBlock, 0, st>>>(s);
-      sort_place_kernel<<<dim3(s.tiles), kBlock, 0, st>>>(s);
+      dim3 grid = share(s.tiles);
+      sort_count_kernel<<<grid, kBlock, 0, st>>>(s, clear);
+      grid = share(kDigits);
+      sort_scan_kernel<<<grid, kBlock, 0, st>>>(s, clear);
+      grid = share(s.tiles);
+      sort_place_kernel<<<grid, kBlock, 0, st>>>(s, clear);
       err = hipGetLastError();
     }
   }

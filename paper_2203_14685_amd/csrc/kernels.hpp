@@ -393,6 +393,10 @@ struct EmbedSortPass {
   int32_t *counts, *totals; // [digits, tiles], [digits]
   int32_t* crossing;
 };
+struct EmbedClear {
+  void* to;
+  int64_t first, end;       // pieces of 16 bytes
+};
 int embed_chunk_length(int T, int d, int dtype);
 int embed_chunks(const EmbedArgs& a);
 int embed_sort_tiles(int T);
