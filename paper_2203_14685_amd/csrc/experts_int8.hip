@@ -9,10 +9,24 @@ namespace hetumoe {
 
 namespace {
 
+// Tiles of 256 x 256 where the slots fill them (rows in use vary below them) and there are two
+// rounds of them; the others as for bf16.  (us of the whole call, 256 and 128: 64 x 2560 x 2048 x 2048
+// gated 1775 and 2105, 16 x 1280 x 1024 x 4096 243 and 262, 64 x 256 x 2048 x 2048 gated 298 and 327; 60 x 313
+// x 1408 x 1008 gated 180 and 160, 32 x 640 x 1024 x 2048 gated 229 and 219, 8 x 2048 x 1024 x 1024, one round, 97
+// and 89.  128 x 256: slower everywhere, 64 x 64 where 128 x 128 fill the CUs: 32 x 128 x 1024 x 1024 50 and 40.)
+template <class Fn>
+hipError_t by_tile_int8(const ExpertArgs& x, int M, int N, Fn fn) {
+  auto tiles = [&](int t) { return static_cast<int64_t>(x.E) * ((M + t - 1) / t) * ((N + t - 1) / t); };
+  const int rows256 = (M + 255) / 256 * 256;
+  if (10 * rows256 <= 11 * M && tiles(256) >= 512) return fn(Tile<256, 256, 2, 4, 1>());
+  if (M > 64 && tiles(128) >= 256) return fn(Tile<128, 128, 2, 2, 2>());
+  return fn(Tile<64, 64, 2, 1, 2>());
+}
+
 template <int EPI>
 hipError_t product(const ExpertArgs& x, const ExpertGemmArgs& a, hipStream_t st) {
   constexpr bool kAct = expert_acts(EPI);
-  return by_tile(x, a.M, kAct && x.gated ? 2 * a.N : a.N, [&](auto tile) {
+  return by_tile_int8(x, a.M, kAct && x.gated ? 2 * a.N : a.N, [&](auto tile) {
     using TL = decltype(tile);
     if constexpr (kAct) {
       if (x.gated) return launch_tile_bf16<TL, kRows, kRows, EPI, true>(x, a, st);

@@ -1,7 +1,7 @@
 // Rows and weights as 8-bit integers with a scale each.
 //
 // Rows: bound by memory, one read and half (bf16) or a quarter (fp32) of it written; a row's
-// threads hold it in registers between its maximum and its quantization.  Weights: once, when
+// threads hold it in registers between its maximum and its quantization.  FIGURES  Weights: once, when
 // they are loaded: a pass for the columns' maxima, one that quantizes and transposes.
 #include <algorithm>
 
@@ -13,16 +13,6 @@ namespace hetumoe {
 namespace {
 
 constexpr int kPiece = 16;  // elements that a thread takes at a time: 16 bytes of integers
-
-template <class T>
-__device__ __forceinline__ void load_row_piece(const T* p, float* f) {
-  constexpr int PE = Chunk<T>::kElems;
-  u32x4 v[kPiece / PE];
-#pragma unroll
-  for (int q = 0; q < kPiece / PE; ++q) v[q] = reinterpret_cast<const u32x4*>(p)[q];
-#pragma unroll
-  for (int q = 0; q < kPiece / PE; ++q) Chunk<T>::unpack(v[q], f + q * PE);
-}
 
 // TPR threads per row; the first HELD pieces of each stay in registers, those of longer rows
 // are read again.
@@ -40,16 +30,7 @@ __global__ __launch_bounds__(kBlock) void quantize_rows_kernel(QuantArgs a) {
   const T* x = static_cast<const T*>(a.x) + (in ? row : 0) * a.n;
   const int pieces = in ? a.n / kPiece : 0;
   u32x4 held[HELD][N];
-  int most = 0;
-  auto take = [&](const u32x4 (&v)[N]) __attribute__((always_inline)) {
-#pragma unroll
-    for (int q = 0; q < N; ++q) {
-      float f[PE];
-      Chunk<T>::unpack(v[q], f);
-#pragma unroll
-      for (int j = 0; j < PE; ++j) most = max(most, abs_bits(f[j]));
-    }
-  };
+  MostOf<T> running;
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
     const int p = lane + i * TPR;
@@ -58,14 +39,13 @@ __global__ __launch_bounds__(kBlock) void quantize_rows_kernel(QuantArgs a) {
       held[i][q] = p < pieces ? reinterpret_cast<const u32x4*>(x + p * kPiece)[q] : u32x4{0, 0, 0, 0};
   }
 #pragma unroll
-  for (int i = 0; i < HELD; ++i) take(held[i]);
-  for (int p = lane + HELD * TPR; p < pieces; p += TPR) {
-    u32x4 v[N];
+  for (int i = 0; i < HELD; ++i)
 #pragma unroll
-    for (int q = 0; q < N; ++q) v[q] = reinterpret_cast<const u32x4*>(x + p * kPiece)[q];
-    take(v);
-  }
-  most = group_reduce<(TPR < kWave ? TPR : kWave)>(most, OpMaxI());
+    for (int q = 0; q < N; ++q) running.take(held[i][q]);
+  for (int p = lane + HELD * TPR; p < pieces; p += TPR)
+#pragma unroll
+    for (int q = 0; q < N; ++q) running.take(reinterpret_cast<const u32x4*>(x + p * kPiece)[q]);
+  int most = group_reduce<(TPR < kWave ? TPR : kWave)>(running.bits(), OpMaxI());
   if constexpr (TPR > kWave) {
     static_assert(TPR == kBlock, "a row per block");
     if (lane_id() == 0) wave_most[threadIdx.x / kWave] = most;
@@ -77,10 +57,7 @@ __global__ __launch_bounds__(kBlock) void quantize_rows_kernel(QuantArgs a) {
   const Quantizer quant(most);
   int8_t* out = a.q + row * a.n;
   auto put = [&](const u32x4 (&v)[N], int p) __attribute__((always_inline)) {
-    float f[kPiece];
-#pragma unroll
-    for (int q = 0; q < N; ++q) Chunk<T>::unpack(v[q], f + q * PE);
-    *reinterpret_cast<u32x4*>(out + p * kPiece) = u32x4{quant.four(f), quant.four(f + 4), quant.four(f + 8), quant.four(f + 12)};
+    *reinterpret_cast<u32x4*>(out + p * kPiece) = quantize_piece<T>(quant, v);
   };
 #pragma unroll
   for (int i = 0; i < HELD; ++i) {
