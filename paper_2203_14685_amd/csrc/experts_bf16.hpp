@@ -79,6 +79,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16, NP = NT / 2;
   static_assert(NT == 4, "64 columns per wave");
   constexpr bool kInt8 = expert_int8(EPI);
+  constexpr bool kScratch = kInt8 && expert_acts(EPI);  // nothing reads hidden behind the rows in use
   // columns of the output per block and wave: with GATED in the forward product half of
   // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
   constexpr bool kSplit = expert_acts(EPI) && GATED;
@@ -146,6 +147,8 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   constexpr int kStoresPre = expert_acts(EPI) && !kInt8 ? kStores + MT * NP : kStores;
   f32x4 acc[MT][NT];
   u32x4 fa[MT], fb[NT], fn[NT];
+  // 8-bit integers: the lane's rows' scales, its columns' scales and bias
+  float sr[kInt8 ? MT : 1], sc[kInt8 ? NP : 1][8], sbias[kInt8 ? NP : 1][8];
   auto load = [&](bf16_t* As, bf16_t* Bs) __attribute__((always_inline)) {
     oa.load(As, wave, left);
     ob.load(Bs, wave, left);
@@ -263,7 +266,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   }
   // the tiles without work that this block clears
   int idle = blockIdx.x;
-  if (!work && !tiles.clear(a, idle, at)) return;
+  if (!work && (kScratch || !tiles.clear(a, idle, at))) return;
   for (;;) {
   bool more = false;
 #pragma unroll
@@ -288,6 +291,26 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
 #pragma unroll
     for (int i = 0; i < MT; ++i) fa[i] = ra.read(A0, at_a, 0, i);
     for (int k = kTurn; k < K; k += kTurn) turn(ExpertInt<1>());
+    if constexpr (kInt8) {
+      // requested ahead of the next tile's stages: loads arrive in order, and behind them these would
+      // hold up the results until the stages are there
+      const int ln = expert_opaque(lane), lrow = wm * MT * 16 + ln % 16;
+      const int c0 = at.bn * BNO + (kSplit ? wn * 32 : wn * 64) + 16 * (ln / 16 % 2) + 8 * (ln / 32);
+      const int N1 = kSplit ? 2 * a.N : a.N;
+      const float* sa = a.sa + static_cast<int64_t>(at.e) * a.C + at.bm * BM + lrow;
+#pragma unroll
+      for (int i = 0; i < MT; ++i) sr[i] = at.bm * BM + lrow + 16 * i < n ? sa[16 * i] : 0.f;
+#pragma unroll
+      for (int p = 0; p < NP; ++p) {
+        const int c = kSplit ? c0 : c0 + 32 * p;
+        const int64_t from = static_cast<int64_t>(at.e) * N1 + c + (kSplit && p ? a.N : 0);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+          sc[p][q] = c < a.N ? a.sb[from + q] : 0.f;
+          sbias[p][q] = a.bias && c < a.N ? a.bias[from + q] : 0.f;
+        }
+      }
+    }
     aim(more, next);
     turn(ExpertInt<0>());
     // the last sums leave the matrix unit before they are read
@@ -332,43 +355,27 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
     using Out = std::conditional_t<expert_int8_f32(EPI), float, bf16_t>;
     constexpr int kElt = static_cast<int>(sizeof(Out));
     constexpr bool kAct = expert_acts(EPI);
-    const int N1 = kSplit ? 2 * a.N : a.N;
     const __amdgpu_buffer_rsrc_t out =
         expert_rows<Out>(reinterpret_cast<const Out*>(a.out) + e * a.sO, m0, a.ldo, valid);
-    // scales of the rows in use; the others' are not written
-    const float* sa = a.sa + static_cast<int64_t>(e) * a.C + m0 + lrow;
-    float sr[MT];
-#pragma unroll
-    for (int i = 0; i < MT; ++i) sr[i] = m0 + lrow + 16 * i < rows ? sa[16 * i] : 0.f;
 #pragma unroll
     for (int p = 0; p < (kSplit ? 1 : NP); ++p) {
       const int c = col0 + 32 * p;
-      const int64_t at = static_cast<int64_t>(e) * N1 + c;
-      // of the 8 columns, and of the other factor's 8
-      float sc[kSplit ? 2 : 1][8], bias[kSplit ? 2 : 1][8];
-#pragma unroll
-      for (int s = 0; s < (kSplit ? 2 : 1); ++s)
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-          sc[s][q] = c < a.N ? a.sb[at + s * a.N + q] : 0.f;
-          bias[s][q] = a.bias && c < a.N ? a.bias[at + s * a.N + q] : 0.f;
-        }
       auto finish = [&](auto which) {
         constexpr int ACT = decltype(which)::v;
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
           const bool used = m0 + lrow + 16 * i < rows;
           // an exact sum, rounded once to 24 bits
-          auto scaled = [&](int pair, int s, int q) {
-            const float v = static_cast<float>(__float_as_int(value(i, pair, q))) * sr[i] * sc[s][q] + bias[s][q];
+          auto scaled = [&](int pair, int q) {
+            const float v = static_cast<float>(__float_as_int(value(i, pair, q))) * sr[i] * sc[pair][q] + sbias[pair][q];
             return used ? v : 0.f;
           };
           float f[8];
 #pragma unroll
           for (int q = 0; q < 8; ++q) {
-            f[q] = scaled(p, 0, q);
+            f[q] = scaled(p, q);
             if constexpr (kAct) f[q] = expert_act<ACT>(f[q]);
-            if constexpr (kSplit) f[q] *= scaled(1, 1, q);
+            if constexpr (kSplit) f[q] *= scaled(1, q);
           }
           const unsigned off = static_cast<unsigned>(c < a.N ? (lrow * a.ldo + c) * kElt : kExpertOob) + i * 16 * kElt * a.ldo;
           if constexpr (kElt == 2) {
@@ -538,7 +545,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   if (work) expert_stage_barrier();  // nothing is on its way to LDS when the block ends
   else idle += gridDim.x;
   work = false;
-  if (!tiles.clear(a, idle, at)) return;
+  if (kScratch || !tiles.clear(a, idle, at)) return;
   }
 }
 
