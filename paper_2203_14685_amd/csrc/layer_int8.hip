@@ -5,10 +5,12 @@
 // along K, so 16 bytes of one are a lane's part of a matrix-core operand: 16 rows of the
 // matrix are one operand, 16 tokens the other.  A block's waves take ranges of K and add their
 // sums, which are exact, in LDS; K of the second product is also split over blocks.
-// Tokens and hidden rows are quantized by launches of their own: a row's scale needs all of it.
+// Tokens and hidden rows are quantized by launches of their own, since a row's scale needs all of it, or,
+// few rows, by every block that reads them.
 #include <algorithm>
 
 #include "experts.hpp"
+#include "int8.hpp"
 #include "layer_choices.hpp"
 
 namespace hetumoe {
@@ -23,6 +25,9 @@ constexpr int kInt8Strip = 16 * kInt8Tiles;
 constexpr int kInt8Step = 256;                 // K of one stage: bytes of a row that are read together
 constexpr int kInt8Stage = 16 * kInt8Step;     // bytes of a stage: 16 rows, four loads to LDS
 constexpr int kInt8Ring = 4;                   // stages of a wave
+// Rows that a block quantizes itself: at most 4 of at most 8192 elements, the bytes of its range of K in
+// LDS beside the rings of two blocks.
+constexpr int kInt8HeldRows = 4, kInt8HeldK = 8192, kInt8HeldBytes = 12 * 1024;
 
 // A wave's stages come straight to its own part of LDS, 16 rows x 256 bytes each, so that memory is
 // read in whole stretches (40 experts of 4096 rows of 2048 bytes: 6.9 TB/s non-temporal; with
@@ -45,58 +50,84 @@ __device__ __forceinline__ void int8_operands(unsigned at, i32x4 (&f)[4]) {
       : "memory");
 }
 
-// Sums of the strip with MT tiles of 16 tokens over steps lo .. hi - 1 of K.
-template <int MT>
-struct Int8Sums {
-  static constexpr int kStages = MT + kInt8Tiles;  // per step
-  i32x4 acc[MT][kInt8Tiles];
+// The same of tokens in LDS, whose places the block has filled.
+__device__ __forceinline__ void int8_tokens(unsigned at, i32x4 (&f)[4]) {
+  asm volatile(
+      "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\t"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(f[0]), "=&v"(f[1]), "=&v"(f[2]), "=&v"(f[3])
+      : "v"(at), "v"(at + 64), "v"(at + 128), "v"(at + 192)
+      : "memory");
+}
 
-  // w0, w1: the matrix from the strip's first row on, for the first and the other half of its
-  // tiles; xrow[i][q]: byte of the row of tile i that the lane fetches in load q, or kExpertOob.
-  __device__ __forceinline__ void run(__amdgpu_buffer_rsrc_t w0, __amdgpu_buffer_rsrc_t w1, int pitch,
-                                      __amdgpu_buffer_rsrc_t x, const int (&xrow)[MT][4], int K, int lo, int hi,
-                                      char* ring) {
+__device__ __forceinline__ unsigned lds_address(const void* p) {
+  return static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) const char*)(p)));
+}
+
+// Sums of the strip with MT tiles of 16 tokens over steps lo .. hi - 1 of K.  HELD: the tokens lie in
+// LDS already, else they come with the matrix.
+template <int MT, bool HELD>
+struct Int8Sums {
+  static constexpr int kTokens = HELD ? 0 : MT;       // stages of tokens
+  static constexpr int kStages = kTokens + kInt8Tiles;  // per step
+  i32x4 acc[MT][kInt8Tiles];
+  __amdgpu_buffer_rsrc_t w0, w1;  // the matrix from the strip's first row on: of the first and the other half of its tiles
+  __amdgpu_buffer_rsrc_t x;
+  int pitch, K, lo, hi;
+  int xrow[MT][4];                // byte of the row of tile i that the lane fetches in load q, or kExpertOob
+  char* ring;
+
+  // Stage s of step st, to place p; behind the last step: zeros, so that the count of loads stays.  Load
+  // q of a stage: rows 4 q + g.
+  __device__ __forceinline__ void load(int s, int st, int p) const {
     const int lane = lane_id(), g = lane / 16, m = lane % 16;
+    char* dst = ring + p * kInt8Stage;
+    const int k = st * kInt8Step, j = s - kTokens;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int piece = (m ^ (4 * q + g)) * 16;
+      const bool in = st < hi && k + piece < K;
+      if (s < kTokens) {
+        const int row = xrow[s < MT ? s : 0][q];
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(x, (lds_void*)(dst + q * 1024), 16,
+                                                 in && row != kExpertOob ? row + k + piece : kExpertOob, 0, 0, 0);
+      } else {
+        // non-temporal: a strip is read once
+        const int off = in ? (j % (kInt8Tiles / 2) * 16 + 4 * q + g) * pitch + piece + k : kExpertOob;
+        if (j < kInt8Tiles / 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(w0, (lds_void*)(dst + q * 1024), 16, off, 0, 0, 2);
+        else __builtin_amdgcn_raw_ptr_buffer_load_lds(w1, (lds_void*)(dst + q * 1024), 16, off, 0, 0, 2);
+      }
+    }
+  }
+
+  // The first stages.
+  __device__ __forceinline__ void begin() {
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
       for (int j = 0; j < kInt8Tiles; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
-    // load q of a stage: rows 4 q + g
-    int wrow[4], piece[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      piece[q] = (m ^ (4 * q + g)) * 16;
-      wrow[q] = (4 * q + g) * pitch + piece[q];
-    }
-    // stage s of step st, to place p; behind the last step: zeros, so that the count of loads stays
-    auto load = [&](int s, int st, int p) __attribute__((always_inline)) {
-      char* dst = ring + p * kInt8Stage;
-      const int k = st * kInt8Step, j = s - MT;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const bool in = st < hi && k + piece[q] < K;
-        if (s < MT) {
-          const int off = in && xrow[s < MT ? s : 0][q] != kExpertOob ? xrow[s < MT ? s : 0][q] + k + piece[q] : kExpertOob;
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(x, (lds_void*)(dst + q * 1024), 16, off, 0, 0, 0);
-        } else {
-          // non-temporal: a strip is read once
-          const int off = in ? j % (kInt8Tiles / 2) * 16 * pitch + wrow[q] + k : kExpertOob;
-          if (j < kInt8Tiles / 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(w0, (lds_void*)(dst + q * 1024), 16, off, 0, 0, 2);
-          else __builtin_amdgcn_raw_ptr_buffer_load_lds(w1, (lds_void*)(dst + q * 1024), 16, off, 0, 0, 2);
-        }
-      }
-    };
-    const unsigned at = static_cast<unsigned>(reinterpret_cast<uintptr_t>((__attribute__((address_space(3))) char*)(ring))) +
-                        m * kInt8Step + (g ^ m) * 16;
 #pragma unroll
     for (int s = 0; s < kInt8Ring; ++s) load(s % kStages, lo + s / kStages, s);
+  }
+
+  // HELD: token row m lies at `tokens`, the steps from `first` on, for m < n.
+  __device__ __forceinline__ void finish(unsigned tokens, int first, int n) {
+    const int lane = lane_id(), g = lane / 16, m = lane % 16;
+    const unsigned at = lds_address(ring) + m * kInt8Step + (g ^ m) * 16;
     i32x4 xf[MT][4];
-    int n = 0;  // stages taken: the next one lies at place n % 4
+    int taken = 0;  // stages: the next one lies at place taken % 4
     for (int st = lo; st < hi; ++st) {
+      if constexpr (HELD) {
+        int8_tokens(tokens + (st - first) * kInt8Step + g * 16, xf[0]);
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) xf[0][u][q] = m < n ? xf[0][u][q] : 0;
+      }
 #pragma unroll
       for (int s = 0; s < kStages; ++s) {
-        const int p = n++ % kInt8Ring;
-        if (s < MT) {
+        const int p = taken++ % kInt8Ring;
+        if (s < kTokens) {
           int8_operands(at + p * kInt8Stage, xf[s < MT ? s : 0]);
         } else {
           i32x4 wf[4];
@@ -105,7 +136,7 @@ struct Int8Sums {
           for (int u = 0; u < 4; ++u)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
-              acc[i][s < MT ? 0 : s - MT] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[u], xf[i][u], acc[i][s < MT ? 0 : s - MT], 0, 0, 0);
+              acc[i][s < kTokens ? 0 : s - kTokens] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wf[u], xf[i][u], acc[i][s < kTokens ? 0 : s - kTokens], 0, 0, 0);
         }
         load((s + kInt8Ring) % kStages, st + (s + kInt8Ring) / kStages, p);
       }
@@ -123,9 +154,46 @@ struct Int8Sums {
   }
 };
 
+// Row `row` of K elements of T quantized by the block: its bytes p0 .. p0 + bytes - 1 (zeros behind K) to
+// `to`; returns the scale.  `most`: LDS of a value per wave, not in use by other rows.  between() runs while
+// the row is on its way.
+template <class T, class Fn>
+__device__ __forceinline__ float int8_hold(const T* row, int K, int p0, int bytes, char* to, int* most, Fn between) {
+  constexpr int N = 16 / Chunk<T>::kElems, kThreads = kInt8Waves * kWave, kPieces = kInt8HeldK / 16 / kThreads;
+  const __amdgpu_buffer_rsrc_t r = expert_rsrc(row, K * static_cast<int>(sizeof(T)));
+  u32x4 v[kPieces][N];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int q = 0; q < N; ++q)  // zeros behind the row
+      v[i][q] = __builtin_amdgcn_raw_buffer_load_b128(
+          r, (i * kThreads + static_cast<int>(threadIdx.x)) * 16 * static_cast<int>(sizeof(T)) + 16 * q, 0, 0);
+  __builtin_amdgcn_sched_barrier(0);
+  between();
+  __builtin_amdgcn_sched_barrier(0);
+  MostOf<T> running;
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i)
+#pragma unroll
+    for (int q = 0; q < N; ++q) running.take(v[i][q]);
+  int a = group_reduce<kWave>(running.bits(), OpMaxI());
+  if (lane_id() == 0) most[threadIdx.x / kWave] = a;
+  expert_stage_barrier<63>();  // the stages on their way need not arrive
+#pragma unroll
+  for (int w = 0; w < kInt8Waves; ++w) a = max(a, most[w]);
+  const Quantizer quant(a);
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int k = (i * kThreads + static_cast<int>(threadIdx.x)) * 16 - p0;
+    if (k >= 0 && k < bytes) *reinterpret_cast<u32x4*>(to + k) = quantize_piece<T>(quant, v[i]);
+  }
+  return quant.scale;
+}
+
 // One strip of an expert's matrix past its rows, MT tiles of them at a time, passes dealt to
-// `shares` blocks.  FIRST: hidden (T), else partial integer sums.
-template <class T, int MT, bool FIRST, bool GATED>
+// `shares` blocks.  FIRST: hidden (T), else partial integer sums.  HELD: the block quantizes its few rows
+// itself (x or hidden in T) while its first stages are on their way, else they were before.
+template <class T, int MT, bool FIRST, bool GATED, bool HELD>
 __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerInt8Args b, int shares) {
   constexpr bool kSplit = FIRST && GATED;  // half of the strip's rows are the gate's
   constexpr int NBO = kSplit ? kInt8Strip / 2 : kInt8Strip;
@@ -133,7 +201,10 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
   // the waves' rings; then, in the same places, a tile of sums of each
   __shared__ __align__(1024) char ring[kInt8Waves][kInt8Ring * kInt8Stage];
   static_assert(16 * kPitch * 4 <= kInt8Ring * kInt8Stage, "room for a tile");
-  __shared__ int lists[kLayerMaxChoices];
+  __shared__ __align__(16) char tokens[HELD ? kInt8HeldBytes : 16];
+  __shared__ float token_scale[kInt8HeldRows];
+  __shared__ int most[kInt8HeldRows][kInt8Waves];
+  __shared__ int lists[HELD ? kInt8Waves * kWave : kLayerMaxChoices];  // HELD: a list per wave
   __shared__ int wave_n[kInt8Waves];
   const LayerArgs& a = b.a;
   const int tid = threadIdx.x, g = lane_id() / 16;
@@ -142,6 +213,7 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
   const int* list;
   if (!layer_choices<kInt8Waves>(a, lists, wave_n, e, n, list)) return;
   e = __builtin_amdgcn_readfirstlane(e);
+  n = __builtin_amdgcn_readfirstlane(n);
   const int share = blockIdx.z % shares, z = blockIdx.z / shares, zs = gridDim.z / shares;
   if (n <= 16 * MT * share) return;
 
@@ -152,23 +224,41 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
   const int half = kSplit ? NBO : NBO / 2;
   const int64_t apart = static_cast<int64_t>(kSplit ? N : half) * K;
   const int v0 = min(half, N - n0), v1 = kSplit ? v0 : max(0, min(half, N - n0 - half));
-  const __amdgpu_buffer_rsrc_t w0 = expert_rsrc(w, __builtin_amdgcn_readfirstlane(v0 * K));
-  const __amdgpu_buffer_rsrc_t w1 = expert_rsrc(w + apart, __builtin_amdgcn_readfirstlane(v1 * K));
-  const __amdgpu_buffer_rsrc_t x = expert_rsrc(FIRST ? b.qx : b.qh, (FIRST ? a.S : a.S * a.k) * K);
   const int steps = (K + kInt8Step - 1) / kInt8Step, parts = zs * kInt8Waves;
-  const int per = (steps + parts - 1) / parts, lo = (z * kInt8Waves + wave) * per;
+  const int per = (steps + parts - 1) / parts, first = z * kInt8Waves * per;
+  Int8Sums<MT, HELD> sums;
+  sums.w0 = expert_rsrc(w, __builtin_amdgcn_readfirstlane(v0 * K));
+  sums.w1 = expert_rsrc(w + apart, __builtin_amdgcn_readfirstlane(v1 * K));
+  sums.x = expert_rsrc(FIRST ? b.qx : b.qh, (FIRST ? a.S : a.S * a.k) * K);
+  sums.pitch = sums.K = K;
+  sums.lo = first + wave * per;
+  sums.hi = min(steps, sums.lo + per);
+  sums.ring = ring[wave];
 
   for (int r0 = 16 * MT * share; r0 < n; r0 += 16 * MT * shares) {
-    int xrow[MT][4];
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int li = r0 + 16 * i + 4 * q + g;
-        xrow[i][q] = li < n ? (FIRST ? list[li] / a.k : list[li]) * K : kExpertOob;
+    if constexpr (HELD) {
+      const int bytes = kInt8Waves * per * kInt8Step;  // of a row, from step `first` on
+      for (int r = 0; r < n; ++r) {
+        const int64_t row = __builtin_amdgcn_readfirstlane(FIRST ? list[r] / a.k : list[r]);
+        const float scale = int8_hold(reinterpret_cast<const T*>(FIRST ? a.x : a.hidden) + row * K, K, first * kInt8Step, bytes,
+                                      tokens + r * bytes, most[r], [&]() { if (r == 0) sums.begin(); });
+        if (tid == 0) token_scale[r] = scale;
+        if (!FIRST && tid == 0 && blockIdx.x == 0 && z == 0) b.sh[row] = scale;
       }
-    Int8Sums<MT> sums;
-    sums.run(w0, w1, K, x, xrow, K, lo, min(steps, lo + per), ring[wave]);
+      expert_stage_barrier<63>();
+      const int m = min(static_cast<int>(lane_id() % 16), n - 1);
+      sums.finish(lds_address(tokens) + m * bytes, first, n);
+    } else {
+#pragma unroll
+      for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int li = r0 + 16 * i + 4 * q + g;
+          sums.xrow[i][q] = li < n ? (FIRST ? list[li] / a.k : list[li]) * K : kExpertOob;
+        }
+      sums.begin();
+      sums.finish(0, 0, 0);
+    }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
       if (r0 + 16 * i >= n) break;
@@ -186,7 +276,7 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
         }
         const int choice = list[li];
         if constexpr (FIRST) {
-          const float sx = b.sx[choice / a.k];
+          const float sx = HELD ? token_scale[li] : b.sx[choice / a.k];
           const int64_t at = static_cast<int64_t>(e) * N1 + n0 + c;
           const float p = static_cast<float>(v) * sx * b.s1[at] + (a.b1 ? a.b1[at] : 0.f);
           float f = 0.f;
@@ -231,7 +321,15 @@ __global__ __launch_bounds__(kBlock) void layer_int8_combine_kernel(LayerInt8Arg
 
 int slots(const LayerArgs& a) { return a.by_choice ? a.S * a.k : a.E; }
 
-template <class T, int MT, bool FIRST>
+// Whether the strips' blocks quantize their rows themselves: few rows, whose launches would take longer.
+bool held(const LayerArgs& a, bool first, int z) {
+  const int K = first ? a.d : a.h;
+  const int steps = (K + kInt8Step - 1) / kInt8Step, parts = z * kInt8Waves;
+  return a.S <= kInt8HeldRows && K <= kInt8HeldK &&
+         static_cast<int64_t>(a.S) * ((steps + parts - 1) / parts) * kInt8Waves * kInt8Step <= kInt8HeldBytes;
+}
+
+template <class T, int MT, bool FIRST, bool HELD>
 hipError_t strip(const LayerInt8Args& b, int z, hipStream_t st) {
   const LayerArgs& a = b.a;
   const int N = FIRST ? a.h : a.d, nbo = FIRST && a.gated ? kInt8Strip / 2 : kInt8Strip;
@@ -240,32 +338,38 @@ hipError_t strip(const LayerInt8Args& b, int z, hipStream_t st) {
   const int shares = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(passes, 512 / blocks)));
   const dim3 grid(static_cast<unsigned>(strips), slots(a), z * shares);
   constexpr int kThreads = kInt8Waves * kWave;
-  if (FIRST && a.gated) layer_int8_kernel<T, MT, FIRST, true><<<grid, kThreads, 0, st>>>(b, shares);
-  else layer_int8_kernel<T, MT, FIRST, false><<<grid, kThreads, 0, st>>>(b, shares);
+  if (FIRST && a.gated) layer_int8_kernel<T, MT, FIRST, true, HELD><<<grid, kThreads, 0, st>>>(b, shares);
+  else layer_int8_kernel<T, MT, FIRST, false, HELD><<<grid, kThreads, 0, st>>>(b, shares);
   return hipGetLastError();
 }
 
+// Tokens (x) or hidden rows quantized, and the strips.
 template <class T, bool FIRST>
 hipError_t strips(const LayerInt8Args& b, hipStream_t st) {
   const LayerArgs& a = b.a;
   const int z = FIRST ? 1 : a.z2;
+  if (held(a, FIRST, z)) return strip<T, 1, FIRST, true>(b, z, st);
+  QuantArgs q{};
+  q.dtype = a.dtype;
+  if (FIRST) {
+    q.rows = a.S; q.n = a.d; q.x = a.x; q.q = b.qx; q.scale = b.sx;
+  } else {
+    q.rows = static_cast<int64_t>(a.S) * a.k; q.n = a.h; q.x = a.hidden; q.q = b.qh; q.scale = b.sh;
+  }
+  const hipError_t err = launch_quantize(q, st);
+  if (err != hipSuccess) return err;
   // token tiles in registers for about twice the mean rows of an expert
   const int64_t rows = std::min<int64_t>(a.S, 2 * ((static_cast<int64_t>(a.S) * a.k + a.E - 1) / a.E));
-  if (rows <= 16) return strip<T, 1, FIRST>(b, z, st);
-  if (rows <= 32) return strip<T, 2, FIRST>(b, z, st);
-  return strip<T, 4, FIRST>(b, z, st);
+  if (rows <= 16) return strip<T, 1, FIRST, false>(b, z, st);
+  if (rows <= 32) return strip<T, 2, FIRST, false>(b, z, st);
+  return strip<T, 4, FIRST, false>(b, z, st);
 }
 
 template <class T>
 hipError_t run_layer(const LayerInt8Args& b, hipStream_t st) {
   const LayerArgs& a = b.a;
-  QuantArgs q{};
-  q.rows = a.S; q.n = a.d; q.dtype = a.dtype; q.x = a.x; q.q = b.qx; q.scale = b.sx;
-  hipError_t err = launch_quantize(q, st);
+  hipError_t err = strips<T, true>(b, st);
   if (err != hipSuccess) return err;
-  if ((err = strips<T, true>(b, st)) != hipSuccess) return err;
-  q.rows = static_cast<int64_t>(a.S) * a.k; q.n = a.h; q.x = a.hidden; q.q = b.qh; q.scale = b.sh;
-  if ((err = launch_quantize(q, st)) != hipSuccess) return err;
   if ((err = strips<T, false>(b, st)) != hipSuccess) return err;
   layer_int8_combine_kernel<T><<<dim3((a.d + 4 * kBlock - 1) / (4 * kBlock), a.S), kBlock, 0, st>>>(b);
   return hipGetLastError();
