@@ -25,7 +25,7 @@ constexpr int kInt8Strip = 16 * kInt8Tiles;
 constexpr int kInt8Step = 256;                 // K of one stage: bytes of a row that are read together
 constexpr int kInt8Stage = 16 * kInt8Step;     // bytes of a stage: 16 rows, four loads to LDS
 constexpr int kInt8Ring = 4;                   // stages of a wave
-// Rows that a block quantizes itself: at most 4 of at most 8192 elements, the bytes of its range of K in
+// Rows that a block quantizes itself: 4 at a time of at most 8192 elements, the bytes of its range of K in
 // LDS beside the rings of two blocks.
 constexpr int kInt8HeldRows = 4, kInt8HeldK = 8192, kInt8HeldBytes = 12 * 1024;
 
@@ -215,7 +215,8 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
   e = __builtin_amdgcn_readfirstlane(e);
   n = __builtin_amdgcn_readfirstlane(n);
   const int share = blockIdx.z % shares, z = blockIdx.z / shares, zs = gridDim.z / shares;
-  if (n <= 16 * MT * share) return;
+  constexpr int kPass = HELD ? kInt8HeldRows : 16 * MT;  // rows at a time
+  if (n <= kPass * share) return;
 
   const int K = FIRST ? a.d : a.h, N = FIRST ? a.h : a.d, N1 = kSplit ? 2 * N : N;
   const int n0 = blockIdx.x * NBO;
@@ -235,19 +236,20 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
   sums.hi = min(steps, sums.lo + per);
   sums.ring = ring[wave];
 
-  for (int r0 = 16 * MT * share; r0 < n; r0 += 16 * MT * shares) {
+  for (int r0 = kPass * share; r0 < n; r0 += kPass * shares) {
     if constexpr (HELD) {
       const int bytes = kInt8Waves * per * kInt8Step;  // of a row, from step `first` on
-      for (int r = 0; r < n; ++r) {
-        const int64_t row = __builtin_amdgcn_readfirstlane(FIRST ? list[r] / a.k : list[r]);
+      const int held = min(kPass, n - r0);
+      for (int r = 0; r < held; ++r) {
+        const int64_t row = __builtin_amdgcn_readfirstlane(FIRST ? list[r0 + r] / a.k : list[r0 + r]);
         const float scale = int8_hold(reinterpret_cast<const T*>(FIRST ? a.x : a.hidden) + row * K, K, first * kInt8Step, bytes,
                                       tokens + r * bytes, most[r], [&]() { if (r == 0) sums.begin(); });
         if (tid == 0) token_scale[r] = scale;
         if (!FIRST && tid == 0 && blockIdx.x == 0 && z == 0) b.sh[row] = scale;
       }
       expert_stage_barrier<63>();
-      const int m = min(static_cast<int>(lane_id() % 16), n - 1);
-      sums.finish(lds_address(tokens) + m * bytes, first, n);
+      const int m = min(static_cast<int>(lane_id() % 16), held - 1);
+      sums.finish(lds_address(tokens) + m * bytes, first, held);
     } else {
 #pragma unroll
       for (int i = 0; i < MT; ++i)
@@ -264,7 +266,7 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
       if (r0 + 16 * i >= n) break;
       sums.put(reinterpret_cast<int*>(ring[wave]), i);
       __syncthreads();
-      for (int o = tid; o < 16 * NBO; o += kThreads) {
+      for (int o = tid; o < (HELD ? kInt8HeldRows : 16) * NBO; o += kThreads) {
         const int row = o / NBO, c = o % NBO, li = r0 + 16 * i + row;
         if (li >= n || n0 + c >= N) continue;
         int v = 0, u = 0;
@@ -276,7 +278,7 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
         }
         const int choice = list[li];
         if constexpr (FIRST) {
-          const float sx = HELD ? token_scale[li] : b.sx[choice / a.k];
+          const float sx = HELD ? token_scale[row] : b.sx[choice / a.k];
           const int64_t at = static_cast<int64_t>(e) * N1 + n0 + c;
           const float p = static_cast<float>(v) * sx * b.s1[at] + (a.b1 ? a.b1[at] : 0.f);
           float f = 0.f;
@@ -295,24 +297,55 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
 }
 
 // y[s, c] = sum over r of weights[s, r] (sum over z of part[z, s k + r, c] sh[s k + r] s2[e, c] + b2[e, c]).
+// Two choices and four parts of each are requested together: with one block per 256 columns it is
+// their latency that counts (one token, two choices, four parts: 7.0 -> 4.5 us).
 template <class T>
-__global__ __launch_bounds__(kBlock) void layer_int8_combine_kernel(LayerInt8Args b) {
+__global__ __launch_bounds__(kWave) void layer_int8_combine_kernel(LayerInt8Args b) {
   const LayerArgs& a = b.a;
-  const int s = blockIdx.y, c = (blockIdx.x * kBlock + threadIdx.x) * 4;
+  const int s = blockIdx.y, c = (blockIdx.x * kWave + threadIdx.x) * 4;
   if (c >= a.d) return;
   const int64_t choices = static_cast<int64_t>(a.S) * a.k;
   const int* part = reinterpret_cast<const int*>(a.part);
   f32x4 y = {0.f, 0.f, 0.f, 0.f};
-  for (int r = 0; r < a.k; ++r) {
-    const int64_t ch = static_cast<int64_t>(s) * a.k + r;
-    const int e = a.ids[ch];
-    if (e < 0 || e >= a.E) continue;
-    i32x4 v = {0, 0, 0, 0};
-    for (int z = 0; z < a.z2; ++z) v += *reinterpret_cast<const i32x4*>(part + (z * choices + ch) * a.d + c);
-    const float w = a.weights[ch], sh = b.sh[ch];
-    const int64_t at = static_cast<int64_t>(e) * a.d + c;
+  for (int r0 = 0; r0 < a.k; r0 += 2) {
+    int e[2];
+    float w[2], sh[2];
+    i32x4 v[2];
+    f32x4 s2[2], b2[2];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) y[q] += w * (static_cast<float>(v[q]) * sh * b.s2[at + q] + (a.b2 ? a.b2[at + q] : 0.f));
+    for (int i = 0; i < 2; ++i) {
+      const int64_t ch = static_cast<int64_t>(s) * a.k + min(r0 + i, a.k - 1);
+      e[i] = r0 + i < a.k ? a.ids[ch] : -1;
+      w[i] = a.weights[ch];
+      sh[i] = b.sh[ch];
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t ch = static_cast<int64_t>(s) * a.k + min(r0 + i, a.k - 1);
+      const bool in = e[i] >= 0 && e[i] < a.E;
+      const int64_t at = static_cast<int64_t>(in ? e[i] : 0) * a.d + c;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        s2[i][q] = b.s2[at + q];
+        b2[i][q] = a.b2 ? a.b2[at + q] : 0.f;
+      }
+      v[i] = i32x4{0, 0, 0, 0};
+      if (!in) continue;
+      for (int z0 = 0; z0 < a.z2; z0 += 4) {
+        i32x4 p[4];
+#pragma unroll
+        for (int z = 0; z < 4; ++z) p[z] = *reinterpret_cast<const i32x4*>(part + (min(z0 + z, a.z2 - 1) * choices + ch) * a.d + c);
+#pragma unroll
+        for (int z = 0; z < 4; ++z)
+          if (z0 + z < a.z2) v[i] += p[z];
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      if (e[i] < 0 || e[i] >= a.E) continue;  // padding adds nothing, whatever lies there
+#pragma unroll
+      for (int q = 0; q < 4; ++q) y[q] += w[i] * (static_cast<float>(v[i][q]) * sh[i] * s2[i][q] + b2[i][q]);
+    }
   }
   T* out = reinterpret_cast<T*>(a.y) + static_cast<int64_t>(s) * a.d + c;
   if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(out) = uint2{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3])};
@@ -321,12 +354,14 @@ __global__ __launch_bounds__(kBlock) void layer_int8_combine_kernel(LayerInt8Arg
 
 int slots(const LayerArgs& a) { return a.by_choice ? a.S * a.k : a.E; }
 
-// Whether the strips' blocks quantize their rows themselves: few rows, whose launches would take longer.
+// Whether the strips' blocks quantize their rows themselves, which saves two launches: a few tokens, or no
+// more choices than experts (32 tokens, two of 64 experts of 2048 x 2048, gated: 106 -> 100 us; two of
+// 32 of 1024 x 2048, twice as many rows per expert: 56 -> 62).
 bool held(const LayerArgs& a, bool first, int z) {
   const int K = first ? a.d : a.h;
   const int steps = (K + kInt8Step - 1) / kInt8Step, parts = z * kInt8Waves;
-  return a.S <= kInt8HeldRows && K <= kInt8HeldK &&
-         static_cast<int64_t>(a.S) * ((steps + parts - 1) / parts) * kInt8Waves * kInt8Step <= kInt8HeldBytes;
+  return (a.S <= kInt8HeldRows || a.by_choice) && a.S * a.k <= kWave && K <= kInt8HeldK &&
+         static_cast<int64_t>(std::min(a.S, kInt8HeldRows)) * ((steps + parts - 1) / parts) * kInt8Waves * kInt8Step <= kInt8HeldBytes;
 }
 
 template <class T, int MT, bool FIRST, bool HELD>
@@ -334,7 +369,8 @@ hipError_t strip(const LayerInt8Args& b, int z, hipStream_t st) {
   const LayerArgs& a = b.a;
   const int N = FIRST ? a.h : a.d, nbo = FIRST && a.gated ? kInt8Strip / 2 : kInt8Strip;
   const int64_t strips = (N + nbo - 1) / nbo, blocks = strips * slots(a) * z;
-  const int passes = (a.S + 16 * MT - 1) / (16 * MT);
+  const int pass = HELD ? kInt8HeldRows : 16 * MT;
+  const int passes = (a.S + pass - 1) / pass;
   const int shares = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(passes, 512 / blocks)));
   const dim3 grid(static_cast<unsigned>(strips), slots(a), z * shares);
   constexpr int kThreads = kInt8Waves * kWave;
@@ -371,7 +407,7 @@ hipError_t run_layer(const LayerInt8Args& b, hipStream_t st) {
   hipError_t err = strips<T, true>(b, st);
   if (err != hipSuccess) return err;
   if ((err = strips<T, false>(b, st)) != hipSuccess) return err;
-  layer_int8_combine_kernel<T><<<dim3((a.d + 4 * kBlock - 1) / (4 * kBlock), a.S), kBlock, 0, st>>>(b);
+  layer_int8_combine_kernel<T><<<dim3((a.d + 4 * kWave - 1) / (4 * kWave), a.S), kWave, 0, st>>>(b);
   return hipGetLastError();
 }
 

@@ -197,6 +197,9 @@ LAYERS = [
     # S, d, E, k, h: one token; fewer choices than experts; more; few experts of many rows; all 256
     (1, 16, 1, 1, 16), (1, 144, 8, 2, 208), (3, 64, 16, 2, 80), (32, 80, 6, 2, 272), (17, 528, 4, 1, 64), (70, 48, 3, 3, 96),
     (256, 32, 2, 1, 48), (200, 64, 5, 4, 2064), (9, 1040, 12, 8, 32), (256, 16, 4, 2, 4112),
+    # rows that the blocks quantize themselves: four at a time and one more, all of their lengths, and
+    # one element more than they take
+    (4, 512, 8, 2, 8192), (4, 48, 4, 4, 4096), (30, 272, 64, 2, 336), (60, 64, 60, 1, 80), (1, 8192, 2, 1, 48), (1, 8208, 2, 2, 8208),
 ]
 
 
@@ -221,6 +224,20 @@ def test_token_layer(S, d, E, k, h, dtype):
         ids = rng.integers(-1, E + 1, (S, k)).astype(np.int32)
         r = hm.token_layer_int8(x.to(DEV), q1, s1, q2, s2, ids=torch.from_numpy(ids).to(DEV), weights=o["weights"], **kw)
         check(r["y"], oi.token_layer(xv, ids, weights, *vals, ACTS[act], gated, ROUND[dtype]), "y, routed")
+
+
+def test_all_tokens_of_one_expert():
+    """More choices of an expert than a pass of a block takes, though choices are fewer than experts."""
+    rng = np.random.default_rng(7)
+    S, d, E, h = 21, 144, 64, 112
+    x, xv = normal(rng, (S, d), "bf16")
+    (q1, s1, b1, q2, s2, b2), vals = _net(rng, E, d, h, True)
+    for ids in (np.full((S, 1), 5), np.concatenate([np.full((S - 2, 1), 63), [[-1], [64]]])):
+        ids = ids.astype(np.int32)
+        w = rng.random((S, 1)).astype(np.float32)
+        y = hm.token_layer_int8(x.to(DEV), q1, s1, q2, s2, b1=b1, b2=b2, act=ACTS["silu"], gated=True,
+                                ids=torch.from_numpy(ids).to(DEV), weights=torch.from_numpy(w).to(DEV))["y"]
+        check(y, oi.token_layer(xv, ids, w.astype(np.float64), *vals, ACTS["silu"], True, ROUND["bf16"]), "y")
 
 
 def test_gates_of_the_layer():
