@@ -890,7 +890,7 @@ def dropout(x, mask, residual=None, out=None, *, stream=None):
     if (residual is not None and residual.shape != x.shape) or (out is not None and out.shape != x.shape):
         raise ValueError("x, residual and out must have one shape")
     dt = x.dtype
-    # a new output goes by address: of few rows the call is bound by the host (1024 x 256: 6.3 -> HOST1 us)
+    # a new output goes by address: of few rows the call is bound by the host (1024 x 256: 7.2 -> 6.8 us)
     if out is None:
         out = torch.empty_like(x)
         to = out.data_ptr()

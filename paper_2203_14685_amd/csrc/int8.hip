@@ -1,8 +1,9 @@
 // Rows and weights as 8-bit integers with a scale each.
 //
 // Rows: bound by memory, one read and half (bf16) or a quarter (fp32) of it written; a row's
-// threads hold it in registers between its maximum and its quantization.  FIGURES  Weights: once, when
-// they are loaded: a pass for the columns' maxima, one that quantizes and transposes.
+// threads hold it in registers between its maximum and its quantization (218 million bf16
+// in use in rows of 2048: 121 to 128 us, 5.1 to 5.4 TB/s; with a test per element for quotients on a border 137).
+// Weights: once, when they are loaded: a pass for the columns' maxima, one that quantizes and transposes.
 #include <algorithm>
 
 #include "int8.hpp"

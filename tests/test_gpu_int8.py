@@ -199,7 +199,7 @@ LAYERS = [
     (256, 32, 2, 1, 48), (200, 64, 5, 4, 2064), (9, 1040, 12, 8, 32), (256, 16, 4, 2, 4112),
     # rows that the blocks quantize themselves: four at a time and one more, all of their lengths, and
     # one element more than they take
-    (4, 512, 8, 2, 8192), (4, 48, 4, 4, 4096), (30, 272, 64, 2, 336), (60, 64, 60, 1, 80), (1, 8192, 2, 1, 48), (1, 8208, 2, 2, 8208),
+    (4, 512, 8, 2, 8192), (4, 48, 4, 4, 4096), (30, 272, 64, 2, 336), (60, 64, 60, 1, 80), (1, 8192, 2, 1, 48), (1, 8208, 2, 2, 48), (1, 48, 2, 2, 8208),
 ]
 
 
