@@ -79,7 +79,8 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   constexpr int MT = BM / WM / 16, NT = BN / WN / 16, NP = NT / 2;
   static_assert(NT == 4, "64 columns per wave");
   constexpr bool kInt8 = expert_int8(EPI);
-  constexpr bool kScratch = kInt8 && expert_acts(EPI);  // nothing reads hidden behind the rows in use
+  // 8-bit integers: nothing reads hidden behind the rows in use, and those of ye are cleared before
+  constexpr bool kNoClear = kInt8;
   // columns of the output per block and wave: with GATED in the forward product half of
   // them are the gate's, half the other factor's, 32 and 32 of each wave's 64
   constexpr bool kSplit = expert_acts(EPI) && GATED;
@@ -266,7 +267,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   }
   // the tiles without work that this block clears
   int idle = blockIdx.x;
-  if (!work && (kScratch || !tiles.clear(a, idle, at))) return;
+  if (!work && (kNoClear || !tiles.clear(a, idle, at))) return;
   for (;;) {
   bool more = false;
 #pragma unroll
@@ -547,7 +548,7 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   if (work) expert_stage_barrier();  // nothing is on its way to LDS when the block ends
   else idle += gridDim.x;
   work = false;
-  if (kScratch || !tiles.clear(a, idle, at)) return;
+  if (kNoClear || !tiles.clear(a, idle, at)) return;
   }
 }
 

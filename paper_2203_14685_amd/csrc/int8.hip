@@ -54,7 +54,13 @@ __global__ __launch_bounds__(kBlock) void quantize_rows_kernel(QuantArgs a) {
 #pragma unroll
     for (int w = 0; w < kWavesPerBlock; ++w) most = max(most, wave_most[w]);
   }
-  if (!in) return;
+  if (!in) {
+    if (a.clear && row < a.rows) {
+      u32x4* p = reinterpret_cast<u32x4*>(static_cast<char*>(a.clear) + row * a.clear_bytes);
+      for (int i = lane; i < a.clear_bytes / 16; i += TPR) p[i] = u32x4{0, 0, 0, 0};
+    }
+    return;
+  }
   const Quantizer quant(most);
   int8_t* out = a.q + row * a.n;
   auto put = [&](const u32x4 (&v)[N], int p) __attribute__((always_inline)) {

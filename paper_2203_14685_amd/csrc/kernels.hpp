@@ -294,6 +294,8 @@ struct QuantArgs {
   const void* x;
   int8_t* q;
   float* scale;
+  void* clear;              // rows of clear_bytes (whole 16-byte pieces) to zero behind the counts, or null
+  int clear_bytes;
 };
 hipError_t launch_quantize(const QuantArgs& a, hipStream_t st);
 hipError_t launch_quantize_weights(int E, int K, int N, int dtype, const void* w, int8_t* q, float* scale, hipStream_t st);
