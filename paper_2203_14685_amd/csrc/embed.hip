@@ -489,6 +489,7 @@ hipError_t run_bwd(const EmbedArgs& a, hipStream_t st) {
 // Sorted tokens per chunk: so that about 4096 waves' worth of chunks and strips run, 8 at least.  (65536
 // tokens of 8 KB by Zipf's law: 16384 waves leave 19 us of parts to join, 4096 leave 8.)
 int embed_chunk_length(int T, int d, int dtype) {
+  if (T <= 32) return 32;  // no parts to join
   const int64_t row = static_cast<int64_t>(d) * (dtype == 1 ? 2 : 4);
   const int64_t want = T * std::max<int64_t>(row, 128) / 1024 / 4096;
   int n = 8;
