@@ -624,7 +624,7 @@ MOE_API moe_status moe_embed_bwd_workspace_size(const moe_embed_params* p, size_
 /*
  * moe_embed_bwd -- gradient of moe_embed:
  *   dtable[v,:] = [dtable[v,:] if accumulate] + scale * sum over t with ids[t] == v of dy[t,:]
- * Sums are fp32 in a fixed order that depends on ids alone (tokens are sorted by id; no
+ * Sums are fp32 in a fixed order that the ids and sizes decide (tokens are sorted by id; no
  * floating-point atomics): bitwise reproducible.  Rounded once.  Rows that no token names
  * become zero, with accumulate they are neither read nor written.
  *
@@ -690,7 +690,8 @@ MOE_API moe_status moe_experts_dropout_bwd(const moe_experts_params* p, const mo
  * a row of zeros has scale 0 and zeros; one that holds an infinity or a NaN has scale NaN
  * and zeros.
  *
- * Inputs   x [rows, n] (dtype), n a multiple of 16.   Outputs  q [rows, n] int8, scale [rows].
+ * Inputs   x [rows, n] (dtype), n a multiple of 16, rows up to 2^32.   Outputs  q [rows, n] int8,
+ *          scale [rows].
  * x and q 16-byte aligned.
  */
 MOE_API moe_status moe_quantize(int64_t rows, int32_t n, int32_t dtype, const void* x, int8_t* q, float* scale,

@@ -1413,7 +1413,7 @@ moe_status moe_quantize(int64_t rows, int32_t n, int32_t dtype, const void* x, i
   if (dtype != MOE_F32 && dtype != MOE_BF16) return fail(MOE_ERR_INVALID_ARG, "%s: dtype %d unknown", who, dtype);
   if (rows < 0 || n < 1) return fail(MOE_ERR_INVALID_ARG, "%s: need rows >= 0 and n >= 1, got %lld and %d", who, static_cast<long long>(rows), n);
   if (n % 16 != 0) return fail(MOE_ERR_UNSUPPORTED, "%s: rows of n = %d elements, a multiple of 16 is required", who, n);
-  if (rows > (int64_t(1) << 36)) return fail(MOE_ERR_UNSUPPORTED, "%s: more than 2^36 rows", who);
+  if (rows > (int64_t(1) << 32)) return fail(MOE_ERR_UNSUPPORTED, "%s: more than 2^32 rows", who);
   CHECK(need(x, rows, 16, who, "x"));
   CHECK(need(q, rows, 16, who, "q"));
   CHECK(need(scale, rows, 4, who, "scale"));

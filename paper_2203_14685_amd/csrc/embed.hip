@@ -387,7 +387,7 @@ __global__ __launch_bounds__(kBlock) void embed_sums_kernel(EmbedArgs a) {
 }
 
 // The runs that cross chunks: the parts are added by the block's waves, every kJoinWaves-th
-// each, then over the waves, in an order that the ids alone decide.
+// each, then over the waves, in an order that the ids and sizes decide.
 constexpr int kJoinWaves = 8;
 template <class T>
 __global__ __launch_bounds__(kJoinWaves* kWave) void embed_join_kernel(EmbedArgs a) {

@@ -111,7 +111,7 @@ def test_bad_quantize_calls(lib):
     assert q(4, 16, 1, None, A, A, None) == INVALID and q(4, 16, 1, A, None, A, None) == INVALID
     assert q(4, 16, 1, A, A, None, None) == INVALID and q(4, 16, 1, A + 8, A, A, None) == UNSUPPORTED
     assert q(4, 16, 1, A, A + 8, A, None) == UNSUPPORTED and q(4, 16, 1, A, A, A + 2, None) == INVALID
-    assert q((1 << 36) + 1, 16, 1, A, A, A, None) == UNSUPPORTED
+    assert q((1 << 32) + 1, 16, 1, A, A, A, None) == UNSUPPORTED
     assert q(0, 16, 1, None, None, None, None) == b.MOE_OK
     w = lib.moe_quantize_weights
     assert w(0, 16, 16, 1, A, A, A, None) == INVALID and w(1025, 16, 16, 1, A, A, A, None) == INVALID

@@ -197,6 +197,9 @@ def test_experts_drop_what_rows_drop(dtype, gated, big):
     # two roundings of hidden and one product on either side
     assert (np.abs(got - want) <= (2 * ROUND[dtype] + ROUND[dtype] ** 2 + 4 * 2.0 ** -24) * np.abs(want)).all()
     zero = hm.dropout_mask(0.0, 21, 4)
+    z = hm.experts(xe, w1, w2, b1=b1, b2=b2, want_pre=True, dropout=hm.dropout_mask(1.0, 21, 4), **kw)
+    assert not z["hidden"].any() and torch.equal(z["pre"], plain["pre"])  # all dropped: the bias is what remains
+    assert (f64(z["ye"]) == f64(b2.to(TORCH[dtype]))[:, None, :]).all()
     z = hm.experts(xe, w1, w2, b1=b1, b2=b2, want_pre=True, dropout=zero, **kw)
     for key in ("pre", "hidden", "ye"):
         assert torch.equal(z[key], plain[key])

@@ -147,6 +147,28 @@ def test_large_tiles(dtype, gated):
             check(y[e:e + 1], ref, f"ye of expert {e}")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("E,C,d,h,gated", [(16, 512, 272, 2064, True), (16, 512, 272, 4112, False), (32, 512, 2064, 272, False)])
+def test_tiles_of_256(E, C, d, h, gated, dtype):
+    """The first product and the second in tiles of 256 x 256 cut short along K and N, with their last
+    round in quarters; all rows in use, and some."""
+    rng = np.random.default_rng(C + h)
+    xe, xv = normal(rng, (E, C, d), dtype)
+    (q1, s1, b1, q2, s2, b2), vals = _net(rng, E, d, h, gated)
+    for counts in (None, rng.integers(0, C + 1, E).astype(np.int32)):
+        announce(f"experts_int8 256 {dtype} E={E} C={C} d={d} h={h} gated={gated} counts={counts is not None}")
+        ye = torch.full((E, C, d), float("nan"), dtype=TORCH[dtype], device=DEV)
+        params = hm.experts_params(E, C, d, h, ACTS["silu"], gated, hm.MOE_BF16 if dtype == "bf16" else hm.MOE_F32)
+        ws = torch.full((hm.moe_experts_int8_workspace_size(params),), 0xff, dtype=torch.uint8, device=DEV)
+        cd = None if counts is None else torch.from_numpy(counts).to(DEV)
+        hm.moe_experts_int8(params, xe.to(DEV), q1, s1, b1, q2, s2, b2, cd, ye, ws)
+        for e in (0, E // 2, E - 1):
+            ref = oi.experts(xv[e:e + 1], *[v[e:e + 1] for v in vals], None if counts is None else counts[e:e + 1], ACTS["silu"],
+                             gated, ROUND[dtype])
+            check(ye[e:e + 1], ref, f"ye of expert {e}")
+        assert torch.isfinite(ye).all()
+
+
 def test_exact_sums():
     """Sums up to 2^31: all integers 127, K = 2^17; and alternating signs that cancel."""
     d, h = 1 << 17, 16
