@@ -12,6 +12,7 @@
 #include "experts.hpp"
 #include "int8.hpp"
 #include "layer_choices.hpp"
+#include "layer_int8_rows.hpp"
 
 namespace hetumoe {
 
@@ -19,15 +20,10 @@ namespace {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kInt8Waves = 4;
 constexpr int kInt8Tiles = 4;                  // of 16 rows of the matrix per block
 constexpr int kInt8Strip = 16 * kInt8Tiles;
-constexpr int kInt8Step = 256;                 // K of one stage: bytes of a row that are read together
 constexpr int kInt8Stage = 16 * kInt8Step;     // bytes of a stage: 16 rows, four loads to LDS
 constexpr int kInt8Ring = 4;                   // stages of a wave
-// Rows that a block quantizes itself: 4 at a time of at most 8192 elements, the bytes of its range of K in
-// LDS beside the rings of two blocks.
-constexpr int kInt8HeldRows = 4, kInt8HeldK = 8192, kInt8HeldBytes = 12 * 1024;
 
 // A wave's stages come straight to its own part of LDS, 16 rows x 256 bytes each, so that memory is
 // read in whole stretches (40 experts of 4096 rows of 2048 bytes: 6.9 TB/s non-temporal; with
@@ -215,18 +211,20 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
   e = __builtin_amdgcn_readfirstlane(e);
   n = __builtin_amdgcn_readfirstlane(n);
   const int share = blockIdx.z % shares, z = blockIdx.z / shares, zs = gridDim.z / shares;
-  constexpr int kPass = HELD ? kInt8HeldRows : 16 * MT;  // rows at a time
-  if (n <= kPass * share) return;
+  const int K = FIRST ? a.d : a.h;
+  const int per = layer_int8_steps(K, zs), first = z * kInt8Waves * per;
+  const int bytes = layer_int8_row_bytes(K, zs);               // HELD: of a row, from step `first` on
+  const int pass = HELD ? layer_int8_held_rows(bytes) : 16 * MT;  // rows at a time
+  if (n <= pass * share) return;
 
-  const int K = FIRST ? a.d : a.h, N = FIRST ? a.h : a.d, N1 = kSplit ? 2 * N : N;
+  const int N = FIRST ? a.h : a.d, N1 = kSplit ? 2 * N : N;
   const int n0 = blockIdx.x * NBO;
   const int8_t* w = reinterpret_cast<const int8_t*>(FIRST ? a.w1 : a.w2) + (static_cast<int64_t>(e) * N1 + n0) * K;
   // rows of the matrix behind N: zeros
   const int half = kSplit ? NBO : NBO / 2;
   const int64_t apart = static_cast<int64_t>(kSplit ? N : half) * K;
   const int v0 = min(half, N - n0), v1 = kSplit ? v0 : max(0, min(half, N - n0 - half));
-  const int steps = (K + kInt8Step - 1) / kInt8Step, parts = zs * kInt8Waves;
-  const int per = (steps + parts - 1) / parts, first = z * kInt8Waves * per;
+  const int steps = (K + kInt8Step - 1) / kInt8Step;
   Int8Sums<MT, HELD> sums;
   sums.w0 = expert_rsrc(w, __builtin_amdgcn_readfirstlane(v0 * K));
   sums.w1 = expert_rsrc(w + apart, __builtin_amdgcn_readfirstlane(v1 * K));
@@ -236,10 +234,10 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
   sums.hi = min(steps, sums.lo + per);
   sums.ring = ring[wave];
 
-  for (int r0 = kPass * share; r0 < n; r0 += kPass * shares) {
+  for (int r0 = pass * share; r0 < n; r0 += pass * shares) {
+    const int end = min(n, r0 + pass);
     if constexpr (HELD) {
-      const int bytes = kInt8Waves * per * kInt8Step;  // of a row, from step `first` on
-      const int held = min(kPass, n - r0);
+      const int held = end - r0;
       for (int r = 0; r < held; ++r) {
         const int64_t row = __builtin_amdgcn_readfirstlane(FIRST ? list[r0 + r] / a.k : list[r0 + r]);
         const float scale = int8_hold(reinterpret_cast<const T*>(FIRST ? a.x : a.hidden) + row * K, K, first * kInt8Step, bytes,
@@ -268,7 +266,7 @@ __global__ __launch_bounds__(kInt8Waves* kWave, 2) void layer_int8_kernel(LayerI
       __syncthreads();
       for (int o = tid; o < (HELD ? kInt8HeldRows : 16) * NBO; o += kThreads) {
         const int row = o / NBO, c = o % NBO, li = r0 + 16 * i + row;
-        if (li >= n || n0 + c >= N) continue;
+        if (li >= end || n0 + c >= N) continue;
         int v = 0, u = 0;
 #pragma unroll
         for (int q = 0; q < kInt8Waves; ++q) {
@@ -358,10 +356,8 @@ int slots(const LayerArgs& a) { return a.by_choice ? a.S * a.k : a.E; }
 // more choices than experts (32 tokens, two of 64 experts of 2048 x 2048, gated: 106 -> 100 us; two of
 // 32 of 1024 x 2048, twice as many rows per expert: 56 -> 62).
 bool held(const LayerArgs& a, bool first, int z) {
-  const int K = first ? a.d : a.h;
-  const int steps = (K + kInt8Step - 1) / kInt8Step, parts = z * kInt8Waves;
-  return (a.S <= kInt8HeldRows || a.by_choice) && a.S * a.k <= kWave && K <= kInt8HeldK &&
-         static_cast<int64_t>(std::min(a.S, kInt8HeldRows)) * ((steps + parts - 1) / parts) * kInt8Waves * kInt8Step <= kInt8HeldBytes;
+  static_assert(kWave == 64, "a wave lists all choices");
+  return layer_int8_held(a.S, a.k, a.by_choice != 0, first ? a.d : a.h, z);
 }
 
 template <class T, int MT, bool FIRST, bool HELD>
@@ -369,7 +365,7 @@ hipError_t strip(const LayerInt8Args& b, int z, hipStream_t st) {
   const LayerArgs& a = b.a;
   const int N = FIRST ? a.h : a.d, nbo = FIRST && a.gated ? kInt8Strip / 2 : kInt8Strip;
   const int64_t strips = (N + nbo - 1) / nbo, blocks = strips * slots(a) * z;
-  const int pass = HELD ? kInt8HeldRows : 16 * MT;
+  const int pass = HELD ? layer_int8_held_rows(layer_int8_row_bytes(FIRST ? a.d : a.h, z)) : 16 * MT;
   const int passes = (a.S + pass - 1) / pass;
   const int shares = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(passes, 512 / blocks)));
   const dim3 grid(static_cast<unsigned>(strips), slots(a), z * shares);
