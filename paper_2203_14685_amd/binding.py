@@ -258,8 +258,15 @@ def _stream(stream):
     return getattr(stream, "cuda_stream", stream)
 
 
+def _sizes(*sizes):
+    """Refuses sizes past 32 bits, of which ctypes would keep the low ones without a word."""
+    if max(sizes) > 0x7FFFFFFF:
+        raise ValueError(f"a size of {max(sizes)} is past 2^31 - 1")
+
+
 def gate_params(S, d, E, k, capacity, kind, normalize=0, logits_in=0, dtype=MOE_F32, hash_seed=0, groups=0,
                 temperature=0.0, hash_vocab=0):
+    _sizes(S, d, E, k, capacity, hash_vocab)
     return GateParams(S, d, E, k, capacity, kind, normalize, logits_in, dtype, groups, hash_seed, temperature,
                       hash_vocab)
 
@@ -586,6 +593,7 @@ def gate_bwd(kind, logits, ids, dw, *, x=None, wg=None, normalize=0, dx=None, ac
 # ---------------------------------------------------------------- expert networks
 
 def experts_params(E, capacity, d, h, act=MOE_ACT_RELU, gated=False, dtype=MOE_F32):
+    _sizes(E, capacity, d, h)
     return ExpertsParams(E, capacity, d, h, act, int(bool(gated)), dtype)
 
 
@@ -735,6 +743,7 @@ def experts_bwd(dye, xe, w1, w2, pre, hidden, *, counts=None, act=MOE_ACT_RELU, 
 
 def token_layer_params(S, d, E, k, h, kind=MOE_GATE_TOPK, act=MOE_ACT_RELU, gated=False, dtype=MOE_F32, normalize=0,
                        routed=False, groups=0, hash_seed=0, temperature=0.0, hash_vocab=0):
+    _sizes(h)
     return TokenLayerParams(gate_params(S, d, E, k, 0, kind, normalize, 0, dtype, hash_seed, groups, temperature,
                                         hash_vocab), h, act, int(bool(gated)), int(bool(routed)))
 
@@ -904,6 +913,7 @@ def dropout(x, mask, residual=None, out=None, *, stream=None):
 # ---------------------------------------------------------------- embedding rows
 
 def embed_params(T, V, d, dtype=MOE_F32, scale=1.0, accumulate=False):
+    _sizes(T, V, d)
     return EmbedParams(T, V, d, dtype, scale, int(bool(accumulate)))
 
 
@@ -931,8 +941,10 @@ def embed(ids, table, scale=1.0, *, stream=None):
     """scale * table[ids] for int32 ids of any shape; zero rows where an id is outside the
     table (padding)."""
     V, d = table.shape
+    T = ids.numel()
+    _sizes(T, V, d)
     y = table.new_empty((*ids.shape, d))  # goes by address, as in dropout
-    _check(load().moe_embed(EmbedParams(ids.numel(), V, d, _dtype_code(table), scale, 0), _ptr(ids, torch.int32, "ids"),
+    _check(load().moe_embed(EmbedParams(T, V, d, _dtype_code(table), scale, 0), _ptr(ids, torch.int32, "ids"),
                             _ptr(table, None, "table"), y.data_ptr(), _stream(stream)))
     return y
 
@@ -946,7 +958,7 @@ def embed_bwd(dy, ids, V, scale=1.0, dtable=None, accumulate=False, *, stream=No
         raise ValueError(f"dy {tuple(dy.shape)} and ids {tuple(ids.shape)} do not go together")
     if accumulate and dtable is None:
         raise ValueError("accumulate needs a dtable to add to")
-    params = EmbedParams(ids.numel(), V, d, _dtype_code(dy), scale, int(bool(accumulate)))
+    params = embed_params(ids.numel(), V, d, _dtype_code(dy), scale, accumulate)
     n = ctypes.c_size_t(0)
     lib = load()
     _check(lib.moe_embed_bwd_workspace_size(params, n))
@@ -966,11 +978,13 @@ def embed_bwd(dy, ids, V, scale=1.0, dtable=None, accumulate=False, *, stream=No
 # ---------------------------------------------------------------- 8-bit integers
 
 def moe_quantize(rows, n, dtype, x, q, scale, stream=None):
+    _sizes(n)
     _check(load().moe_quantize(rows, n, dtype, _ptr(x, _dt(dtype), "x", rows * n), _ptr(q, torch.int8, "q", rows * n),
                                _ptr(scale, torch.float32, "scale", rows), _stream(stream)))
 
 
 def moe_quantize_weights(E, K, N, dtype, w, q, scale, stream=None):
+    _sizes(E, K, N)
     _check(load().moe_quantize_weights(E, K, N, dtype, _ptr(w, _dt(dtype), "w", E * K * N),
                                        _ptr(q, torch.int8, "q", E * K * N), _ptr(scale, torch.float32, "scale", E * N),
                                        _stream(stream)))
@@ -1031,7 +1045,7 @@ def experts_int8(xe, q1, s1, q2, s2, *, b1=None, b2=None, counts=None, act=MOE_A
     E_, h = _int8_shapes(q1, q2, d, gated)
     if E_ != E:
         raise ValueError(f"xe has {E} experts, the weights {E_}")
-    params = ExpertsParams(E, C, d, h, act, int(bool(gated)), _dtype_code(xe))
+    params = experts_params(E, C, d, h, act, gated, _dtype_code(xe))
     n = ctypes.c_size_t(0)
     lib = load()
     _check(lib.moe_experts_int8_workspace_size(params, n))
