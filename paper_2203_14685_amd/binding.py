@@ -623,6 +623,15 @@ def _allocates_on_stream(fn):
     return run
 
 
+def _mask(mask):
+    """The mask, its step checked like every tensor of the call: a mask may outlive the device that
+    was current when it was made."""
+    step = getattr(mask, "step_tensor", None)
+    if step is not None:
+        _ptr(step, None, "step", 1)
+    return mask
+
+
 def _masked(call, mask, params, *args):
     return call(params, mask, *args)
 
@@ -646,7 +655,7 @@ def moe_experts(params, xe, w1, b1, w2, b2, counts, pre, hidden, ye, stream=None
 
 
 def moe_experts_dropout(params, mask, xe, w1, b1, w2, b2, counts, pre, hidden, ye, stream=None):
-    _check(load().moe_experts_dropout(ctypes.byref(params), ctypes.byref(mask),
+    _check(load().moe_experts_dropout(ctypes.byref(params), ctypes.byref(_mask(mask)),
                                       *_experts_pointers(params, xe, w1, b1, w2, b2, counts, pre, hidden, ye),
                                       _stream(stream)))
 
@@ -677,7 +686,7 @@ def moe_experts_bwd(params, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1,
 def moe_experts_dropout_bwd(params, mask, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace,
                             stream=None):
     _check(load().moe_experts_dropout_bwd(
-        ctypes.byref(params), ctypes.byref(mask),
+        ctypes.byref(params), ctypes.byref(_mask(mask)),
         *_experts_bwd_pointers(params, dye, xe, w1, w2, counts, pre, hidden, dxe, dw1, db1, dw2, db2, workspace),
         _stream(stream)))
 
@@ -888,7 +897,7 @@ def dropout_mask(p, seed, call=0, step=None):
 
 def moe_dropout(mask, n, dtype, x, residual, y, stream=None):
     dt = _dt(dtype)
-    _check(load().moe_dropout(ctypes.byref(mask), n, dtype, _ptr(x, dt, "x", n), _ptr(residual, dt, "residual", n),
+    _check(load().moe_dropout(ctypes.byref(_mask(mask)), n, dtype, _ptr(x, dt, "x", n), _ptr(residual, dt, "residual", n),
                               _ptr(y, dt, "y", n), _stream(stream)))
 
 
@@ -905,7 +914,7 @@ def dropout(x, mask, residual=None, out=None, *, stream=None):
         to = out.data_ptr()
     else:
         to = _ptr(out, dt, "out")
-    _check(load().moe_dropout(mask, x.numel(), _dtype_code(x), _ptr(x, None, "x"), _ptr(residual, dt, "residual"), to,
+    _check(load().moe_dropout(_mask(mask), x.numel(), _dtype_code(x), _ptr(x, None, "x"), _ptr(residual, dt, "residual"), to,
                               _stream(stream)))
     return out
 
