@@ -2,11 +2,14 @@
 //
 // Forward: a gather of rows, bound by the rows written.  Backward: the tokens are sorted by id
 // (stable, so that every sum runs over its tokens in their order), then the rows' gradients are
-// added in runs of equal ids: the sorted tokens are cut into chunks of equal length, however
-// the ids are spread, one group of lanes per chunk and strip of columns.  A run inside one chunk is
-// written at once; the parts of a run that crosses chunks go to the workspace and are added
-// by a last launch.  The table is cleared beside the sorting, whose few blocks wait for one
-// another most of the time; rows in use are written again later, which is less than to find the others.
+// added in runs of equal ids: the sorted tokens are cut into chunks of equal length, one group of lanes
+// per chunk and strip of columns, so the first sums take as long however the ids are spread.  A run
+// inside one chunk is written at once; the parts of a run that crosses chunks go to the workspace and
+// are added by a last launch, one block per run and strip, whose time does grow with the longest run's parts
+// (262144 rows of 64 bf16, chunks of 8: 476 us with a run of 101073, 159 with even ids; 65536 rows of
+// 512: 118 with one id on half of them, 71; of 4096 with a tenth on one: 8 of 205).  The table is cleared
+// beside the sorting, whose few blocks wait for one another most of the time; rows in use are written
+// again later, which is less than to find the others.
 #include <algorithm>
 
 #include "common.hpp"

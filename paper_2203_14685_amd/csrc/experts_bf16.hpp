@@ -349,7 +349,9 @@ __global__ __launch_bounds__(WM* WN * 64) void experts_gemm_bf16_kernel(ExpertGe
   if constexpr (expert_drops(EPI)) call = drop_call(a.drop);
   // dropout's words of 8 columns from c on of row lrow + 16 i of hidden: one generator call for the lane's
   // store.  (First product of 16 x 1280 x 1024 x 4096: 193 us, without dropout 169; drawn between the
-  // products, each turn by half of the waves, 218; a call per stage 188, for state that is not worth it.)
+  // products, each turn by half of the waves, 218; a call per stage 188, for state that is not worth it.
+  // The gradient's product draws them again: backward pass of that size 591 us, without dropout 565;
+  // gated, by a loop for the registers' sake, 1063 and 1027.)
   auto words = [&](int i, int c) {
     return philox<expert_act_grads(EPI) && GATED ? 1 : 10>(
         a.drop, call, static_cast<uint64_t>((static_cast<int64_t>(e) * a.C + m0 + lrow + 16 * i) * a.N + c) >> 3);

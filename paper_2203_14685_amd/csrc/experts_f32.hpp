@@ -214,7 +214,8 @@ __global__ __launch_bounds__(WM* WN* KG * 64, BM == 128 ? 2 : 4) void experts_ge
   auto value = [&](int i, int r, int q) { return sum[i][(4 * r + q) % NT][(4 * r + q) / NT]; };
   uint64_t call = 0;
   if constexpr (expert_drops(EPI)) call = drop_call(a.drop);
-  // dropout's words of columns c .. c + 3 of a row of hidden: one half of a block's
+  // dropout's words of columns c .. c + 3 of a row of hidden: one half of a block's, so each call is made
+  // twice (the other half lies with another lane)
   auto words = [&](int row, int c) {
     const uint64_t i = static_cast<uint64_t>((static_cast<int64_t>(e) * a.C + row) * a.N + c);
     const u32x4 w = philox(a.drop, call, i >> 3);
