@@ -8,9 +8,6 @@ import torch
 import paper_2203_14685_amd as hm
 from paper_2203_14685_amd import binding as b
 
-if torch.cuda.is_available():
-    pytest.skip("stand-ins for GPU tensors: only where no call can reach a GPU", allow_module_level=True)
-
 
 class _OnGpu(torch.Tensor):
     is_cuda = True
@@ -24,6 +21,7 @@ def _on(index, *shape, dtype=torch.float32):
     return t
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="stand-ins for GPU tensors: only where no call can reach a GPU")
 def test_step_of_another_device(monkeypatch):
     now = [0]
     monkeypatch.setattr(b, "_multi_gpu", True)
